@@ -46,9 +46,14 @@
  * the context's workspace.  Distinct contexts are independent.  A context belongs to the device
  * that was current when it was created: forward, forward_host and query_status return
  * SLIDE_ATTN_ERR_INVALID_ARG, before launching anything, when another device is current.
+ *
+ * Beside that forward and what belongs to a context stand operators that take sizes instead of one (group norm, dropout,
+ * block-sparse attention; at the end of this file).
  */
 #ifndef SLIDE_ATTN_H_
 #define SLIDE_ATTN_H_
+
+#include <stddef.h>
 
 #ifdef __cplusplus
 extern "C" {
@@ -310,6 +315,144 @@ slide_attn_status slide_attn_forward_noalloc(const void* q, const void* k, const
  */
 slide_attn_status slide_attn_profile_begin(slide_attn_ctx* ctx);
 slide_attn_status slide_attn_profile_end(slide_attn_ctx* ctx, double* forward_ms, double* main_ms, int* n);
+
+/* ==================================================================================================
+ * Operators around and beside the local attention: what a residual block of a network of these maps
+ * needs when it is trained (group norm ahead of the projections, dropout behind them), and attention
+ * that reaches further than a k x k window.
+ *
+ * They take sizes instead of a context and own nothing.  Tensors are dense, DEVICE memory of the
+ * current device, 16-byte aligned (rng: 8); maps have the element type `dtype`, everything else is as
+ * declared.  Scratch memory, where one is needed, is the caller's `workspace` (16-byte aligned, at least
+ * as many bytes as the function ..._workspace says; its contents need not be kept or set between calls).
+ * A workspace belongs to one call at a time: calls that may overlap on the GPU, and graphs that may be
+ * replayed side by side, need one each.  Every call is asynchronous on `cuda_stream`, allocates nothing,
+ * may be captured into a graph, and gives the same bits every time.  Arguments are checked on the host
+ * before anything is launched; a workspace that is missing or too small is SLIDE_ATTN_ERR_INVALID_ARG.
+ * Outputs may not be inputs unless that is said.
+ * ================================================================================================== */
+
+typedef enum {
+    SLIDE_ATTN_ACT_NONE = 0,
+    SLIDE_ATTN_ACT_SILU = 1,    /* z / (1 + exp(-z))             */
+    SLIDE_ATTN_ACT_GELU = 2     /* z (1 + erf(z / sqrt 2)) / 2   */
+} slide_attn_activation;
+
+/*
+ * Group norm with an activation over channels-last maps.  For every image b and group g of C / groups
+ * neighbouring channels, over the group's H * W * C / groups values:
+ *     mean = average of x,  rstd = 1 / sqrt(average of (x - mean)^2 + eps)
+ *     y    = act((x - mean) * rstd * gamma[c] + beta[c])
+ *   x, y         [in / out] [B][H][W][C]
+ *   gamma, beta  [in]  float [C], each may be NULL (ones, zeros)
+ *   mean, rstd   [out] float [B][groups]: what the backward takes
+ * Arithmetic is fp32 (the variance from deviations from the mean, so that a large mean costs nothing);
+ * y is rounded to the dtype once.  Supported: C a multiple of 8 and of groups; whole groups that share
+ * 16-byte pieces of a pixel at most 4096 (bf16) or 2048 (fp32) channels wide; eps >= 0.
+ */
+slide_attn_status slide_attn_group_norm_forward(const void* x, const float* gamma, const float* beta,
+                                                void* y, float* mean, float* rstd,
+                                                int B, int H, int W, int C, int groups, float eps,
+                                                slide_attn_activation act, slide_attn_dtype dtype,
+                                                void* cuda_stream);
+
+/*
+ * Its gradients for dy = d(loss)/d(y):
+ *   x, gamma, beta, mean, rstd  [in] what the forward was given and gave
+ *   dy, dx         [in / out] [B][H][W][C]
+ *   dgamma, dbeta  [out] float [C], overwritten; both or neither may be NULL
+ *   workspace      slide_attn_group_norm_workspace bytes; not used, and may be NULL, without dgamma
+ */
+slide_attn_status slide_attn_group_norm_backward(const void* x, const float* gamma, const float* beta,
+                                                 const float* mean, const float* rstd, const void* dy,
+                                                 void* dx, float* dgamma, float* dbeta,
+                                                 int B, int H, int W, int C, int groups,
+                                                 slide_attn_activation act, slide_attn_dtype dtype,
+                                                 void* workspace, size_t workspace_bytes, void* cuda_stream);
+slide_attn_status slide_attn_group_norm_workspace(int B, int H, int W, int C, int groups,
+                                                  slide_attn_dtype dtype, size_t* bytes);
+
+typedef enum {
+    SLIDE_ATTN_DROP_ELEMENTS = 0,   /* each element is dropped by itself                           */
+    SLIDE_ATTN_DROP_IMAGES   = 1    /* all of an image or nothing of it (stochastic depth)         */
+} slide_attn_drop_unit;
+
+/*
+ * Dropout with a residual, from a counter-based generator; the mask is never stored:
+ *     y = residual + (kept ? x / (1 - p) : 0)
+ *   x, y       [in / out] `images` times `per_image` elements; y may be x or residual
+ *   residual   [in]  the same, or NULL (zeros)
+ *   p          0 <= p <= 1; with p = 1 nothing is kept
+ *   rng        [in, DEVICE] two unsigned 64-bit integers: seed and offset.  They are read when the call
+ *              runs on the GPU, so that a captured graph draws new masks when its caller changes them; the
+ *              call does not.  Calls with the same two draw the same mask.
+ * Element e (unit ELEMENTS) or image e (unit IMAGES) is kept if word e % 4 of Philox4x32 with ten rounds, at
+ * the counter (e / 4 low, e / 4 high, offset low, offset high) under the key (seed low, seed high), is at
+ * least floor(p * 2^32).  What a dropped x holds, an infinity or a NaN too, does not matter.
+ */
+slide_attn_status slide_attn_dropout_forward(const void* x, const void* residual, void* y,
+                                             long long images, long long per_image, float p,
+                                             slide_attn_drop_unit unit, const void* rng,
+                                             slide_attn_dtype dtype, void* cuda_stream);
+
+/* Its gradient dx = kept ? dy / (1 - p) : 0, from the same rng; dx may be dy.  (The residual's is dy.) */
+slide_attn_status slide_attn_dropout_backward(const void* dy, void* dx, long long images, long long per_image,
+                                              float p, slide_attn_drop_unit unit, const void* rng,
+                                              slide_attn_dtype dtype, void* cuda_stream);
+
+/*
+ * Block-sparse attention.  The map is cut into blocks of block_h x block_w pixels, smaller at the right and
+ * lower edges where these do not divide it, numbered row by row; there are
+ * blocks = ceil(H / block_h) * ceil(W / block_w).  Every block of queries has, head by head, a list of `top`
+ * blocks, and its queries attend to all pixels of the listed blocks.  A sequence of n tokens is a map with
+ * H = 1, W = n.
+ * Supported: head_dim 16, 32 or 64; block edges up to 32; up to 1024 blocks; top up to 64.
+ *
+ * slide_attn_select_blocks fills the lists by a score of pooled queries and keys,
+ *     score(r, s) = sum over d of (sum of q over block r)[d] * (mean of k over block s)[d]
+ * with the `top` <= blocks largest, the largest first; equal scores in the order of their numbers, a NaN
+ * counted as -infinity.  Sums and scores are fp64.
+ *   q, k   [in]  [B][H][W][heads][head_dim]
+ *   idx    [out] int [B][heads][blocks][top]
+ */
+slide_attn_status slide_attn_select_blocks(const void* q, const void* k, int* idx,
+                                           int B, int H, int W, int heads, int head_dim,
+                                           int block_h, int block_w, int top, slide_attn_dtype dtype,
+                                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+slide_attn_status slide_attn_select_workspace(int B, int H, int W, int heads, int head_dim,
+                                              int block_h, int block_w, size_t* bytes);
+
+/*
+ *     out = softmax over the listed pixels of (q . k / sqrt(head_dim)), times v
+ *     lse = log of the softmax's sum of exp(q . k / sqrt(head_dim)): what the backward takes
+ *   q, k, v, out  [in / out] [B][H][W][heads][head_dim]
+ *   idx           [in]  int [B][heads][blocks][top], any `top` (not only slide_attn_select_blocks' result).
+ *                 Entries that are no block (below 0, or `blocks` and above) are left out; a block that is
+ *                 listed twice counts twice.
+ *   lse           [out] float [B][H][W][heads]
+ * Queries that see nothing, or nothing but scores of -infinity, get out = 0 and lse = -infinity.  fp32
+ * storage: fp32 arithmetic (products of operands in two TF32 parts).  bf16: products of bf16 operands, softmax weights rounded
+ * to bf16 for the product with v, sums in fp32, out rounded once.
+ */
+slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const void* v, const int* idx,
+                                            void* out, float* lse,
+                                            int B, int H, int W, int heads, int head_dim,
+                                            int block_h, int block_w, int top, slide_attn_dtype dtype,
+                                            void* cuda_stream);
+
+/*
+ * Its gradients for dout = d(loss)/d(out); the lists are constants.
+ *   q, k, v, idx, out, lse  [in] what the forward was given and gave
+ *   dq, dk, dv              [out] [B][H][W][heads][head_dim], overwritten
+ */
+slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const void* v, const int* idx,
+                                             const void* out, const float* lse, const void* dout,
+                                             void* dq, void* dk, void* dv,
+                                             int B, int H, int W, int heads, int head_dim,
+                                             int block_h, int block_w, int top, slide_attn_dtype dtype,
+                                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, int head_dim,
+                                              int block_h, int block_w, size_t* bytes);
 
 /* Frees the context and everything it owns.  NULL is accepted.  The caller must make sure no
  * forward of this context is still running. */

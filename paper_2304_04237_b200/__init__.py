@@ -10,4 +10,8 @@ from .binding import (BF16, ERR_ALIGNMENT, ERR_ALLOC, ERR_ARCH, ERR_CUDA, ERR_IN
                       slide_attn_profile_begin, slide_attn_profile_end,
                       slide_attn_query_status, slide_attn_set_variant, slide_attn_status_string,
                       slide_attn_set_fixed_shift, slide_attn_detect_fixed_shift,
-                      slide_attn_project, slide_attn_block_forward)
+                      slide_attn_project, slide_attn_block_forward,
+                      ACT_GELU, ACT_NONE, ACT_SILU, DROP_ELEMENTS, DROP_IMAGES,
+                      slide_attn_group_norm_forward, slide_attn_group_norm_backward,
+                      slide_attn_dropout_forward, slide_attn_dropout_backward,
+                      slide_attn_select_blocks, slide_attn_sparse_forward, slide_attn_sparse_backward)

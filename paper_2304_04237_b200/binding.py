@@ -20,12 +20,18 @@ VARIANT_UMMA_SPLIT = 11
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_ALLOC, ERR_CUDA, ERR_ARCH, ERR_TIMEOUT = range(8)
 ERR_TOO_LARGE = 8
 ERR_NOT_FIXED_SHIFT = 9
+ACT_NONE, ACT_SILU, ACT_GELU = range(3)
+DROP_ELEMENTS, DROP_IMAGES = range(2)
 
 EXPORTS = ("slide_attn_create", "slide_attn_forward", "slide_attn_forward_host", "slide_attn_backward",
            "slide_attn_forward_noalloc", "slide_attn_project", "slide_attn_block_forward",
            "slide_attn_set_variant", "slide_attn_get_variant", "slide_attn_launches_per_forward",
            "slide_attn_set_fixed_shift", "slide_attn_detect_fixed_shift",
            "slide_attn_profile_begin", "slide_attn_profile_end",
+           "slide_attn_group_norm_forward", "slide_attn_group_norm_backward", "slide_attn_group_norm_workspace",
+           "slide_attn_dropout_forward", "slide_attn_dropout_backward",
+           "slide_attn_select_blocks", "slide_attn_select_workspace",
+           "slide_attn_sparse_forward", "slide_attn_sparse_backward", "slide_attn_sparse_workspace",
            "slide_attn_query_status", "slide_attn_destroy", "slide_attn_status_string")
 
 _lib = None
@@ -65,6 +71,17 @@ def load() -> ctypes.CDLL:
         lib.slide_attn_profile_begin.argtypes = [vp]
         lib.slide_attn_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_double),
                                                ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i)]
+        ll, f, sz = ctypes.c_longlong, ctypes.c_float, ctypes.c_size_t
+        lib.slide_attn_group_norm_forward.argtypes = [vp] * 6 + [i] * 5 + [f, i, i, vp]
+        lib.slide_attn_group_norm_backward.argtypes = [vp] * 9 + [i] * 7 + [vp, sz, vp]
+        lib.slide_attn_group_norm_workspace.argtypes = [i] * 6 + [ctypes.POINTER(sz)]
+        lib.slide_attn_dropout_forward.argtypes = [vp] * 3 + [ll, ll, f, i, vp, i, vp]
+        lib.slide_attn_dropout_backward.argtypes = [vp] * 2 + [ll, ll, f, i, vp, i, vp]
+        lib.slide_attn_select_blocks.argtypes = [vp] * 3 + [i] * 9 + [vp, sz, vp]
+        lib.slide_attn_select_workspace.argtypes = [i] * 7 + [ctypes.POINTER(sz)]
+        lib.slide_attn_sparse_forward.argtypes = [vp] * 6 + [i] * 9 + [vp]
+        lib.slide_attn_sparse_backward.argtypes = [vp] * 10 + [i] * 9 + [vp, sz, vp]
+        lib.slide_attn_sparse_workspace.argtypes = [i] * 7 + [ctypes.POINTER(sz)]
         lib.slide_attn_query_status.argtypes = [vp, vp]
         lib.slide_attn_destroy.argtypes = [vp]
         lib.slide_attn_status_string.argtypes = [i]
@@ -219,3 +236,167 @@ def slide_attn_query_status(ctx, stream=None) -> int:
 
 def slide_attn_destroy(ctx) -> None:
     _check(load().slide_attn_destroy(ctx), "slide_attn_destroy")
+
+
+# ---- operators around and beside the local attention: sizes from the tensors, scratch memory from torch unless it is given ----------
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _device_ptrs(where, *tensors):
+    """Addresses of contiguous CUDA tensors (None stays None), all on the current device."""
+    device, ptrs = None, []
+    for t in tensors:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{where} takes contiguous CUDA tensors")
+        if device is None:
+            device = _raw_device() if _raw_device else torch.cuda.current_device()
+        if t.get_device() != device:
+            raise ValueError(f"{where}: a tensor is on device {t.get_device()}, the current device is {device}")
+        ptrs.append(t.data_ptr())
+    return ptrs
+
+
+def _dtype_of(where, x):
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError(f"{where} takes float32 or bfloat16 maps, not {x.dtype}")
+    return dtype
+
+
+def _expect(where, name, t, shape, dtype):
+    if t is not None and (t.dtype != dtype or t.shape != shape):
+        raise ValueError(f"{where}: {name} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _workspace(where, given, stream, size, *args):
+    """(tensor, address, bytes) of the scratch memory that `size` asks for.  Without one of the caller's it is torch's, taken from the pool
+    of the stream that the call runs on, so that it can be handed back as soon as the call is made."""
+    need = ctypes.c_size_t()
+    _check(size(*args, ctypes.byref(need)), where)
+    if given is None:
+        if stream is None:
+            given = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        else:
+            handle = _stream_ptr(stream)
+            with torch.cuda.stream(torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()):
+                given = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+    return given, _device_ptrs(where, given)[0], given.numel() * given.element_size()
+
+
+def slide_attn_group_norm_forward(x, gamma, beta, groups, eps, act, y, mean, rstd, stream=None) -> None:
+    """y = act(group norm of x * gamma + beta) over [B, H, W, C] maps; act: ACT_NONE, ACT_SILU or ACT_GELU; gamma, beta: float32 [C] or None;
+    mean, rstd: float32 [B, groups], written for the backward.  Asynchronous on `stream`."""
+    where = "slide_attn_group_norm_forward"
+    dtype = _dtype_of(where, x)
+    B, H, W, C = x.shape
+    _expect(where, "y", y, x.shape, x.dtype)
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        _expect(where, name, t, (C,), torch.float32)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _expect(where, name, t, (B, groups), torch.float32)
+    _check(load().slide_attn_group_norm_forward(*_device_ptrs(where, x, gamma, beta, y, mean, rstd), B, H, W, C, groups, eps, act, dtype,
+                                                _stream_ptr(stream)), where)
+
+
+def slide_attn_group_norm_backward(x, gamma, beta, groups, act, mean, rstd, dy, dx, dgamma, dbeta, stream=None, workspace=None) -> None:
+    """Gradients of the forward's x, gamma and beta for dy = d(loss)/d(y); dgamma and dbeta: float32 [C], or both None."""
+    where = "slide_attn_group_norm_backward"
+    dtype = _dtype_of(where, x)
+    B, H, W, C = x.shape
+    for name, t in (("dy", dy), ("dx", dx)):
+        _expect(where, name, t, x.shape, x.dtype)
+    for name, t in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
+        _expect(where, name, t, (C,), torch.float32)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _expect(where, name, t, (B, groups), torch.float32)
+    lib, at, size = load(), None, 0
+    ptrs = _device_ptrs(where, x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta)
+    if dgamma is not None:
+        workspace, at, size = _workspace(where, workspace, stream, lib.slide_attn_group_norm_workspace, B, H, W, C, groups, dtype)
+    _check(lib.slide_attn_group_norm_backward(*ptrs, B, H, W, C, groups, act, dtype, at, size, _stream_ptr(stream)), where)
+
+
+def _dropout_sizes(where, x, rng, **others):
+    for name, t in others.items():
+        _expect(where, name, t, x.shape, x.dtype)
+    if rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2:
+        raise ValueError(f"{where}: rng has to be two 64-bit integers (seed, offset)")
+    if x.numel() == 0:
+        raise ValueError(f"{where}: x is empty")
+    return x.shape[0] if x.dim() else 1, x.numel() // (x.shape[0] if x.dim() else 1)
+
+
+def slide_attn_dropout_forward(x, residual, p, unit, rng, y, stream=None) -> None:
+    """y = residual + (kept ? x / (1 - p) : 0); residual may be None, y may be x or residual.  unit: DROP_ELEMENTS, or DROP_IMAGES for all of
+    an image (x's first dimension) or nothing of it.  rng: device tensor of two 64-bit integers, seed and offset, read when the call runs."""
+    where = "slide_attn_dropout_forward"
+    dtype = _dtype_of(where, x)
+    images, per_image = _dropout_sizes(where, x, rng, residual=residual, y=y)
+    px, pr, py, prng = _device_ptrs(where, x, residual, y, rng)
+    _check(load().slide_attn_dropout_forward(px, pr, py, images, per_image, p, unit, prng, dtype, _stream_ptr(stream)), where)
+
+
+def slide_attn_dropout_backward(dy, p, unit, rng, dx, stream=None) -> None:
+    """dx = kept ? dy / (1 - p) : 0 with the mask of a forward of the same p, unit and rng; dx may be dy."""
+    where = "slide_attn_dropout_backward"
+    dtype = _dtype_of(where, dy)
+    images, per_image = _dropout_sizes(where, dy, rng, dx=dx)
+    pdy, pdx, prng = _device_ptrs(where, dy, dx, rng)
+    _check(load().slide_attn_dropout_backward(pdy, pdx, images, per_image, p, unit, prng, dtype, _stream_ptr(stream)), where)
+
+
+def _lists(where, q, idx, block):
+    """Blocks and entries of the lists of a call on [B, H, W, heads, head_dim] maps."""
+    B, H, W, heads, _ = q.shape
+    bh, bw = block
+    if bh < 1 or bw < 1:
+        raise ValueError(f"{where}: a block has at least one pixel")
+    _expect(where, "idx", idx, (B, heads, -(-H // bh) * -(-W // bw), idx.shape[-1]), torch.int32)
+    return bh, bw, idx.shape[-1]
+
+
+def slide_attn_select_blocks(q, k, block, idx, stream=None, workspace=None) -> None:
+    """Writes, for every block of queries and every head, the numbers of the idx.shape[-1] blocks of keys with the largest scores (pooled
+    query times pooled key).  block: (height, width) in pixels; idx: int32 [B, heads, blocks, top]."""
+    where = "slide_attn_select_blocks"
+    dtype = _dtype_of(where, q)
+    B, H, W, heads, d = q.shape
+    _expect(where, "k", k, q.shape, q.dtype)
+    bh, bw, top = _lists(where, q, idx, block)
+    lib = load()
+    ptrs = _device_ptrs(where, q, k, idx)
+    workspace, at, size = _workspace(where, workspace, stream, lib.slide_attn_select_workspace, B, H, W, heads, d, bh, bw)
+    _check(lib.slide_attn_select_blocks(*ptrs, B, H, W, heads, d, bh, bw, top, dtype, at, size, _stream_ptr(stream)), where)
+
+
+def slide_attn_sparse_forward(q, k, v, idx, block, out, lse, stream=None) -> None:
+    """Attention of every query to the pixels of the blocks that idx (int32 [B, heads, blocks, top]) lists for its own block; lse: float32
+    [B, H, W, heads], written for the backward."""
+    where = "slide_attn_sparse_forward"
+    dtype = _dtype_of(where, q)
+    B, H, W, heads, d = q.shape
+    for name, t in (("k", k), ("v", v), ("out", out)):
+        _expect(where, name, t, q.shape, q.dtype)
+    _expect(where, "lse", lse, (B, H, W, heads), torch.float32)
+    bh, bw, top = _lists(where, q, idx, block)
+    _check(load().slide_attn_sparse_forward(*_device_ptrs(where, q, k, v, idx, out, lse), B, H, W, heads, d, bh, bw, top, dtype,
+                                            _stream_ptr(stream)), where)
+
+
+def slide_attn_sparse_backward(q, k, v, idx, block, out, lse, dout, dq, dk, dv, stream=None, workspace=None) -> None:
+    """Gradients of the forward's q, k and v for dout = d(loss)/d(out); the lists are constants."""
+    where = "slide_attn_sparse_backward"
+    dtype = _dtype_of(where, q)
+    B, H, W, heads, d = q.shape
+    for name, t in (("k", k), ("v", v), ("out", out), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv)):
+        _expect(where, name, t, q.shape, q.dtype)
+    _expect(where, "lse", lse, (B, H, W, heads), torch.float32)
+    bh, bw, top = _lists(where, q, idx, block)
+    lib = load()
+    ptrs = _device_ptrs(where, q, k, v, idx, out, lse, dout, dq, dk, dv)
+    workspace, at, size = _workspace(where, workspace, stream, lib.slide_attn_sparse_workspace, B, H, W, heads, d, bh, bw)
+    _check(lib.slide_attn_sparse_backward(*ptrs, B, H, W, heads, d, bh, bw, top, dtype, at, size, _stream_ptr(stream)), where)

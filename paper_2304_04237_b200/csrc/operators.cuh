@@ -1,0 +1,28 @@
+// The operators around and beside the local attention: what the C ABI layer (operators_api.cu) launches.
+#pragma once
+#include "sparse_common.cuh"
+
+namespace slide_attn {
+
+// Group norm over [B][P][C].  sums: 2 B C floats for the weights' gradients (unused without them).
+bool group_norm_supports(long long B, long long P, int C, int groups, slide_attn_dtype dtype);
+cudaError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, long long B, long long P, int C, int groups, float eps,
+                                      slide_attn_activation act, slide_attn_dtype dtype, void* y, float* mean, float* rstd, int num_sms,
+                                      cudaStream_t stream);
+cudaError_t launch_group_norm_backward(const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, const void* dy,
+                                       long long B, long long P, int C, int groups, slide_attn_activation act, slide_attn_dtype dtype, void* dx,
+                                       float* dgamma, float* dbeta, float* sums, int num_sms, cudaStream_t stream);
+
+bool dropout_supports(long long images, long long per_image, bool whole_images);
+cudaError_t launch_dropout(const void* x, const void* residual, void* y, long long images, long long per_image, double p, bool whole_images,
+                           const unsigned long long* rng, slide_attn_dtype dtype, int num_sms, cudaStream_t stream);
+
+// pooled: 2 B heads blocks head_dim doubles; delta: B H W heads floats.
+cudaError_t launch_select(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
+                          int* idx, cudaStream_t stream);
+cudaError_t launch_sparse_forward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k,
+                                  const void* v, const int* idx, void* out, float* lse, cudaStream_t stream);
+cudaError_t launch_sparse_backward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const sparse::BackwardMaps& m,
+                                   float* delta, cudaStream_t stream);
+
+}  // namespace slide_attn

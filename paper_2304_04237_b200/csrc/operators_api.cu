@@ -1,0 +1,238 @@
+// C ABI of the operators around and beside the local attention: group norm, dropout, block-sparse attention.  They take sizes instead of a
+// context and workspaces instead of owning any; here their arguments are checked, the arithmetic lives in the kernel files.
+#include <math.h>
+
+#include "operators.cuh"
+
+using namespace slide_attn;
+
+namespace {
+
+bool misaligned(const void* p, unsigned to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+template <typename... P> bool any_null(P... p) { return (... || (p == nullptr)); }
+template <typename... P> bool any_misaligned(P... p) { return (... || misaligned(p)); }
+
+// Whether an output is also one of the others.
+template <typename... P> bool among(const void* out, P... p) { return (... || (out == static_cast<const void*>(p))); }
+
+// The current device is one that the kernels run on; its SMs.
+slide_attn_status current_device(int* num_sms) {
+    static int known[64] = {};
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SLIDE_ATTN_ERR_CUDA; }
+    if (dev < 64) n = known[dev];
+    if (n == 0) {
+        int major = 0;
+        if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+            cudaGetLastError();
+            return SLIDE_ATTN_ERR_CUDA;
+        }
+        if (major != 10) return SLIDE_ATTN_ERR_ARCH;
+        if (dev < 64) known[dev] = n;
+    }
+    *num_sms = n;
+    return SLIDE_ATTN_OK;
+}
+
+slide_attn_status launched(cudaError_t e) {
+    if (e == cudaSuccess) return SLIDE_ATTN_OK;
+    cudaGetLastError();
+    return SLIDE_ATTN_ERR_CUDA;
+}
+
+bool known_dtype(slide_attn_dtype t) { return t == SLIDE_ATTN_F32 || t == SLIDE_ATTN_BF16; }
+
+slide_attn_status norm_shape(int B, int H, int W, int C, int groups, slide_attn_dtype dtype) {
+    if (B < 1 || H < 1 || W < 1 || C < 1 || groups < 1 || !known_dtype(dtype)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (C % groups != 0 || C % 8 != 0) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    const long long P = (long long)H * W;
+    if (P > (1LL << 30) || B > (1LL << 40) / P / C || !group_norm_supports(B, P, C, groups, dtype)) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    return SLIDE_ATTN_OK;
+}
+
+bool known_activation(slide_attn_activation a) { return a == SLIDE_ATTN_ACT_NONE || a == SLIDE_ATTN_ACT_SILU || a == SLIDE_ATTN_ACT_GELU; }
+
+slide_attn_status sparse_shape(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, sparse::Geometry* g) {
+    if (B < 1 || H < 1 || W < 1 || heads < 1 || head_dim < 1 || block_h < 1 || block_w < 1) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (head_dim != 16 && head_dim != 32 && head_dim != 64) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    if (block_h > sparse::kMaxEdge || block_w > sparse::kMaxEdge) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    const long long across = ((long long)W + block_w - 1) / block_w, down = ((long long)H + block_h - 1) / block_h;
+    if (across > sparse::kMaxBlocks || down > sparse::kMaxBlocks || across * down > sparse::kMaxBlocks) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    g->H = H; g->W = W; g->heads = heads; g->bh = block_h; g->bw = block_w;
+    g->across = (int)across; g->blocks = (int)(across * down); g->top = 0;
+    g->tiles = (block_h * block_w + sparse::kRows - 1) / sparse::kRows;
+    // the CTAs of one image and head (also a bound for those that pool and rank), times those of the batch, in a grid's first dimension
+    if ((long long)B * heads > (1LL << 30) / ((long long)g->blocks * g->tiles)) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    return SLIDE_ATTN_OK;
+}
+
+slide_attn_status with_top(sparse::Geometry* g, int top) {
+    if (top < 1) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (top > sparse::kMaxTop) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    g->top = top;
+    return SLIDE_ATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+slide_attn_status slide_attn_group_norm_workspace(int B, int H, int W, int C, int groups, slide_attn_dtype dtype, size_t* bytes)
+{
+    if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
+    const slide_attn_status st = norm_shape(B, H, W, C, groups, dtype);
+    if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(float) * (size_t)B * C;
+    return st;
+}
+
+slide_attn_status slide_attn_group_norm_forward(const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, int B, int H,
+                                                int W, int C, int groups, float eps, slide_attn_activation act, slide_attn_dtype dtype,
+                                                void* cuda_stream)
+{
+    if (any_null(x, static_cast<const void*>(y), static_cast<const void*>(mean), static_cast<const void*>(rstd))) return SLIDE_ATTN_ERR_INVALID_ARG;
+    slide_attn_status st = norm_shape(B, H, W, C, groups, dtype);
+    if (st != SLIDE_ATTN_OK) return st;
+    if (!known_activation(act) || !(eps >= 0.0f) || isinf(eps)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(x, gamma, beta, y, mean, rstd)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    if (y == x || among(mean, x, y, gamma, beta, rstd) || among(rstd, x, y, gamma, beta) || among(y, gamma, beta)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    int sms = 0;
+    st = current_device(&sms);
+    if (st != SLIDE_ATTN_OK) return st;
+    return launched(launch_group_norm_forward(x, gamma, beta, B, (long long)H * W, C, groups, eps, act, dtype, y, mean, rstd, sms,
+                                              static_cast<cudaStream_t>(cuda_stream)));
+}
+
+slide_attn_status slide_attn_group_norm_backward(const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd,
+                                                 const void* dy, void* dx, float* dgamma, float* dbeta, int B, int H, int W, int C, int groups,
+                                                 slide_attn_activation act, slide_attn_dtype dtype, void* workspace, size_t workspace_bytes,
+                                                 void* cuda_stream)
+{
+    if (any_null(x, static_cast<const void*>(mean), static_cast<const void*>(rstd), dy, static_cast<const void*>(dx))) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if ((dgamma == nullptr) != (dbeta == nullptr)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    slide_attn_status st = norm_shape(B, H, W, C, groups, dtype);
+    if (st != SLIDE_ATTN_OK) return st;
+    if (!known_activation(act)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (dgamma && (!workspace || workspace_bytes < 2 * sizeof(float) * (size_t)B * C)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta) || (dgamma && misaligned(workspace))) return SLIDE_ATTN_ERR_ALIGNMENT;
+    if (among(dx, x, dy, gamma, beta, mean, rstd)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (dgamma && (among(dgamma, dbeta, x, dy, dx, gamma, beta, mean, rstd, workspace) || among(dbeta, x, dy, dx, gamma, beta, mean, rstd, workspace) ||
+                   among(workspace, x, dy, dx, gamma, beta, mean, rstd)))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
+    int sms = 0;
+    st = current_device(&sms);
+    if (st != SLIDE_ATTN_OK) return st;
+    return launched(launch_group_norm_backward(x, gamma, beta, mean, rstd, dy, B, (long long)H * W, C, groups, act, dtype, dx, dgamma, dbeta,
+                                               static_cast<float*>(workspace), sms, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+namespace {
+
+slide_attn_status dropout(const void* x, const void* residual, void* y, long long images, long long per_image, float p, slide_attn_drop_unit unit,
+                          const void* rng, slide_attn_dtype dtype, void* cuda_stream) {
+    if (any_null(x, static_cast<const void*>(y), rng)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (images < 1 || per_image < 1 || !known_dtype(dtype) || (unit != SLIDE_ATTN_DROP_ELEMENTS && unit != SLIDE_ATTN_DROP_IMAGES))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (!(p >= 0.0f && p <= 1.0f)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (per_image > (1LL << 40) / images || !dropout_supports(images, per_image, unit == SLIDE_ATTN_DROP_IMAGES)) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    if (any_misaligned(x, residual, y) || misaligned(rng, 8)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    if (y == rng) return SLIDE_ATTN_ERR_INVALID_ARG;
+    int sms = 0;
+    const slide_attn_status st = current_device(&sms);
+    if (st != SLIDE_ATTN_OK) return st;
+    return launched(launch_dropout(x, residual, y, images, per_image, p, unit == SLIDE_ATTN_DROP_IMAGES,
+                                   static_cast<const unsigned long long*>(rng), dtype, sms, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+}  // namespace
+
+slide_attn_status slide_attn_dropout_forward(const void* x, const void* residual, void* y, long long images, long long per_image, float p,
+                                             slide_attn_drop_unit unit, const void* rng, slide_attn_dtype dtype, void* cuda_stream)
+{
+    return dropout(x, residual, y, images, per_image, p, unit, rng, dtype, cuda_stream);
+}
+
+slide_attn_status slide_attn_dropout_backward(const void* dy, void* dx, long long images, long long per_image, float p, slide_attn_drop_unit unit,
+                                              const void* rng, slide_attn_dtype dtype, void* cuda_stream)
+{
+    return dropout(dy, nullptr, dx, images, per_image, p, unit, rng, dtype, cuda_stream);
+}
+
+slide_attn_status slide_attn_select_workspace(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, size_t* bytes)
+{
+    if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
+    sparse::Geometry g;
+    const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(double) * (size_t)B * heads * g.blocks * head_dim;
+    return st;
+}
+
+slide_attn_status slide_attn_select_blocks(const void* q, const void* k, int* idx, int B, int H, int W, int heads, int head_dim, int block_h,
+                                           int block_w, int top, slide_attn_dtype dtype, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    if (any_null(q, k, static_cast<const void*>(idx), static_cast<const void*>(workspace)) || !known_dtype(dtype)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    sparse::Geometry g;
+    slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
+    if (st != SLIDE_ATTN_OK) return st;
+    if (top > g.blocks || workspace_bytes < 2 * sizeof(double) * (size_t)B * heads * g.blocks * head_dim) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(q, k, idx, workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    if (among(idx, q, k, workspace) || among(workspace, q, k)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    int sms = 0;
+    st = current_device(&sms);
+    if (st != SLIDE_ATTN_OK) return st;
+    return launched(launch_select(g, B, head_dim, dtype, q, k, static_cast<double*>(workspace), idx, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const void* v, const int* idx, void* out, float* lse, int B, int H, int W,
+                                            int heads, int head_dim, int block_h, int block_w, int top, slide_attn_dtype dtype, void* cuda_stream)
+{
+    if (any_null(q, k, v, static_cast<const void*>(idx), static_cast<const void*>(out), static_cast<const void*>(lse)) || !known_dtype(dtype))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
+    sparse::Geometry g;
+    slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
+    if (st != SLIDE_ATTN_OK) return st;
+    if (any_misaligned(q, k, v, idx, out, lse)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    if (among(out, q, k, v, idx, lse) || among(lse, q, k, v, idx)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    int sms = 0;
+    st = current_device(&sms);
+    if (st != SLIDE_ATTN_OK) return st;
+    return launched(launch_sparse_forward(g, B, head_dim, dtype, q, k, v, idx, out, lse, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, size_t* bytes)
+{
+    if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
+    sparse::Geometry g;
+    const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK) *bytes = sizeof(float) * (size_t)B * H * W * heads;
+    return st;
+}
+
+slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const void* v, const int* idx, const void* out, const float* lse,
+                                             const void* dout, void* dq, void* dk, void* dv, int B, int H, int W, int heads, int head_dim, int block_h,
+                                             int block_w, int top, slide_attn_dtype dtype, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    if (any_null(q, k, v, static_cast<const void*>(idx), out, static_cast<const void*>(lse), dout, static_cast<const void*>(dq),
+                 static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(workspace)) ||
+        !known_dtype(dtype))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
+    sparse::Geometry g;
+    slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
+    if (st != SLIDE_ATTN_OK) return st;
+    if (workspace_bytes < sizeof(float) * (size_t)B * H * W * heads) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(q, k, v, idx, out, lse, dout, dq, dk, dv) || misaligned(workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    for (const void* o : {static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(workspace)})
+        if (among(o, q, k, v, idx, out, lse, dout)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (among(dq, dk, dv, workspace) || among(dk, dv, workspace) || dv == workspace) return SLIDE_ATTN_ERR_INVALID_ARG;
+    int sms = 0;
+    st = current_device(&sms);
+    if (st != SLIDE_ATTN_OK) return st;
+    const sparse::BackwardMaps m = {q, k, v, idx, out, lse, dout, dq, dk, dv};
+    return launched(launch_sparse_backward(g, B, head_dim, dtype, m, static_cast<float*>(workspace), static_cast<cudaStream_t>(cuda_stream)));
+}
+
+}  // extern "C"
