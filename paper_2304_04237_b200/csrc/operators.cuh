@@ -17,12 +17,12 @@ bool dropout_supports(long long images, long long per_image, bool whole_images);
 cudaError_t launch_dropout(const void* x, const void* residual, void* y, long long images, long long per_image, double p, bool whole_images,
                            const unsigned long long* rng, slide_attn_dtype dtype, int num_sms, cudaStream_t stream);
 
-// pooled: 2 B heads blocks head_dim doubles; delta: B H W heads floats.
+// pooled: 2 B heads blocks head_dim doubles; the backward's workspace: two floats a query.
 cudaError_t launch_select(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
                           int* idx, cudaStream_t stream);
 cudaError_t launch_sparse_forward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k,
-                                  const void* v, const int* idx, void* out, float* lse, cudaStream_t stream);
+                                  const void* v, const int* idx, void* out, float* lse, int num_sms, cudaStream_t stream);
 cudaError_t launch_sparse_backward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const sparse::BackwardMaps& m,
-                                   float* delta, cudaStream_t stream);
+                                   void* workspace, int num_sms, cudaStream_t stream);
 
 }  // namespace slide_attn

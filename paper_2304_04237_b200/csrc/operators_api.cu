@@ -199,7 +199,7 @@ slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const 
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
-    return launched(launch_sparse_forward(g, B, head_dim, dtype, q, k, v, idx, out, lse, static_cast<cudaStream_t>(cuda_stream)));
+    return launched(launch_sparse_forward(g, B, head_dim, dtype, q, k, v, idx, out, lse, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, size_t* bytes)
@@ -207,7 +207,7 @@ slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, in
     if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
     sparse::Geometry g;
     const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
-    if (st == SLIDE_ATTN_OK) *bytes = sizeof(float) * (size_t)B * H * W * heads;
+    if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(float) * (size_t)B * H * W * heads;
     return st;
 }
 
@@ -223,7 +223,7 @@ slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const
     slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
     if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st != SLIDE_ATTN_OK) return st;
-    if (workspace_bytes < sizeof(float) * (size_t)B * H * W * heads) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (workspace_bytes < 2 * sizeof(float) * (size_t)B * H * W * heads) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (any_misaligned(q, k, v, idx, out, lse, dout, dq, dk, dv) || misaligned(workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
     for (const void* o : {static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(workspace)})
         if (among(o, q, k, v, idx, out, lse, dout)) return SLIDE_ATTN_ERR_INVALID_ARG;
@@ -232,7 +232,7 @@ slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
     const sparse::BackwardMaps m = {q, k, v, idx, out, lse, dout, dq, dk, dv};
-    return launched(launch_sparse_backward(g, B, head_dim, dtype, m, static_cast<float*>(workspace), static_cast<cudaStream_t>(cuda_stream)));
+    return launched(launch_sparse_backward(g, B, head_dim, dtype, m, workspace, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // extern "C"

@@ -3,20 +3,18 @@
 //
 //   dS = P (dout v^T - delta),   dq = dS k / sqrt(d),   dk = dS^T q / sqrt(d),   dv = P^T dout
 //
-// Two launches: queries (dq, over the blocks of their list; also writes delta) and keys (dk and dv, over the blocks of queries whose
-// lists name the key's block, found by going through the image's lists in their order).  Neither adds to memory that another CTA
-// writes, so results do not depend on which CTA runs first.
+// Two launches: queries (dq, over the blocks of their list; also writes each query's logarithm and delta side by side) and keys (dk and dv, over
+// the blocks of queries whose lists name the key's block, found by going through the image's lists in their order).  Neither adds to
+// memory that another CTA writes, so results do not depend on which CTA runs first.
 #include "operators.cuh"
 
 namespace slide_attn {
 
 namespace sparse {
 
-template <typename T, int D> constexpr int kBackwardTile = D == 64 ? 32 : 64;       // rows of a tile
-constexpr int kListed = 1024;                                                       // entries that the keys' kernel lists at a time
-constexpr int kScan = 4 * kThreads;                                                 // entries of the image's lists that it looks at in one go
+template <typename T, int D> using BackwardPipe = QueryPipe<T, D, sizeof(T) == 4 || D == 64 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 2 : 3, 2>;
 
-// exp2 of a score less the logarithm of its row's sum.  A row that has none (no keys, or none but -inf) has no weights.
+// The logarithm to base 2 of a row's sum.  A row that has none (no keys, or none but -inf) has no weights: exp2 of less infinity.
 __device__ __forceinline__ float log2_of_sum(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
 template <typename T> __device__ __forceinline__ float dot_piece(const T* a, const T* b);
@@ -33,268 +31,270 @@ template <> __device__ __forceinline__ float dot_piece<__nv_bfloat16>(const __nv
     return s;
 }
 
-template <typename T, int D> constexpr size_t queries_smem() {
-    return (size_t)Tile<T, D>::kRowBytes * (2 * kRows + 4 * kBackwardTile<T, D>) + kMaxTop * sizeof(Entry) + kRows * sizeof(float);
-}
-template <typename T, int D> constexpr size_t keys_smem() {
-    return (size_t)Tile<T, D>::kRowBytes * (2 * kRows + 4 * kBackwardTile<T, D>) + kListed * sizeof(Entry) + 4 * kBackwardTile<T, D> * sizeof(float);
+// Each query's logarithm of the sum (base 2) and delta: a thread a query and head.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats)
+{
+    grid_dependency_wait();
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    float s = 0.0f;
+    constexpr int kPiece = 16 / sizeof(T);
+#pragma unroll
+    for (int e = 0; e < D; e += kPiece) s += dot_piece<T>(dout + i * D + e, out + i * D + e);
+    stats[i] = make_float2(log2_of_sum(lse[i]), s);
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
-sparse_queries_kernel(const Geometry g, const T* q, const T* k, const T* v, const int* idx, const T* out, const float* lse, const T* dout, T* dq,
-                      float* delta)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : D == 64 ? 3 : 4)
+sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, const T* dout, const float2* stats, T* dq)
 {
-    using L = Tile<T, D>;
-    constexpr int N = kBackwardTile<T, D>, NT = N / 8;
+    using P = BackwardPipe<T, D>;
+    using L = Layout<T, D>;
+    constexpr int N = (int)(P::kTile / L::kRowBytes), NT = N / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int listed;
-    const uint32_t tile_q = smem_u32(smem), tile_g = tile_q + kRows * L::kRowBytes, tiles = tile_g + kRows * L::kRowBytes;
-    constexpr uint32_t kStage = 2 * N * L::kRowBytes;
-    Entry* list = reinterpret_cast<Entry*>(smem + (size_t)(2 * kRows + 4 * N) * L::kRowBytes);
-    float* own_delta = reinterpret_cast<float*>(list + kMaxTop);
-
-    unsigned u = blockIdx.x;
-    const int h = u % g.heads; u /= g.heads;
-    const int part = u % g.tiles; u /= g.tiles;
-    const int r = u % g.blocks;
-    const size_t b = u / g.blocks;
-    const Block own = block_of(g, r);
-    const int rows = own.size() - part * kRows;
-    const size_t stride = (size_t)g.heads * D;
-    const size_t plane = b * g.H * g.W * stride + (size_t)h * D;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    constexpr float scale = root<D>();
 
     grid_dependency_wait();
-    if (rows <= 0) return;
-    copy_rows<T, D, kRows>(tile_q, tile_g, q + plane, dout + plane, stride, rows,
-                           [&](int row) { return pixel_of(g, own, part * kRows + row); });
-    copies_commit();
-    {
-        // delta: two threads a row
-        const int row = threadIdx.x / 2;
-        float s = 0.0f;
-        size_t pixel = 0;
-        if (row < rows) {
-            pixel = pixel_of(g, own, part * kRows + row);
-            const size_t at = plane + pixel * stride;
-            constexpr int kPiece = 16 / sizeof(T);
-#pragma unroll
-            for (int i = 0; i < L::kPieces / 2; ++i) {
-                const int e = (i * 2 + (threadIdx.x & 1)) * kPiece;
-                s += dot_piece<T>(dout + at + e, out + at + e);
-            }
-        }
-        s += __shfl_xor_sync(0xffffffffu, s, 1);
-        if (!(threadIdx.x & 1)) {
-            own_delta[row] = s;
-            if (row < rows) delta[(b * g.H * g.W + pixel) * g.heads + h] = s;
-        }
-    }
-    if (warp == 0) {
-        const int total = read_list(g, idx + ((b * g.heads + h) * g.blocks + r) * g.top, list, lane);
-        if (lane == 0) listed = total;
-    }
-    __syncthreads();
-    const int keys = listed, steps = (keys + N - 1) / N;
-    Cursor cursor;
-    auto fetch = [&](int step) {
-        const uint32_t at = tiles + (step & 1) * kStage;
-        copy_rows<T, D, N>(at, at + N * L::kRowBytes, k + plane, v + plane, stride, keys - step * N,
-                           [&](int row) { return cursor.pixel(g, list, step * N + row); });
-        copies_commit();
-    };
-    if (steps > 0) fetch(0);
+    P pipe(g, smem, q, dout, k, v, idx, units, chain);
+    pipe.start();
 
-    const bool busy = warp * 16 < rows;
-    constexpr float scale = root<D>();
-    typename L::Rows rows_q, rows_g;
-    float dqs[D / 8][4] = {};
-    float sum[2], del[2];
+    Unit unit;
+    Rows<D, L::kPlanes> rows_q, rows_g;
+    float dqs[D / 8][4];
+    float2 stat[2];
+    int item = 0, step = 0, keys = 0;
+    for (int number = 0; item < pipe.items; ++number) {
+        const bool fresh = step == 0;
+        const uint32_t tile = pipe.next(number, fresh, item);
+        if (fresh) {
+            unit.find(g, pipe.first + item);
+            keys = pipe.rows_of[item % P::kLists];
+            rows_q.load(pipe.own_at(item, 0), P::kOwnPlane, warp * 16, lane);
+            rows_g.load(pipe.own_at(item, 1), P::kOwnPlane, warp * 16, lane);
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int row = warp * 16 + half * 8 + (lane >> 2);
-        sum[half] = INFINITY;
-        if (row < rows) sum[half] = log2_of_sum(lse[(b * g.H * g.W + pixel_of(g, own, part * kRows + row)) * g.heads + h]);
-        del[half] = own_delta[row];
-    }
-    for (int step = 0; step < steps; ++step) {
-        copies_wait_all();
-        __syncthreads();
-        if (step + 1 < steps) fetch(step + 1);
-        if (!busy) continue;
-        if (step == 0) { rows_q.load(tile_q, warp * 16, lane); rows_g.load(tile_g, warp * 16, lane); }
-        const uint32_t at = tiles + (step & 1) * kStage;
+            for (int i = 0; i < 2; ++i) {
+                const int row = warp * 16 + i * 8 + (lane >> 2);
+                stat[i] = make_float2(INFINITY, 0.0f);
+                if (row < unit.rows) stat[i] = stats[((size_t)unit.b * g.H * g.W + unit.pixel(g, row)) * g.heads + unit.h];
+            }
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dqs[n][e] = 0.0f;
+        }
+        const bool busy = warp * 16 < unit.rows;
         const int used = min(N, keys - step * N);
-        float s[NT][4], dp[NT][4];
-        L::template scores<NT>(rows_q, at, lane, used, s);
-        L::template scores<NT>(rows_g, at + N * L::kRowBytes, lane, used, dp);
+        if (busy && used > 0) {
+            float s[NT][4], dp[NT][4];
+            scores<D, L::kPlanes, NT>(rows_q, tile, P::kPlane, lane, used, s);
+            scores<D, L::kPlanes, NT>(rows_g, tile + P::kBehind, P::kPlane, lane, used, dp);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = n * 8 + 2 * (lane & 3) + (e & 1) < used ? fast_exp2(fmaf(s[n][e], scale * kLog2e, -sum[e >> 1])) : 0.0f;
-                s[n][e] = p * (dp[n][e] - del[e >> 1]);
+                for (int i = 0; i < 2; ++i) {
+                    float& x = s[n][2 * i];
+                    float& y = s[n][2 * i + 1];
+                    fma2(x, y, x, y, scale * kLog2e, scale * kLog2e, -stat[i].x, -stat[i].x);
+                    x = fast_exp2(x) * (dp[n][2 * i] - stat[i].y);
+                    y = fast_exp2(y) * (dp[n][2 * i + 1] - stat[i].y);
+                }
+            if (used < N) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = 0.0f;
             }
-        L::template gather<NT>(s, at, lane, used, dqs);
-    }
-    if (!busy) return;
+            gather<D, L::kPlanes, NT>(s, tile, P::kPlane, lane, used, dqs);
+        }
+        if (++step * N < keys) continue;
+        if (busy) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int row = warp * 16 + half * 8 + (lane >> 2);
-        if (row >= rows) continue;
-        T* dst = dq + plane + (size_t)pixel_of(g, own, part * kRows + row) * stride + 2 * (lane & 3);
+            for (int i = 0; i < 2; ++i) {
+                const int row = warp * 16 + i * 8 + (lane >> 2);
+                if (row < unit.rows) {
+                    T* dst = dq + unit.plane(g, D) + (size_t)unit.pixel(g, row) * g.heads * D + 2 * (lane & 3);
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n) store2(dst + n * 8, dqs[n][2 * half] * scale, dqs[n][2 * half + 1] * scale);
+                    for (int n = 0; n < D / 8; ++n) store2(dst + n * 8, dqs[n][2 * i] * scale, dqs[n][2 * i + 1] * scale);
+                }
+            }
+        }
+        step = 0;
+        ++item;
     }
 }
 
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
-}
+constexpr int kScanEach = 8, kScan = kScanEach * kThreads;      // entries of the image's lists that the keys' kernel looks at in one go
+
+template <typename T, int D> struct KeysPlan {
+    using L = Layout<T, D>;
+    static constexpr int N = BackwardPipe<T, D>::kTile / L::kRowBytes, S = sizeof(T) == 4 && D == 64 ? 2 : 3;
+    static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
+    static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D, kBehind = L::kSplit ? kPlane / 2 : kTile;
+    // the rows as they arrive may lie where the tiles' planes will be: these are made later
+    static constexpr uint32_t kOwnAt = S * kStage, kPartsAt = kOwnAt + 2 * kOwn, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
+    static constexpr uint32_t kListAt = kOwnPartsAt + (L::kSplit ? 6 * kOwnPlane : 0), kStatsAt = kListAt + kScan * 4;
+    static constexpr size_t kSmem = kStatsAt + S * N * sizeof(float2);
+};
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
-sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const int* idx, const float* lse, const float* delta, const T* dout, T* dk, T* dv)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3)
+sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const int* idx, const float2* stats, const T* dout, T* dk, T* dv)
 {
-    using L = Tile<T, D>;
-    constexpr int N = kBackwardTile<T, D>, NT = N / 8;
+    using K = KeysPlan<T, D>;
+    using L = Layout<T, D>;
+    constexpr int N = K::N, NT = N / 8, S = K::S;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int warp_sums[kThreads / 32];
-    const uint32_t tile_k = smem_u32(smem), tile_v = tile_k + kRows * L::kRowBytes, tiles = tile_v + kRows * L::kRowBytes;
-    constexpr uint32_t kStage = 2 * N * L::kRowBytes;     // queries, then gradients of the output
-    Entry* list = reinterpret_cast<Entry*>(smem + (size_t)(2 * kRows + 4 * N) * L::kRowBytes);
-    const float* columns = reinterpret_cast<const float*>(list + kListed);      // of each stage: logarithms of the sums, then delta
-    const uint32_t columns_at = smem_u32(columns);
-
-    unsigned u = blockIdx.x;
-    const int h = u % g.heads; u /= g.heads;
-    const int part = u % g.tiles; u /= g.tiles;
-    const int r = u % g.blocks;
-    const size_t b = u / g.blocks;
-    const Block own = block_of(g, r);
-    const int rows = own.size() - part * kRows;
-    const size_t stride = (size_t)g.heads * D;
-    const size_t plane = b * g.H * g.W * stride + (size_t)h * D;
-    const size_t row_plane = b * g.H * g.W * g.heads + h;
+    __shared__ int warp_counts[kThreads / 32], warp_rows[kThreads / 32];
+    const uint32_t base = smem_u32(smem);
+    int* list = reinterpret_cast<int*>(smem + K::kListAt);
+    const float2* columns = reinterpret_cast<const float2*>(smem + K::kStatsAt);        // of each stage's queries
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    constexpr float scale = root<D>();
 
     grid_dependency_wait();
-    if (rows <= 0) return;
-    copy_rows<T, D, kRows>(tile_k, tile_v, k + plane, v + plane, stride, rows,
-                           [&](int row) { return pixel_of(g, own, part * kRows + row); });
-    copies_commit();
-
-    const bool busy = warp * 16 < rows;
-    constexpr float scale = root<D>();
-    typename L::Rows rows_k, rows_v;
-    bool loaded = false;
+    Unit unit;
+    unit.find(g, blockIdx.x);
+    if (unit.rows <= 0) return;
+    const size_t plane = unit.plane(g, D);
+    {
+        const int row = threadIdx.x / (kThreads / kRows);
+        const bool there = row < unit.rows;
+        copy_rows<T, D, kRows>(base + K::kOwnAt, base + K::kOwnAt + K::kOwn, k + plane, v + plane,
+                               there ? (size_t)unit.pixel(g, row) * g.heads * D : 0, there);
+        copies_commit();
+    }
+    const bool busy = warp * 16 < unit.rows;
+    Rows<D, L::kPlanes> rows_k, rows_v;
     float dks[D / 8][4] = {}, dvs[D / 8][4] = {};
-    const int* lists = idx + (b * g.heads + h) * (size_t)g.blocks * g.top;
+    const int* lists = idx + (unit.b * g.heads + unit.h) * (size_t)g.blocks * g.top;
     const int entries = g.blocks * g.top;
-    int seen = 0;
-    while (seen < entries) {
+    for (int seen = 0; seen < entries; seen += kScan) {
         // the next blocks of queries that see this block, in an order that the lists alone decide
-        int n = 0, total = 0;
-        while (seen < entries && n + kScan <= kListed) {
-            int mine[4], own_rows = 0, own_count = 0;
+        int mine[kScanEach], count = 0, size = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = seen + e * kThreads + (int)threadIdx.x;
-                mine[e] = i < entries && lists[i] == r ? i / g.top : -1;
-                if (mine[e] >= 0) { own_rows += block_of(g, mine[e]).size(); ++own_count; }
-            }
-            int sum = own_count << 20 | own_rows;            // at most 512 blocks of 1024 rows
-            const int own_sum = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int x = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += x;
-            }
-            if (lane == 31) warp_sums[warp] = sum;
-            __syncthreads();
-            int before = sum - own_sum, all = 0;
-#pragma unroll
-            for (int w = 0; w < kThreads / 32; ++w) {
-                if (w < warp) before += warp_sums[w];
-                all += warp_sums[w];
-            }
-            int slot = n + (before >> 20), start = total + (before & 0xFFFFF);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (mine[e] >= 0) {
-                    list[slot++] = {mine[e], start};
-                    start += block_of(g, mine[e]).size();
-                }
-            n += all >> 20;
-            total += all & 0xFFFFF;
-            seen += kScan;
-            __syncthreads();
+        for (int e = 0; e < kScanEach; ++e) {
+            const int i = seen + e * kThreads + (int)threadIdx.x;
+            mine[e] = i < entries ? lists[i] : -1;
         }
+#pragma unroll
+        for (int e = 0; e < kScanEach; ++e) {
+            const bool is = mine[e] == unit.r;
+            mine[e] = is ? (seen + e * kThreads + (int)threadIdx.x) / g.top : -1;
+            if (is) { ++count; size += block_of(g, mine[e]).size(); }
+        }
+        int before = count;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int x = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane >= o) before += x;
+        }
+        size = (int)__reduce_add_sync(0xffffffffu, (unsigned)size);
+        if (lane == 31) { warp_counts[warp] = before; warp_rows[warp] = size; }
+        __syncthreads();
+        int slot = before - count, total = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) slot += warp_counts[w];
+            total += warp_rows[w];
+        }
+#pragma unroll
+        for (int e = 0; e < kScanEach; ++e)
+            if (mine[e] >= 0) list[slot++] = mine[e];
+        __syncthreads();
+
         const int steps = (total + N - 1) / N;
         Cursor cursor;
-        auto fetch = [&](int step) {
-            const uint32_t at = tiles + (step & 1) * kStage;
-            constexpr int kPer = kThreads / N;
-            copy_rows<T, D, N>(at, at + N * L::kRowBytes, q + plane, dout + plane, stride, total - step * N, [&](int row) {
-                const int pixel = cursor.pixel(g, list, step * N + row);
-                const uint32_t c = columns_at + (uint32_t)(((step & 1) * 2 * N + row) * 4);
-                if (threadIdx.x % kPer == 0) copy4(c, lse + row_plane + (size_t)pixel * g.heads, true);
-                else if (threadIdx.x % kPer == 1) copy4(c + N * 4, delta + row_plane + (size_t)pixel * g.heads, true);
-                return pixel;
-            });
+        cursor.reset();
+        auto copy = [&](int step) {
+            if (step < steps) {
+                constexpr int kPer = kThreads / N;
+                const int row = (int)threadIdx.x / kPer, j = step * N + row;
+                const bool there = j < total;
+                const size_t pixel = there ? cursor.pixel(g, list, j) : 0;
+                const uint32_t at = base + (uint32_t)(step % S) * K::kStage;
+                copy_rows<T, D, N>(at, at + K::kTile, q + plane, dout + plane, pixel * g.heads * D, there);
+                if (there && threadIdx.x % kPer == 0) {
+                    const uint32_t to = smem_u32(columns + (step % S) * N + row);
+                    const float2* from = stats + ((size_t)unit.b * g.H * g.W + pixel) * g.heads + unit.h;
+                    copy4(to, &from->x);
+                    copy4(to + 4, &from->y);
+                }
+            }
             copies_commit();
         };
-        if (steps > 0) fetch(0);
+        for (int step = 0; step < S - 1; ++step) copy(step);
         for (int step = 0; step < steps; ++step) {
-            copies_wait_all();
+            copies_wait<S - 2>();
             __syncthreads();
-            if (step + 1 < steps) fetch(step + 1);
+            copy(step + S - 1);
+            const uint32_t raw = base + (uint32_t)(step % S) * K::kStage;
+            uint32_t tile = raw;
+            const bool first = step == 0;
+            if constexpr (L::kSplit) {
+                cut_rows<D, 2 * N>(raw, base + K::kPartsAt);
+                if (first)
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) cut_rows<D, kRows>(base + K::kOwnAt + o * K::kOwn, base + K::kOwnPartsAt + o * 3 * K::kOwnPlane);
+                __syncthreads();
+                tile = base + K::kPartsAt;
+            }
             if (!busy) continue;
-            if (!loaded) { rows_k.load(tile_k, warp * 16, lane); rows_v.load(tile_v, warp * 16, lane); loaded = true; }
-            const uint32_t at = tiles + (step & 1) * kStage;
-            const float* col = columns + (step & 1) * 2 * N;
+            if (first) {
+                rows_k.load(L::kSplit ? base + K::kOwnPartsAt : base + K::kOwnAt, K::kOwnPlane, warp * 16, lane);
+                rows_v.load(L::kSplit ? base + K::kOwnPartsAt + 3 * K::kOwnPlane : base + K::kOwnAt + K::kOwn, K::kOwnPlane, warp * 16, lane);
+            }
+            const float4* col = reinterpret_cast<const float4*>(columns + (step % S) * N) + (lane & 3);      // two queries
             const int used = min(N, total - step * N);
             float s[NT][4], dp[NT][4];
-            L::template scores<NT>(rows_k, at, lane, used, s);
+            scores<D, L::kPlanes, NT>(rows_k, tile, K::kPlane, lane, used, s);
+            scores<D, L::kPlanes, NT>(rows_v, tile + K::kBehind, K::kPlane, lane, used, dp);
 #pragma unroll
-            for (int n8 = 0; n8 < NT; ++n8)
+            for (int n = 0; n < NT; ++n) {
+                const float4 c = col[n * 4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int c = n8 * 8 + 2 * (lane & 3) + (e & 1);
-                    s[n8][e] = c < used ? fast_exp2(fmaf(s[n8][e], scale * kLog2e, -log2_of_sum(col[c]))) : 0.0f;
+                for (int i = 0; i < 2; ++i) {
+                    float& x = s[n][2 * i];
+                    float& y = s[n][2 * i + 1];
+                    fma2(x, y, x, y, scale * kLog2e, scale * kLog2e, -c.x, -c.z);
+                    x = fast_exp2(x);
+                    y = fast_exp2(y);
+                    dp[n][2 * i] = x * (dp[n][2 * i] - c.y);
+                    dp[n][2 * i + 1] = y * (dp[n][2 * i + 1] - c.w);
                 }
-            L::template gather<NT>(s, at + N * L::kRowBytes, lane, used, dvs);
-            L::template scores<NT>(rows_v, at + N * L::kRowBytes, lane, used, dp);
+            }
+            if (used < N) {                                  // (a key that is not finite makes a NaN of rows that hold nothing)
 #pragma unroll
-            for (int n8 = 0; n8 < NT; ++n8)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int c = n8 * 8 + 2 * (lane & 3) + (e & 1);
-                    s[n8][e] = c < used ? s[n8][e] * (dp[n8][e] - col[N + c]) : 0.0f;
-                }
-            L::template gather<NT>(s, at, lane, used, dks);
+                    for (int e = 0; e < 4; ++e)
+                        if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = dp[n][e] = 0.0f;
+            }
+            gather<D, L::kPlanes, NT>(s, tile + K::kBehind, K::kPlane, lane, used, dvs);
+            gather<D, L::kPlanes, NT>(dp, tile, K::kPlane, lane, used, dks);
         }
         __syncthreads();                                     // the list and the tiles are free again
     }
-    copies_wait_all();                                       // a block that nobody sees never waited for its own rows
+    copies_wait<0>();                                        // a block that nobody sees never waited for its own rows
     if (!busy) return;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int row = warp * 16 + half * 8 + (lane >> 2);
-        if (row >= rows) continue;
-        const size_t at = plane + (size_t)pixel_of(g, own, part * kRows + row) * stride + 2 * (lane & 3);
+    for (int i = 0; i < 2; ++i) {
+        const int row = warp * 16 + i * 8 + (lane >> 2);
+        if (row >= unit.rows) continue;
+        const size_t at = plane + (size_t)unit.pixel(g, row) * g.heads * D + 2 * (lane & 3);
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) {
-            store2(dk + at + n * 8, dks[n][2 * half] * scale, dks[n][2 * half + 1] * scale);
-            store2(dv + at + n * 8, dvs[n][2 * half], dvs[n][2 * half + 1]);
+            store2(dk + at + n * 8, dks[n][2 * i] * scale, dks[n][2 * i + 1] * scale);
+            store2(dv + at + n * 8, dvs[n][2 * i], dvs[n][2 * i + 1]);
         }
     }
 }
 
 template <typename T, int D>
-cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, float* delta, cudaStream_t stream) {
-    constexpr size_t smem_q = queries_smem<T, D>(), smem_k = keys_smem<T, D>();
+cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, float2* stats, int sms, cudaStream_t stream) {
+    constexpr size_t smem_q = BackwardPipe<T, D>::kSmem, smem_k = KeysPlan<T, D>::kSmem;
     static bool ready[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -305,29 +305,34 @@ cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& 
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev] = true;
     }
-    const dim3 grid((unsigned)(B * g.blocks * g.tiles * g.heads));
+    const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads);
+    const int chain = chain_of(g, units, sms, BackwardPipe<T, D>::kTile / Layout<T, D>::kRowBytes);
+    const long long n = B * g.H * g.W * g.heads;
     auto in = [](const void* p) { return static_cast<const T*>(p); };
     auto to = [](void* p) { return static_cast<T*>(p); };
-    e = launch_chained(sparse_queries_kernel<T, D>, grid, kThreads, smem_q, stream, g, in(m.q), in(m.k), in(m.v), m.idx, in(m.out), m.lse, in(m.dout),
-                       to(m.dq), delta);
+    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + 255) / 256)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats);
     if (e != cudaSuccess) return e;
-    return launch_chained(sparse_keys_kernel<T, D>, grid, kThreads, smem_k, stream, g, in(m.q), in(m.k), in(m.v), m.idx, m.lse,
-                          static_cast<const float*>(delta), in(m.dout), to(m.dk), to(m.dv));
+    e = launch_chained(sparse_queries_kernel<T, D>, dim3((units + chain - 1) / chain), kThreads, smem_q, stream, g, units, chain, in(m.q), in(m.k),
+                       in(m.v), m.idx, in(m.dout), static_cast<const float2*>(stats), to(m.dq));
+    if (e != cudaSuccess) return e;
+    return launch_chained(sparse_keys_kernel<T, D>, dim3(units), kThreads, smem_k, stream, g, in(m.q), in(m.k), in(m.v), m.idx,
+                          static_cast<const float2*>(stats), in(m.dout), to(m.dk), to(m.dv));
 }
 
 }  // namespace sparse
 
 cudaError_t launch_sparse_backward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const sparse::BackwardMaps& m,
-                                   float* delta, cudaStream_t stream) {
+                                   void* workspace, int sms, cudaStream_t stream) {
     using namespace sparse;
+    float2* stats = static_cast<float2*>(workspace);
     if (dtype == SLIDE_ATTN_BF16) {
-        if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, delta, stream);
-        if (head_dim == 32) return launch_backward<__nv_bfloat16, 32>(g, B, m, delta, stream);
-        return launch_backward<__nv_bfloat16, 64>(g, B, m, delta, stream);
+        if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, stats, sms, stream);
+        if (head_dim == 32) return launch_backward<__nv_bfloat16, 32>(g, B, m, stats, sms, stream);
+        return launch_backward<__nv_bfloat16, 64>(g, B, m, stats, sms, stream);
     }
-    if (head_dim == 16) return launch_backward<float, 16>(g, B, m, delta, stream);
-    if (head_dim == 32) return launch_backward<float, 32>(g, B, m, delta, stream);
-    return launch_backward<float, 64>(g, B, m, delta, stream);
+    if (head_dim == 16) return launch_backward<float, 16>(g, B, m, stats, sms, stream);
+    if (head_dim == 32) return launch_backward<float, 32>(g, B, m, stats, sms, stream);
+    return launch_backward<float, 64>(g, B, m, stats, sms, stream);
 }
 
 }  // namespace slide_attn

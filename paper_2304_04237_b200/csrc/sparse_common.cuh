@@ -4,9 +4,13 @@
 // block of queries attends to.  A CTA keeps 64 rows (queries of one block, or keys of one block in the gradient of keys and values) and
 // takes the pixels of the listed blocks one after the other, packed into tiles without gaps whatever the blocks' sizes: each row of a
 // tile is looked up by itself and copied in pieces of 16 bytes.
+//
+// bf16: mma.sync m16n8k16 on the tiles as they are.  fp32: every tile is cut into three bf16 planes in shared memory, once for the four
+// warps (split.cuh: exact), and a product is six bf16 products, down to 2^-24 of it.
 #pragma once
 #include "common.cuh"
 #include "ptx.cuh"
+#include "split.cuh"
 
 namespace slide_attn {
 namespace sparse {
@@ -56,98 +60,172 @@ struct BackwardMaps {
 
 template <int D> __device__ __forceinline__ constexpr float root() { return D == 16 ? 0.25f : D == 32 ? 0.17677669529663688f : 0.125f; }
 
-// An entry of a list: its block and how many rows come before it.
-struct Entry { int id, start; };
+// (d0, d1) = (a0, a1) * (b0, b1) + (c0, c1)
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b0, float b1, float c0, float c1) {
+    asm("{\n\t.reg .b64 ra, rb, rc;\n\t"
+        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
+        "fma.rn.f32x2 rc, ra, rb, rc;\n\t"
+        "mov.b64 {%0, %1}, rc;\n\t}"
+        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 
-// The row of the list that a thread copies next; rows are asked for in rising order.
-struct Cursor {
-    int at = -1, start = 0, end = 0;
-    Block block = {};
-    __device__ __forceinline__ int pixel(const Geometry& g, const Entry* list, int j) {
-        while (j >= end) {
-            ++at;
-            block = block_of(g, list[at].id);
-            start = list[at].start;
-            end = start + block.size();
-        }
-        return pixel_of(g, block, j - start);
-    }
-};
-
-// 16 bytes to shared memory, zeros where there is no row.
+// 16 (4) bytes to shared memory, zeros where there is nothing to copy.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at) : "memory");
+__device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ void ldmatrix4_trans(uint32_t at, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// x = hi + lo with 11 bits each: what the three products kept of (a_hi + a_lo)(b_hi + b_lo) lose is 2^-22 of it.  Of an infinity or a NaN
-// only the product of the upper parts is to have anything: `finite` is hi, or 0 where that is not finite, and lo is 0 there.
-struct Parts { uint32_t hi, finite, lo; };
-__device__ __forceinline__ Parts split_tf32(float x) {
-    Parts p;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(p.hi) : "f"(x));
-    const float rest = x - __uint_as_float(p.hi);
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(p.lo) : "f"(rest));
-    const bool ok = (p.hi & 0x7F800000u) != 0x7F800000u;
-    p.finite = ok ? p.hi : 0u;
-    p.lo = ok ? p.lo : 0u;
-    return p;
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t at, uint32_t (&r)[4]) { split::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]); }
+
+__device__ __forceinline__ void sts128(uint32_t at, const uint32_t (&v)[4]) {
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
-// Tiles of rows of D values in shared memory, and the two products with them.  A warp's operand of 16 rows:
-//   scores:  s[n-tile] += rows . tile^T       (16 x D times D x N)
-//   gather:  o[n-tile] += weights . tile      (16 x N times N x D), the weights in the layout that `scores` leaves
-// `used`: rows of the tile that hold something; whole runs of 16 behind them are skipped.
-template <typename T, int D> struct Tile;
+// Where row `row`, 16-byte piece `piece` of a plane of bf16 rows of D values lies: pieces are exchanged by the row, so that the eight rows of
+// an ldmatrix fall into different banks.
+template <int D> __device__ __forceinline__ uint32_t plane_at(int row, int piece) {
+    const int turn = D == 64 ? row & 7 : D == 32 ? (row >> 1) & 3 : (row >> 2) & 1;
+    return (uint32_t)(row * (2 * D) + ((piece ^ turn) << 4));
+}
 
-// bf16: mma.sync m16n8k16.  Rows of 2 D bytes, their 16-byte pieces exchanged by the row so that the eight rows of an ldmatrix fall into
-// different banks.
-template <int D> struct Tile<__nv_bfloat16, D> {
-    static constexpr int kPieces = D / 8;
-    static constexpr int kRowBytes = D * 2;
+// A tile of N rows of D values as it arrives, and the planes that the tensor core reads.
+template <typename T, int D> struct Layout {
+    static constexpr bool kSplit = sizeof(T) == 4;
+    static constexpr int kPlanes = kSplit ? 3 : 1;
+    static constexpr int kPieces = D * (int)sizeof(T) / 16;      // of a row as it arrives
+    static constexpr int kRowBytes = D * (int)sizeof(T);
     static __device__ __forceinline__ uint32_t at(int row, int piece) {
-        const int turn = kPieces == 8 ? row & 7 : kPieces == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
-        return (uint32_t)(row * kRowBytes + ((piece ^ turn) << 4));
+        if constexpr (kSplit) return (uint32_t)(row * kRowBytes + piece * 16);
+        else return plane_at<D>(row, piece);
     }
-    struct Rows {
-        uint32_t a[D / 16][4];
-        __device__ __forceinline__ void load(uint32_t tile, int row0, int lane) {
+};
+
+// fp32 rows to three planes of N rows, by all threads of a CTA.
+template <int D, int N>
+__device__ __forceinline__ void cut_rows(uint32_t raw, uint32_t planes) {
+    constexpr int kGroups = N * D / 8;                           // of eight values
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                ldmatrix4(tile + at(row0 + (lane & 15), 2 * ks + (lane >> 4)), a[ks][0], a[ks][1], a[ks][2], a[ks][3]);
+    for (int i = 0; i < (kGroups + kThreads - 1) / kThreads; ++i) {
+        const int e = i * kThreads + (int)threadIdx.x;
+        if (kGroups % kThreads != 0 && e >= kGroups) break;
+        const int row = e / (D / 8), piece = e % (D / 8);
+        float2 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = split::lds_f2(raw + (uint32_t)(row * D * 4 + piece * 32 + j * 8));
+#pragma unroll
+        for (int plane = 0; plane < 3; ++plane) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j] = split::pack_upper(v[j].x, v[j].y);
+                if (plane < 2) v[j] = split::rest2(v[j]);
+            }
+            sts128(planes + (uint32_t)(plane * N * 2 * D) + plane_at<D>(row, piece), w);
         }
-    };
-    template <int NT>
-    static __device__ __forceinline__ void scores(const Rows& q, uint32_t tile, int lane, int used, float (&s)[NT][4]) {
+    }
+}
+
+// An operand of 16 rows of a warp: in registers (bf16), or where its planes lie.
+template <int D, int Planes> struct Rows;
+template <int D> struct Rows<D, 1> {
+    uint32_t a[D / 16][4];
+    __device__ __forceinline__ void load(uint32_t tile, int, int row0, int lane) {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) ldmatrix4(tile + plane_at<D>(row0 + (lane & 15), 2 * ks + (lane >> 4)), a[ks]);
+    }
+    __device__ __forceinline__ void get(int ks, int, uint32_t (&r)[1][4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[0][i] = a[ks][i];
+    }
+};
+template <int D> struct Rows<D, 3> {
+    uint32_t tile, stride;
+    int row0;
+    __device__ __forceinline__ void load(uint32_t planes, int plane_bytes, int first, int) { tile = planes; stride = (uint32_t)plane_bytes; row0 = first; }
+    __device__ __forceinline__ void get(int ks, int lane, uint32_t (&r)[3][4]) const {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) ldmatrix4(tile + p * stride + plane_at<D>(row0 + (lane & 15), 2 * ks + (lane >> 4)), r[p]);
+    }
+};
+
+// large (+)= a . b and small (+)= the five products of parts below, for two neighbouring n-tiles.  Operands that are not finite have parts
+// that are not numbers: where `large` is not finite it is the result (`settle`).
+__device__ __forceinline__ void products(float (&large0)[4], float (&large1)[4], float (&small0)[4], float (&small1)[4], const uint32_t (&a)[3][4],
+                                         const uint32_t (&b)[3][4]) {
+    constexpr int kA[5] = {2, 0, 1, 1, 0}, kB[5] = {0, 2, 1, 0, 1};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        mma_bf16(small0, a[kA[i]], b[kB[i]][0], b[kB[i]][1]);
+        mma_bf16(small1, a[kA[i]], b[kB[i]][2], b[kB[i]][3]);
+    }
+    mma_bf16(large0, a[0], b[0][0], b[0][1]);
+    mma_bf16(large1, a[0], b[0][2], b[0][3]);
+}
+__device__ __forceinline__ float settle(float large, float small) {
+    return (__float_as_uint(large) & 0x7F800000u) == 0x7F800000u ? large : large + small;
+}
+
+// s[n-tile] = rows . tile^T (16 x D times D x 8 NT); `stride`: from a plane of the tile to the next.  `used` rows of the tile hold something; runs of 16 behind them are skipped (zeros).
+template <int D, int Planes, int NT>
+__device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t tile, uint32_t stride, int lane, int used, float (&s)[NT][4]) {
+    const int row = (lane & 7) + ((lane >> 4) << 3), piece = (lane >> 3) & 1;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
+    if constexpr (Planes == 1) {
 #pragma unroll
         for (int n = 0; n < NT; n += 2) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = s[n + 1][e] = 0.0f;
             if (n * 8 < used) {
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    uint32_t b0, b1, b2, b3;
-                    ldmatrix4(tile + at(n * 8 + (lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1)), b0, b1, b2, b3);
-                    mma_bf16(s[n], q.a[ks], b0, b1);
-                    mma_bf16(s[n + 1], q.a[ks], b2, b3);
+                    uint32_t b[4];
+                    ldmatrix4(tile + plane_at<D>(n * 8 + row, 2 * ks + piece), b);
+                    mma_bf16(s[n], rows.a[ks], b[0], b[1]);
+                    mma_bf16(s[n + 1], rows.a[ks], b[2], b[3]);
                 }
             }
         }
+    } else {
+        float small[NT][4] = {};
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            uint32_t a[3][4];
+            rows.get(ks, lane, a);
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                if (n * 8 < used) {
+                    uint32_t b[3][4];
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) ldmatrix4(tile + p * stride + plane_at<D>(n * 8 + row, 2 * ks + piece), b[p]);
+                    products(s[n], s[n + 1], small[n], small[n + 1], a, b);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = settle(s[n][e], small[n][e]);
     }
-    template <int NT>
-    static __device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, int lane, int used, float (&o)[D / 8][4]) {
+}
+
+// o[n-tile] += weights . tile (16 x 8 NT times 8 NT x D), the weights as `scores` leaves them.  fp32: the tensor core truncates as it adds, so a
+// tile's sums start at zero and are added in fp32.
+template <int D, int Planes, int NT>
+__device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, uint32_t stride, int lane, int used, float (&o)[D / 8][4]) {
+    if constexpr (Planes == 1) {
 #pragma unroll
         for (int ks = 0; ks < NT / 2; ++ks) {
             if (ks * 16 < used) {
@@ -155,140 +233,211 @@ template <int D> struct Tile<__nv_bfloat16, D> {
                                        pack_bf16(w[2 * ks + 1][0], w[2 * ks + 1][1]), pack_bf16(w[2 * ks + 1][2], w[2 * ks + 1][3])};
 #pragma unroll
                 for (int n = 0; n < D / 8; n += 2) {
-                    uint32_t b0, b1, b2, b3;
-                    ldmatrix4_trans(tile + at(ks * 16 + (lane & 15), n + (lane >> 4)), b0, b1, b2, b3);
-                    mma_bf16(o[n], a, b0, b1);
-                    mma_bf16(o[n + 1], a, b2, b3);
+                    uint32_t b[4];
+                    ldmatrix4_trans(tile + plane_at<D>(ks * 16 + (lane & 15), n + (lane >> 4)), b);
+                    mma_bf16(o[n], a, b[0], b[1]);
+                    mma_bf16(o[n + 1], a, b[2], b[3]);
                 }
             }
         }
-    }
-};
-
-// fp32: mma.sync m16n8k8 with TF32 operands in two parts each and three products.  The tensor core truncates as it adds, so the small
-// products go first and a tile's sums start at zero; sums over tiles are fp32 additions.  Rows are padded by 16 bytes, which puts the
-// words of every access into different banks.
-template <int D> struct Tile<float, D> {
-    static constexpr int kPieces = D / 4;
-    static constexpr int kStride = D + 4;                // words
-    static constexpr int kRowBytes = kStride * 4;
-    static __device__ __forceinline__ uint32_t at(int row, int piece) { return (uint32_t)(row * kRowBytes + piece * 16); }
-    static __device__ __forceinline__ float word(uint32_t tile, int row, int col) {
-        float v;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(tile + (uint32_t)(row * kRowBytes + col * 4)) : "memory");
-        return v;
-    }
-    struct Rows {
-        uint32_t tile;
-        int row0;
-        __device__ __forceinline__ void load(uint32_t t, int r0, int) { tile = t; row0 = r0; }
-        __device__ __forceinline__ float value(int ks, int lane, int i) const {
-            return word(tile, row0 + (lane >> 2) + (i & 1) * 8, ks * 8 + (lane & 3) + (i >> 1) * 4);
-        }
-    };
-    template <int NT>
-    static __device__ __forceinline__ void scores(const Rows& q, uint32_t tile, int lane, int used, float (&s)[NT][4]) {
-        const int g = lane >> 2, t = lane & 3;
-        float small[NT][4];
+    } else {
+        float large[D / 8][4] = {}, small[D / 8][4] = {};
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = small[n][e] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < D / 8; ++ks) {
-            uint32_t hi[4], finite[4], lo[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Parts p = split_tf32(q.value(ks, lane, i));
-                hi[i] = p.hi; finite[i] = p.finite; lo[i] = p.lo;
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (n * 8 < used) {
-                    const Parts a = split_tf32(word(tile, n * 8 + g, ks * 8 + t)), b = split_tf32(word(tile, n * 8 + g, ks * 8 + t + 4));
-                    mma_tf32(small[n], lo, a.finite, b.finite);
-                    mma_tf32(small[n], finite, a.lo, b.lo);
-                    mma_tf32(s[n], hi, a.hi, b.hi);
-                }
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] += small[n][e];
-    }
-    // The order of the keys in a product is free: k = t and k = t + 4 of a step are keys 2 t and 2 t + 1, which is where `scores` leaves them.
-    template <int NT>
-    static __device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, int lane, int used, float (&o)[D / 8][4]) {
-        const int g = lane >> 2, t = lane & 3;
-        float sum[D / 8][4], small[D / 8][4];
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[n][e] = small[n][e] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < NT; ++ks) {
-            if (ks * 8 < used) {
-                uint32_t hi[4], finite[4], lo[4];
+        for (int ks = 0; ks < NT / 2; ++ks) {
+            if (ks * 16 < used) {
+                uint32_t a[3][4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const Parts p = split_tf32(w[ks][(i & 1) * 2 + (i >> 1)]);
-                    hi[i] = p.hi; finite[i] = p.finite; lo[i] = p.lo;
+                    float2 v = make_float2(w[2 * ks + (i >> 1)][2 * (i & 1)], w[2 * ks + (i >> 1)][2 * (i & 1) + 1]);
+                    a[0][i] = split::pack_upper(v.x, v.y);
+                    v = split::rest2(v);
+                    a[1][i] = split::pack_upper(v.x, v.y);
+                    v = split::rest2(v);
+                    a[2][i] = split::pack_upper(v.x, v.y);
                 }
 #pragma unroll
-                for (int n = 0; n < D / 8; ++n) {
-                    const Parts a = split_tf32(word(tile, ks * 8 + 2 * t, n * 8 + g)), b = split_tf32(word(tile, ks * 8 + 2 * t + 1, n * 8 + g));
-                    mma_tf32(small[n], lo, a.finite, b.finite);
-                    mma_tf32(small[n], finite, a.lo, b.lo);
-                    mma_tf32(sum[n], hi, a.hi, b.hi);
+                for (int n = 0; n < D / 8; n += 2) {
+                    uint32_t b[3][4];
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+                        ldmatrix4_trans(tile + p * stride + plane_at<D>(ks * 16 + (lane & 15), n + (lane >> 4)), b[p]);
+                    products(large[n], large[n + 1], small[n], small[n + 1], a, b);
                 }
             }
         }
 #pragma unroll
         for (int n = 0; n < D / 8; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[n][e] += sum[n][e] + small[n][e];
-    }
-};
-
-// Copies rows [0, N) of a tile: row r is pixel(r) of the head's plane in `a` (and in `b`, into the tile behind), or zeros.
-// Threads per row: kThreads / N.
-template <typename T, int D, int N, typename Pixel>
-__device__ __forceinline__ void copy_rows(uint32_t tile_a, uint32_t tile_b, const T* a, const T* b, size_t pixel_stride, int count, Pixel pixel) {
-    using L = Tile<T, D>;
-    constexpr int kPer = kThreads / N, kEach = L::kPieces / kPer;
-    static_assert(kEach >= 1 && kEach * kPer == L::kPieces, "whole pieces for each thread");
-    const int row = threadIdx.x / kPer, part = threadIdx.x % kPer;
-    const bool there = row < count;
-    const size_t off = there ? (size_t)pixel(row) * pixel_stride : 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int piece = part + i * kPer;
-        copy16(tile_a + L::at(row, piece), reinterpret_cast<const unsigned char*>(a + off) + piece * 16, there);
-        if (b) copy16(tile_b + L::at(row, piece), reinterpret_cast<const unsigned char*>(b + off) + piece * 16, there);
+            for (int e = 0; e < 4; ++e) o[n][e] += settle(large[n][e], small[n][e]);
     }
 }
 
-// The list of a block of queries, by one warp: entries that name no block are left out.  Returns the rows of all of them.
-__device__ __forceinline__ int read_list(const Geometry& g, const int* mine, Entry* list, int lane) {
-    int n = 0, total = 0;
-    for (int i0 = 0; i0 < g.top; i0 += 32) {
-        const int i = i0 + lane;
-        const int id = i < g.top ? mine[i] : -1;
-        const bool there = id >= 0 && id < g.blocks;
-        const int size = there ? block_of(g, id).size() : 0;
-        const unsigned ones = __ballot_sync(0xffffffffu, there);
-        int before = size;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int x = __shfl_up_sync(0xffffffffu, before, o);
-            if (lane >= o) before += x;
+// The row of a list that a thread copies next; rows are asked for in rising order and lie within the list.  Entries that name no block
+// hold no rows.
+struct Cursor {
+    int at, start, end;
+    Block block;
+    __device__ __forceinline__ void reset() { at = -1; start = end = 0; }
+    __device__ __forceinline__ int pixel(const Geometry& g, const int* list, int j) {
+        while (j >= end) {
+            const int id = list[++at];
+            if ((unsigned)id < (unsigned)g.blocks) {
+                block = block_of(g, id);
+                start = end;
+                end += block.size();
+            }
         }
-        if (there) list[n + __popc(ones & ((1u << lane) - 1u))] = {id, total + before - size};
-        n += __popc(ones);
-        total += __shfl_sync(0xffffffffu, before, 31);
+        return pixel_of(g, block, j - start);
     }
-    return total;
+};
+
+// Copies row threadIdx.x / (kThreads / N) of a tile (and of the tile behind it) from that pixel of a head's plane, or zeros.
+template <typename T, int D, int N>
+__device__ __forceinline__ void copy_rows(uint32_t tile_a, uint32_t tile_b, const T* a, const T* b, size_t offset, bool there) {
+    using L = Layout<T, D>;
+    constexpr int kPer = kThreads / N, kEach = L::kPieces / kPer;
+    static_assert(kEach >= 1 && kEach * kPer == L::kPieces, "whole pieces for each thread");
+    const int row = threadIdx.x / kPer, part = threadIdx.x % kPer;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int piece = part + i * kPer;
+        copy16(tile_a + L::at(row, piece), reinterpret_cast<const unsigned char*>(a + offset) + piece * 16, there);
+        if (b) copy16(tile_b + L::at(row, piece), reinterpret_cast<const unsigned char*>(b + offset) + piece * 16, there);
+    }
+}
+
+// One unit of work of the kernels that keep queries: 64 rows (part `part`) of block r, of one image and head.
+struct Unit {
+    int h, part, r;
+    long long b;
+    Block own;
+    int rows;                        // rows of this part, or none
+    __device__ __forceinline__ void find(const Geometry& g, unsigned u) {
+        h = u % g.heads; u /= g.heads;
+        part = u % g.tiles; u /= g.tiles;
+        r = u % g.blocks;
+        b = u / g.blocks;
+        own = block_of(g, r);
+        rows = min(own.size() - part * kRows, kRows);
+    }
+    __device__ __forceinline__ size_t plane(const Geometry& g, int d) const { return ((size_t)b * g.H * g.W * g.heads + h) * d; }
+    __device__ __forceinline__ const int* list(const Geometry& g, const int* idx) const { return idx + ((b * g.heads + h) * (size_t)g.blocks + r) * g.top; }
+    __device__ __forceinline__ int pixel(const Geometry& g, int row) const { return pixel_of(g, own, part * kRows + row); }
+};
+
+// What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run S - 1 tiles ahead
+// of the arithmetic, across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
+// trips to memory.  Lists come S - 1 units ahead.
+//   own0, own1: the rows that stay (queries; gradients of the output, or null);  k, v: the tiles.
+template <typename T, int D, int N, int S, int Own> struct QueryPipe {
+    using L = Layout<T, D>;
+    static constexpr int kLists = 8;                                                 // 2 S - 1 at least
+    static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
+    static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D;      // a plane holds keys and, behind them, values
+    static constexpr uint32_t kBehind = L::kSplit ? kPlane / 2 : kTile;              // from the keys to the values
+    static constexpr uint32_t kOwnAt = S * kStage, kPartsAt = kOwnAt + S * Own * kOwn;
+    static constexpr uint32_t kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0), kListsAt = kOwnPartsAt + (L::kSplit ? Own * 3 * kOwnPlane : 0);
+    static constexpr size_t kSmem = kListsAt + kLists * (kMaxTop + 1) * sizeof(int);
+
+    const Geometry& g;
+    const T *own0, *own1, *k, *v;
+    const int* idx;
+    unsigned first;
+    int items;
+    uint32_t base;
+    int* lists;
+    int* rows_of;                    // rows of an item's list
+    // the copies' place
+    int item, step, steps, listed;
+    Unit unit;
+    Cursor cursor;
+    size_t plane;
+
+    __device__ __forceinline__ QueryPipe(const Geometry& geometry, unsigned char* smem, const T* o0, const T* o1, const T* keys, const T* values,
+                                         const int* index, unsigned units, int chain)
+        : g(geometry), own0(o0), own1(o1), k(keys), v(values), idx(index) {
+        base = smem_u32(smem);
+        lists = reinterpret_cast<int*>(smem + kListsAt);
+        rows_of = lists + kLists * kMaxTop;
+        first = blockIdx.x * (unsigned)chain;
+        items = (int)min((unsigned)chain, units - first);
+        item = step = 0;
+    }
+    __device__ __forceinline__ void start() {
+        for (int i = 0; i < min(S - 1, items); ++i) {
+            Unit u;
+            u.find(g, first + i);
+            if ((int)threadIdx.x < g.top) lists[i * kMaxTop + threadIdx.x] = u.list(g, idx)[threadIdx.x];
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i < S - 1; ++i) copy(i);
+    }
+    // The copies of the tile that comes `number` tiles after the CTA's first.
+    __device__ __forceinline__ void copy(int number) {
+        if (item < items) {
+            const int* list = lists + (item % kLists) * kMaxTop;
+            if (step == 0) {
+                unit.find(g, first + item);
+                plane = unit.plane(g, D);
+                const int lane = threadIdx.x % 32;
+                listed = 0;
+                if (unit.rows > 0)
+                    for (int i = 0; i < g.top; i += 32) {
+                        const int id = i + lane < g.top ? list[i + lane] : -1;
+                        listed += (int)__reduce_add_sync(0xffffffffu, (unsigned)id < (unsigned)g.blocks ? (unsigned)block_of(g, id).size() : 0u);
+                    }
+                steps = max(1, (listed + N - 1) / N);
+                if (threadIdx.x == 0) rows_of[item % kLists] = listed;
+                cursor.reset();
+                const int row = threadIdx.x / (kThreads / kRows);
+                const bool there = row < unit.rows;
+                const uint32_t at = base + kOwnAt + (uint32_t)(item % S) * (Own * kOwn);
+                copy_rows<T, D, kRows>(at, at + kOwn, own0 + plane, Own > 1 ? own1 + plane : static_cast<const T*>(nullptr),
+                                       there ? (size_t)unit.pixel(g, row) * g.heads * D : 0, there);
+                if (item + S - 1 < items && (int)threadIdx.x < g.top) {
+                    Unit u;
+                    u.find(g, first + item + S - 1);
+                    copy4(smem_u32(lists + ((item + S - 1) % kLists) * kMaxTop + threadIdx.x), u.list(g, idx) + threadIdx.x);
+                }
+            }
+            const int j = step * N + (int)threadIdx.x / (kThreads / N);
+            const bool there = j < listed;
+            const uint32_t at = base + (uint32_t)(number % S) * kStage;
+            copy_rows<T, D, N>(at, at + kTile, k + plane, v + plane, there ? (size_t)cursor.pixel(g, list, j) * g.heads * D : 0, there);
+            if (++step == steps) { step = 0; ++item; }
+        }
+        copies_commit();
+    }
+    // Tile `number` has arrived and every thread is done with the one before; the next copies are sent for.  fp32: the tile's planes, and
+    // (`fresh`) those of the unit's own rows, are made.  Returns where the keys are.
+    __device__ __forceinline__ uint32_t next(int number, bool fresh, int compute_item) {
+        copies_wait<S - 2>();
+        __syncthreads();
+        copy(number + S - 1);
+        const uint32_t raw = base + (uint32_t)(number % S) * kStage;
+        if constexpr (!L::kSplit) return raw;
+        cut_rows<D, 2 * N>(raw, base + kPartsAt);
+        if (fresh) {
+            const uint32_t at = base + kOwnAt + (uint32_t)(compute_item % S) * (Own * kOwn);
+#pragma unroll
+            for (int o = 0; o < Own; ++o) cut_rows<D, kRows>(at + o * kOwn, base + kOwnPartsAt + o * 3 * kOwnPlane);
+        }
+        __syncthreads();
+        return base + kPartsAt;
+    }
+    __device__ __forceinline__ uint32_t own_at(int compute_item, int which) const {
+        if constexpr (L::kSplit) return base + kOwnPartsAt + which * 3 * kOwnPlane;
+        else return base + kOwnAt + (uint32_t)(compute_item % S) * (Own * kOwn) + which * kOwn;
+    }
+};
+
+// Units a CTA takes one after the other: enough for some ten tiles, while the CTAs still fill the SMs a few times over.
+inline int chain_of(const Geometry& g, unsigned units, int sms, int tile) {
+    const int steps = (g.top * g.bh * g.bw + tile - 1) / tile;
+    int chain = 1;
+    while (chain < 8 && chain * steps < 10 && units / (2 * chain) >= 8u * (unsigned)sms) chain *= 2;
+    return chain;
 }
 
 // Two neighbouring values of a row.
