@@ -31,7 +31,7 @@ template <> __device__ __forceinline__ float dot_piece<__nv_bfloat16>(const __nv
     return s;
 }
 
-// Each query's logarithm of the sum (base 2) and delta: a thread a query and head.
+// Each query's logarithm of the sum (base 2) and delta, a thread a query and head.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats)
 {
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : D == 64 ? 3 : 4)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3)
 sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, const T* dout, const float2* stats, T* dq)
 {
     using P = BackwardPipe<T, D>;
@@ -63,21 +63,21 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
     Unit unit;
     Rows<D, L::kPlanes> rows_q, rows_g;
     float dqs[D / 8][4];
-    float2 stat[2];
+    const pair scales = make_pair(scale * kLog2e, scale * kLog2e);
+    pair sums[2], deltas[2];                                 // less the logarithm, less delta; each twice
     int item = 0, step = 0, keys = 0;
-    for (int number = 0; item < pipe.items; ++number) {
-        const bool fresh = step == 0;
-        const uint32_t tile = pipe.next(number, fresh, item);
-        if (fresh) {
+    while (item < pipe.items) {
+        const uint32_t at = pipe.next();
+        if (step == 0) {
             unit.find(g, pipe.first + item);
-            keys = pipe.rows_of[item % P::kLists];
-            rows_q.load(pipe.own_at(item, 0), P::kOwnPlane, warp * 16, lane);
-            rows_g.load(pipe.own_at(item, 1), P::kOwnPlane, warp * 16, lane);
+            keys = pipe.rows_of(item);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = warp * 16 + i * 8 + (lane >> 2);
-                stat[i] = make_float2(INFINITY, 0.0f);
-                if (row < unit.rows) stat[i] = stats[((size_t)unit.b * g.H * g.W + unit.pixel(g, row)) * g.heads + unit.h];
+                float2 stat = make_float2(INFINITY, 0.0f);
+                if (row < unit.rows) stat = stats[((size_t)unit.b * g.H * g.W + unit.pixel(g, row)) * g.heads + unit.h];
+                sums[i] = make_pair(-stat.x, -stat.x);
+                deltas[i] = make_pair(-stat.y, -stat.y);
             }
 #pragma unroll
             for (int n = 0; n < D / 8; ++n)
@@ -85,31 +85,38 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                 for (int e = 0; e < 4; ++e) dqs[n][e] = 0.0f;
         }
         const bool busy = warp * 16 < unit.rows;
-        const int used = min(N, keys - step * N);
-        if (busy && used > 0) {
-            float s[NT][4], dp[NT][4];
-            scores<D, L::kPlanes, NT>(rows_q, tile, P::kPlane, lane, used, s);
-            scores<D, L::kPlanes, NT>(rows_g, tile + P::kBehind, P::kPlane, lane, used, dp);
+        if (step < P::kOwnSteps) {
+            pipe.take(at, step, warp * 16, lane, rows_q, &rows_g);
+        } else {
+            const uint32_t tile = pipe.tile(at);
+            const int used = min(N, keys - (step - P::kOwnSteps) * N);
+            if (busy) with_width<NT>(used, [&](auto width) {
+                constexpr int W = decltype(width)::value;
+                float s[W][4], dp[W][4];
+                scores<D, L::kPlanes, W>(rows_q, tile, P::kPlane, lane, s);
+                scores<D, L::kPlanes, W>(rows_g, tile + P::kBehind, P::kPlane, lane, dp);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < W; ++n)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float& x = s[n][2 * i];
-                    float& y = s[n][2 * i + 1];
-                    fma2(x, y, x, y, scale * kLog2e, scale * kLog2e, -stat[i].x, -stat[i].x);
-                    x = fast_exp2(x) * (dp[n][2 * i] - stat[i].y);
-                    y = fast_exp2(y) * (dp[n][2 * i + 1] - stat[i].y);
+                    for (int i = 0; i < 2; ++i) {
+                        float x, y;
+                        split_pair(fma2(make_pair(s[n][2 * i], s[n][2 * i + 1]), scales, sums[i]), x, y);
+                        x = fast_exp2(x);
+                        y = fast_exp2(y);
+                        split_pair(mul2(make_pair(x, y), add2(make_pair(dp[n][2 * i], dp[n][2 * i + 1]), deltas[i])), s[n][2 * i], s[n][2 * i + 1]);
+                    }
+                if (used < W * 8) {
+#pragma unroll
+                    for (int n = 0; n < W; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = 0.0f;
                 }
-            if (used < N) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = 0.0f;
-            }
-            gather<D, L::kPlanes, NT>(s, tile, P::kPlane, lane, used, dqs);
+                gather<D, L::kPlanes, W>(s, tile, P::kPlane, lane, dqs);
+            });
         }
-        if (++step * N < keys) continue;
+        ++step;
+        if (step < P::kOwnSteps || (step - P::kOwnSteps) * N < keys) continue;
         if (busy) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -133,10 +140,11 @@ template <typename T, int D> struct KeysPlan {
     static constexpr int N = BackwardPipe<T, D>::kTile / L::kRowBytes, S = sizeof(T) == 4 && D == 64 ? 2 : 3;
     static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
     static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D, kBehind = L::kSplit ? kPlane / 2 : kTile;
-    // the rows as they arrive may lie where the tiles' planes will be: these are made later
-    static constexpr uint32_t kOwnAt = S * kStage, kPartsAt = kOwnAt + 2 * kOwn, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
-    static constexpr uint32_t kListAt = kOwnPartsAt + (L::kSplit ? 6 * kOwnPlane : 0), kStatsAt = kListAt + kScan * 4;
+    // fp32: the rows that stay arrive where the stages are, and what stays are their planes
+    static constexpr uint32_t kPartsAt = S * kStage, kOwnAt = L::kSplit ? 0 : kPartsAt, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
+    static constexpr uint32_t kListAt = kOwnPartsAt + (L::kSplit ? 6 * kOwnPlane : 2 * kOwn), kStatsAt = kListAt + kScan * sizeof(Entry);
     static constexpr size_t kSmem = kStatsAt + S * N * sizeof(float2);
+    static_assert(!L::kSplit || 2 * kOwn <= kPartsAt, "room for the rows that stay");
 };
 
 template <typename T, int D>
@@ -147,9 +155,9 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     using L = Layout<T, D>;
     constexpr int N = K::N, NT = N / 8, S = K::S;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int warp_counts[kThreads / 32], warp_rows[kThreads / 32];
+    __shared__ unsigned warp_sums[kThreads / 32];
     const uint32_t base = smem_u32(smem);
-    int* list = reinterpret_cast<int*>(smem + K::kListAt);
+    Entry* list = reinterpret_cast<Entry*>(smem + K::kListAt);
     const float2* columns = reinterpret_cast<const float2*>(smem + K::kStatsAt);        // of each stage's queries
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     constexpr float scale = root<D>();
@@ -160,124 +168,141 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     if (unit.rows <= 0) return;
     const size_t plane = unit.plane(g, D);
     {
-        const int row = threadIdx.x / (kThreads / kRows);
-        const bool there = row < unit.rows;
-        copy_rows<T, D, kRows>(base + K::kOwnAt, base + K::kOwnAt + K::kOwn, k + plane, v + plane,
-                               there ? (size_t)unit.pixel(g, row) * g.heads * D : 0, there);
+        using Q = Share<T, D, kRows>;
+        const bool there = Q::row() < unit.rows;
+        const size_t off = plane + (there ? (size_t)unit.pixel(g, Q::row()) * g.heads * D : 0);
+        Q::copy(base + K::kOwnAt, reinterpret_cast<const unsigned char*>(k + off) + Q::part() * 16, there);
+        Q::copy(base + K::kOwnAt + K::kOwn, reinterpret_cast<const unsigned char*>(v + off) + Q::part() * 16, there);
         copies_commit();
     }
     const bool busy = warp * 16 < unit.rows;
     Rows<D, L::kPlanes> rows_k, rows_v;
     float dks[D / 8][4] = {}, dvs[D / 8][4] = {};
+    const pair scales = make_pair(scale * kLog2e, scale * kLog2e);
     const int* lists = idx + (unit.b * g.heads + unit.h) * (size_t)g.blocks * g.top;
     const int entries = g.blocks * g.top;
     for (int seen = 0; seen < entries; seen += kScan) {
         // the next blocks of queries that see this block, in an order that the lists alone decide
-        int mine[kScanEach], count = 0, size = 0;
+        int mine[kScanEach];
 #pragma unroll
         for (int e = 0; e < kScanEach; ++e) {
             const int i = seen + e * kThreads + (int)threadIdx.x;
             mine[e] = i < entries ? lists[i] : -1;
         }
+        unsigned sum = 0;                                    // blocks << 21 | rows: 1024 blocks of 1024 at most
 #pragma unroll
         for (int e = 0; e < kScanEach; ++e) {
             const bool is = mine[e] == unit.r;
             mine[e] = is ? (seen + e * kThreads + (int)threadIdx.x) / g.top : -1;
-            if (is) { ++count; size += block_of(g, mine[e]).size(); }
+            if (is) sum += (1u << 21) + (unsigned)block_of(g, mine[e]).size();
         }
-        int before = count;
+        unsigned before = sum;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
-            const int x = __shfl_up_sync(0xffffffffu, before, o);
+            const unsigned x = __shfl_up_sync(0xffffffffu, before, o);
             if (lane >= o) before += x;
         }
-        size = (int)__reduce_add_sync(0xffffffffu, (unsigned)size);
-        if (lane == 31) { warp_counts[warp] = before; warp_rows[warp] = size; }
+        if (lane == 31) warp_sums[warp] = before;
+        if (seen == 0) copies_wait<0>();
         __syncthreads();
-        int slot = before - count, total = 0;
+        if (seen == 0) {                                     // the rows that stay have arrived
+            if constexpr (L::kSplit)
+#pragma unroll
+                for (int o = 0; o < 2; ++o) cut_rows<D, kRows>(base + K::kOwnAt + o * K::kOwn, base + K::kOwnPartsAt + o * 3 * K::kOwnPlane);
+            rows_k.load(L::kSplit ? base + K::kOwnPartsAt : base + K::kOwnAt, K::kOwnPlane, warp * 16, lane);
+            rows_v.load(L::kSplit ? base + K::kOwnPartsAt + 3 * K::kOwnPlane : base + K::kOwnAt + K::kOwn, K::kOwnPlane, warp * 16, lane);
+        }
+        before -= sum;
+        unsigned all = 0;
 #pragma unroll
         for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) slot += warp_counts[w];
-            total += warp_rows[w];
+            if (w < warp) before += warp_sums[w];
+            all += warp_sums[w];
         }
 #pragma unroll
         for (int e = 0; e < kScanEach; ++e)
-            if (mine[e] >= 0) list[slot++] = mine[e];
+            if (mine[e] >= 0) {
+                const Block block = block_of(g, mine[e]);
+                const unsigned slot = before >> 21;
+                before += (1u << 21) + (unsigned)block.size();
+                list[slot] = Entry::of(g, block, (int)(before & 0x1FFFFFu));
+            }
         __syncthreads();
 
-        const int steps = (total + N - 1) / N;
+        const int total = (int)(all & 0x1FFFFFu), steps = (total + N - 1) / N;
+        using Q = Share<T, D, N>;
         Cursor cursor;
-        cursor.reset();
+        cursor.reset(list);
+        uint32_t stage = base, stage_stats = base + K::kStatsAt;
+        const unsigned char* from_q = reinterpret_cast<const unsigned char*>(q + plane) + Q::part() * 16;
+        const unsigned char* from_g = reinterpret_cast<const unsigned char*>(dout + plane) + Q::part() * 16;
+        const float2* from_stats = stats + (size_t)unit.b * g.H * g.W * g.heads + unit.h;
         auto copy = [&](int step) {
+            const int j = step * N + Q::row();
             if (step < steps) {
-                constexpr int kPer = kThreads / N;
-                const int row = (int)threadIdx.x / kPer, j = step * N + row;
                 const bool there = j < total;
-                const size_t pixel = there ? cursor.pixel(g, list, j) : 0;
-                const uint32_t at = base + (uint32_t)(step % S) * K::kStage;
-                copy_rows<T, D, N>(at, at + K::kTile, q + plane, dout + plane, pixel * g.heads * D, there);
-                if (there && threadIdx.x % kPer == 0) {
-                    const uint32_t to = smem_u32(columns + (step % S) * N + row);
-                    const float2* from = stats + ((size_t)unit.b * g.H * g.W + pixel) * g.heads + unit.h;
-                    copy4(to, &from->x);
-                    copy4(to + 4, &from->y);
-                }
+                const unsigned pixel = there ? (unsigned)cursor.pixel(g, j) : 0u;
+                const size_t off = (size_t)pixel * (unsigned)(g.heads * D * (int)sizeof(T));
+                Q::copy(stage, from_q + off, there);
+                Q::copy(stage + K::kTile, from_g + off, there);
+                if (there && Q::part() == 0) copy8(stage_stats + Q::row() * 8, from_stats + (size_t)pixel * (unsigned)g.heads);
             }
+            const bool last = stage == base + (S - 1) * K::kStage;
+            stage = last ? base : stage + K::kStage;
+            stage_stats = last ? base + K::kStatsAt : stage_stats + N * (uint32_t)sizeof(float2);
             copies_commit();
         };
+        uint32_t raw = base;
+        const float4* col = reinterpret_cast<const float4*>(columns) + (lane & 3);      // of two queries each
         for (int step = 0; step < S - 1; ++step) copy(step);
         for (int step = 0; step < steps; ++step) {
             copies_wait<S - 2>();
             __syncthreads();
             copy(step + S - 1);
-            const uint32_t raw = base + (uint32_t)(step % S) * K::kStage;
             uint32_t tile = raw;
-            const bool first = step == 0;
+            const float4* const stat = col;
+            const bool last = raw == base + (S - 1) * K::kStage;
+            raw = last ? base : raw + K::kStage;
+            col = last ? col - (S - 1) * N / 2 : col + N / 2;
             if constexpr (L::kSplit) {
-                cut_rows<D, 2 * N>(raw, base + K::kPartsAt);
-                if (first)
-#pragma unroll
-                    for (int o = 0; o < 2; ++o) cut_rows<D, kRows>(base + K::kOwnAt + o * K::kOwn, base + K::kOwnPartsAt + o * 3 * K::kOwnPlane);
+                cut_rows<D, 2 * N>(tile, base + K::kPartsAt);
                 __syncthreads();
                 tile = base + K::kPartsAt;
             }
             if (!busy) continue;
-            if (first) {
-                rows_k.load(L::kSplit ? base + K::kOwnPartsAt : base + K::kOwnAt, K::kOwnPlane, warp * 16, lane);
-                rows_v.load(L::kSplit ? base + K::kOwnPartsAt + 3 * K::kOwnPlane : base + K::kOwnAt + K::kOwn, K::kOwnPlane, warp * 16, lane);
-            }
-            const float4* col = reinterpret_cast<const float4*>(columns + (step % S) * N) + (lane & 3);      // two queries
             const int used = min(N, total - step * N);
-            float s[NT][4], dp[NT][4];
-            scores<D, L::kPlanes, NT>(rows_k, tile, K::kPlane, lane, used, s);
-            scores<D, L::kPlanes, NT>(rows_v, tile + K::kBehind, K::kPlane, lane, used, dp);
+            with_width<NT>(used, [&](auto width) {
+                constexpr int W = decltype(width)::value;
+                float s[W][4], dp[W][4];
+                scores<D, L::kPlanes, W>(rows_k, tile, K::kPlane, lane, s);
+                scores<D, L::kPlanes, W>(rows_v, tile + K::kBehind, K::kPlane, lane, dp);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float4 c = col[n * 4];
+                for (int n = 0; n < W; ++n) {
+                    const float4 c = stat[n * 4];
+                    const pair sums = make_pair(-c.x, -c.z), deltas = make_pair(-c.y, -c.w);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float& x = s[n][2 * i];
-                    float& y = s[n][2 * i + 1];
-                    fma2(x, y, x, y, scale * kLog2e, scale * kLog2e, -c.x, -c.z);
-                    x = fast_exp2(x);
-                    y = fast_exp2(y);
-                    dp[n][2 * i] = x * (dp[n][2 * i] - c.y);
-                    dp[n][2 * i + 1] = y * (dp[n][2 * i + 1] - c.w);
+                    for (int i = 0; i < 2; ++i) {
+                        float& x = s[n][2 * i];
+                        float& y = s[n][2 * i + 1];
+                        split_pair(fma2(make_pair(x, y), scales, sums), x, y);
+                        x = fast_exp2(x);
+                        y = fast_exp2(y);
+                        split_pair(mul2(make_pair(x, y), add2(make_pair(dp[n][2 * i], dp[n][2 * i + 1]), deltas)), dp[n][2 * i], dp[n][2 * i + 1]);
+                    }
                 }
-            }
-            if (used < N) {                                  // (a key that is not finite makes a NaN of rows that hold nothing)
+                if (used < W * 8) {                              // (a key that is not finite makes a NaN of rows that hold nothing)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int n = 0; n < W; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = dp[n][e] = 0.0f;
-            }
-            gather<D, L::kPlanes, NT>(s, tile + K::kBehind, K::kPlane, lane, used, dvs);
-            gather<D, L::kPlanes, NT>(dp, tile, K::kPlane, lane, used, dks);
+                        for (int e = 0; e < 4; ++e)
+                            if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = dp[n][e] = 0.0f;
+                }
+                gather<D, L::kPlanes, W>(s, tile + K::kBehind, K::kPlane, lane, dvs);
+                gather<D, L::kPlanes, W>(dp, tile, K::kPlane, lane, dks);
+            });
         }
         __syncthreads();                                     // the list and the tiles are free again
     }
-    copies_wait<0>();                                        // a block that nobody sees never waited for its own rows
     if (!busy) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

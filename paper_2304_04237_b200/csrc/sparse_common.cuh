@@ -8,6 +8,8 @@
 // bf16: mma.sync m16n8k16 on the tiles as they are.  fp32: every tile is cut into three bf16 planes in shared memory, once for the four
 // warps (split.cuh: exact), and a product is six bf16 products, down to 2^-24 of it.
 #pragma once
+#include <type_traits>
+
 #include "common.cuh"
 #include "ptx.cuh"
 #include "split.cuh"
@@ -60,13 +62,28 @@ struct BackwardMaps {
 
 template <int D> __device__ __forceinline__ constexpr float root() { return D == 16 ? 0.25f : D == 32 ? 0.17677669529663688f : 0.125f; }
 
-// (d0, d1) = (a0, a1) * (b0, b1) + (c0, c1)
-__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b0, float b1, float c0, float c1) {
-    asm("{\n\t.reg .b64 ra, rb, rc;\n\t"
-        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
-        "fma.rn.f32x2 rc, ra, rb, rc;\n\t"
-        "mov.b64 {%0, %1}, rc;\n\t}"
-        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+// Two fp32 values in a pair of registers, and packed operations on such pairs.  A pair of one value twice is built once, outside of the loops.
+using pair = unsigned long long;
+__device__ __forceinline__ pair make_pair(float x, float y) {
+    pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ void split_pair(pair p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ pair fma2(pair a, pair b, pair c) {
+    pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ pair add2(pair a, pair b) {
+    pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ pair mul2(pair a, pair b) {
+    pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -74,12 +91,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
-// 16 (4) bytes to shared memory, zeros where there is nothing to copy.
+// Bytes to shared memory; 16 of zeros where there is nothing to copy.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -145,10 +165,6 @@ template <int D> struct Rows<D, 1> {
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) ldmatrix4(tile + plane_at<D>(row0 + (lane & 15), 2 * ks + (lane >> 4)), a[ks]);
     }
-    __device__ __forceinline__ void get(int ks, int, uint32_t (&r)[1][4]) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[0][i] = a[ks][i];
-    }
 };
 template <int D> struct Rows<D, 3> {
     uint32_t tile, stride;
@@ -160,58 +176,63 @@ template <int D> struct Rows<D, 3> {
     }
 };
 
+template <bool First> __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (First) mma_bf16_c(c, a, b0, b1, 0.0f, 0.0f, 0.0f, 0.0f);
+    else mma_bf16(c, a, b0, b1);
+}
+
 // large (+)= a . b and small (+)= the five products of parts below, for two neighbouring n-tiles.  Operands that are not finite have parts
 // that are not numbers: where `large` is not finite it is the result (`settle`).
+template <bool First>
 __device__ __forceinline__ void products(float (&large0)[4], float (&large1)[4], float (&small0)[4], float (&small1)[4], const uint32_t (&a)[3][4],
                                          const uint32_t (&b)[3][4]) {
-    constexpr int kA[5] = {2, 0, 1, 1, 0}, kB[5] = {0, 2, 1, 0, 1};
+    mma<First>(small0, a[2], b[0][0], b[0][1]);
+    mma<First>(small1, a[2], b[0][2], b[0][3]);
+    mma<First>(large0, a[0], b[0][0], b[0][1]);
+    mma<First>(large1, a[0], b[0][2], b[0][3]);
+    constexpr int kA[4] = {0, 1, 1, 0}, kB[4] = {2, 1, 0, 1};
 #pragma unroll
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < 4; ++i) {
         mma_bf16(small0, a[kA[i]], b[kB[i]][0], b[kB[i]][1]);
         mma_bf16(small1, a[kA[i]], b[kB[i]][2], b[kB[i]][3]);
     }
-    mma_bf16(large0, a[0], b[0][0], b[0][1]);
-    mma_bf16(large1, a[0], b[0][2], b[0][3]);
 }
 __device__ __forceinline__ float settle(float large, float small) {
     return (__float_as_uint(large) & 0x7F800000u) == 0x7F800000u ? large : large + small;
 }
 
-// s[n-tile] = rows . tile^T (16 x D times D x 8 NT); `stride`: from a plane of the tile to the next.  `used` rows of the tile hold something; runs of 16 behind them are skipped (zeros).
+// s[n-tile] = rows . tile^T (16 x D times D x 8 NT); `stride`: from a plane of the tile to the next.
 template <int D, int Planes, int NT>
-__device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t tile, uint32_t stride, int lane, int used, float (&s)[NT][4]) {
+__device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t tile, uint32_t stride, int lane, float (&s)[NT][4]) {
     const int row = (lane & 7) + ((lane >> 4) << 3), piece = (lane >> 3) & 1;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
     if constexpr (Planes == 1) {
 #pragma unroll
-        for (int n = 0; n < NT; n += 2) {
-            if (n * 8 < used) {
+        for (int n = 0; n < NT; n += 2)
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    uint32_t b[4];
-                    ldmatrix4(tile + plane_at<D>(n * 8 + row, 2 * ks + piece), b);
-                    mma_bf16(s[n], rows.a[ks], b[0], b[1]);
-                    mma_bf16(s[n + 1], rows.a[ks], b[2], b[3]);
+            for (int ks = 0; ks < D / 16; ++ks) {
+                uint32_t b[4];
+                ldmatrix4(tile + n * 8 * 2 * D + plane_at<D>(row, 2 * ks + piece), b);
+                if (ks == 0) {
+                    mma<true>(s[n], rows.a[ks], b[0], b[1]);
+                    mma<true>(s[n + 1], rows.a[ks], b[2], b[3]);
+                } else {
+                    mma<false>(s[n], rows.a[ks], b[0], b[1]);
+                    mma<false>(s[n + 1], rows.a[ks], b[2], b[3]);
                 }
             }
-        }
     } else {
-        float small[NT][4] = {};
+        float small[NT][4];
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
             uint32_t a[3][4];
             rows.get(ks, lane, a);
 #pragma unroll
             for (int n = 0; n < NT; n += 2) {
-                if (n * 8 < used) {
-                    uint32_t b[3][4];
+                uint32_t b[3][4];
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) ldmatrix4(tile + p * stride + plane_at<D>(n * 8 + row, 2 * ks + piece), b[p]);
-                    products(s[n], s[n + 1], small[n], small[n + 1], a, b);
-                }
+                for (int p = 0; p < 3; ++p) ldmatrix4(tile + p * stride + n * 8 * 2 * D + plane_at<D>(row, 2 * ks + piece), b[p]);
+                if (ks == 0) products<true>(s[n], s[n + 1], small[n], small[n + 1], a, b);
+                else products<false>(s[n], s[n + 1], small[n], small[n + 1], a, b);
             }
         }
 #pragma unroll
@@ -224,45 +245,42 @@ __device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t til
 // o[n-tile] += weights . tile (16 x 8 NT times 8 NT x D), the weights as `scores` leaves them.  fp32: the tensor core truncates as it adds, so a
 // tile's sums start at zero and are added in fp32.
 template <int D, int Planes, int NT>
-__device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, uint32_t stride, int lane, int used, float (&o)[D / 8][4]) {
+__device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, uint32_t stride, int lane, float (&o)[D / 8][4]) {
+    const uint32_t at = tile;
     if constexpr (Planes == 1) {
 #pragma unroll
         for (int ks = 0; ks < NT / 2; ++ks) {
-            if (ks * 16 < used) {
-                const uint32_t a[4] = {pack_bf16(w[2 * ks][0], w[2 * ks][1]), pack_bf16(w[2 * ks][2], w[2 * ks][3]),
-                                       pack_bf16(w[2 * ks + 1][0], w[2 * ks + 1][1]), pack_bf16(w[2 * ks + 1][2], w[2 * ks + 1][3])};
+            const uint32_t a[4] = {pack_bf16(w[2 * ks][0], w[2 * ks][1]), pack_bf16(w[2 * ks][2], w[2 * ks][3]),
+                                   pack_bf16(w[2 * ks + 1][0], w[2 * ks + 1][1]), pack_bf16(w[2 * ks + 1][2], w[2 * ks + 1][3])};
 #pragma unroll
-                for (int n = 0; n < D / 8; n += 2) {
-                    uint32_t b[4];
-                    ldmatrix4_trans(tile + plane_at<D>(ks * 16 + (lane & 15), n + (lane >> 4)), b);
-                    mma_bf16(o[n], a, b[0], b[1]);
-                    mma_bf16(o[n + 1], a, b[2], b[3]);
-                }
+            for (int n = 0; n < D / 8; n += 2) {
+                uint32_t b[4];
+                ldmatrix4_trans(at + ks * 16 * 2 * D + plane_at<D>(lane & 15, n + (lane >> 4)), b);
+                mma_bf16(o[n], a, b[0], b[1]);
+                mma_bf16(o[n + 1], a, b[2], b[3]);
             }
         }
     } else {
-        float large[D / 8][4] = {}, small[D / 8][4] = {};
+        float large[D / 8][4], small[D / 8][4];
 #pragma unroll
         for (int ks = 0; ks < NT / 2; ++ks) {
-            if (ks * 16 < used) {
-                uint32_t a[3][4];
+            uint32_t a[3][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float2 v = make_float2(w[2 * ks + (i >> 1)][2 * (i & 1)], w[2 * ks + (i >> 1)][2 * (i & 1) + 1]);
-                    a[0][i] = split::pack_upper(v.x, v.y);
-                    v = split::rest2(v);
-                    a[1][i] = split::pack_upper(v.x, v.y);
-                    v = split::rest2(v);
-                    a[2][i] = split::pack_upper(v.x, v.y);
-                }
+            for (int i = 0; i < 4; ++i) {
+                float2 v = make_float2(w[2 * ks + (i >> 1)][2 * (i & 1)], w[2 * ks + (i >> 1)][2 * (i & 1) + 1]);
+                a[0][i] = split::pack_upper(v.x, v.y);
+                v = split::rest2(v);
+                a[1][i] = split::pack_upper(v.x, v.y);
+                v = split::rest2(v);
+                a[2][i] = split::pack_upper(v.x, v.y);
+            }
 #pragma unroll
-                for (int n = 0; n < D / 8; n += 2) {
-                    uint32_t b[3][4];
+            for (int n = 0; n < D / 8; n += 2) {
+                uint32_t b[3][4];
 #pragma unroll
-                    for (int p = 0; p < 3; ++p)
-                        ldmatrix4_trans(tile + p * stride + plane_at<D>(ks * 16 + (lane & 15), n + (lane >> 4)), b[p]);
-                    products(large[n], large[n + 1], small[n], small[n + 1], a, b);
-                }
+                for (int p = 0; p < 3; ++p) ldmatrix4_trans(at + p * stride + ks * 16 * 2 * D + plane_at<D>(lane & 15, n + (lane >> 4)), b[p]);
+                if (ks == 0) products<true>(large[n], large[n + 1], small[n], small[n + 1], a, b);
+                else products<false>(large[n], large[n + 1], small[n], small[n + 1], a, b);
             }
         }
 #pragma unroll
@@ -272,41 +290,63 @@ __device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, u
     }
 }
 
-// The row of a list that a thread copies next; rows are asked for in rising order and lie within the list.  Entries that name no block
-// hold no rows.
-struct Cursor {
-    int at, start, end;
-    Block block;
-    __device__ __forceinline__ void reset() { at = -1; start = end = 0; }
-    __device__ __forceinline__ int pixel(const Geometry& g, const int* list, int j) {
-        while (j >= end) {
-            const int id = list[++at];
-            if ((unsigned)id < (unsigned)g.blocks) {
-                block = block_of(g, id);
-                start = end;
-                end += block.size();
-            }
-        }
-        return pixel_of(g, block, j - start);
+// Calls f with the smallest of the tile widths (in n-tiles of 8) that holds `used` rows: straight code for each instead of a branch at each step.
+template <int NT, typename F> __device__ __forceinline__ void with_width(int used, F f) {
+    if constexpr (NT > 2) {
+        if (used <= NT * 4) return with_width<NT / 2>(used, f);
+    }
+    f(std::integral_constant<int, NT>{});
+}
+
+// An entry of a list, worked out once: the pixels of a block `width` wide whose first is `pixel`, and the list's rows up to its end.
+struct __align__(8) Entry {
+    unsigned where;                  // pixel (a map has at most 2^20), width << 21
+    int end;
+    static __device__ __forceinline__ Entry of(const Geometry& g, const Block& b, int end) {
+        return {(unsigned)(b.y0 * g.W + b.x0) | (unsigned)b.w << 21, end};
     }
 };
 
-// Copies row threadIdx.x / (kThreads / N) of a tile (and of the tile behind it) from that pixel of a head's plane, or zeros.
-template <typename T, int D, int N>
-__device__ __forceinline__ void copy_rows(uint32_t tile_a, uint32_t tile_b, const T* a, const T* b, size_t offset, bool there) {
-    using L = Layout<T, D>;
-    constexpr int kPer = kThreads / N, kEach = L::kPieces / kPer;
-    static_assert(kEach >= 1 && kEach * kPer == L::kPieces, "whole pieces for each thread");
-    const int row = threadIdx.x / kPer, part = threadIdx.x % kPer;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int piece = part + i * kPer;
-        copy16(tile_a + L::at(row, piece), reinterpret_cast<const unsigned char*>(a + offset) + piece * 16, there);
-        if (b) copy16(tile_b + L::at(row, piece), reinterpret_cast<const unsigned char*>(b + offset) + piece * 16, there);
+// The row that a thread copies next; rows are asked for in rising order and lie within the list.
+struct Cursor {
+    const Entry* next;
+    int start, end;
+    int pixel0, skip;                // the block's first pixel, and what a row of the map has beside the block's
+    float inv;                       // 1 / width
+    __device__ __forceinline__ void reset(const Entry* table) { next = table; start = end = 0; }
+    __device__ __forceinline__ int pixel(const Geometry& g, int j) {
+        if (j >= end) {
+            Entry at;
+            do {
+                at = *next++;
+                start = end;
+                end = at.end;
+            } while (j >= end);
+            const int width = (int)(at.where >> 21);
+            pixel0 = (int)(at.where & 0x1FFFFFu);
+            skip = g.W - width;
+            inv = __fdividef(1.0f, (float)width);
+        }
+        const int r = j - start, y = (int)(((float)r + 0.5f) * inv);      // exact: see pixel_of
+        return pixel0 + y * skip + r;
     }
-}
+};
 
-// One unit of work of the kernels that keep queries: 64 rows (part `part`) of block r, of one image and head.
+// Sixteen-byte pieces of a row that a thread of a tile of N rows copies: thread t row t / kPer, pieces t % kPer and every kPer-th after it.
+template <typename T, int D, int N> struct Share {
+    using L = Layout<T, D>;
+    static constexpr int kPer = kThreads / N, kEach = L::kPieces / kPer;
+    static_assert(kEach >= 1 && kEach * kPer == L::kPieces, "whole pieces for each thread");
+    static __device__ __forceinline__ int row() { return (int)threadIdx.x / kPer; }
+    static __device__ __forceinline__ int part() { return (int)threadIdx.x % kPer; }
+    // from `src`, which points at the thread's first piece, or zeros
+    static __device__ __forceinline__ void copy(uint32_t tile, const unsigned char* src, bool there) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) copy16(tile + L::at(row(), part() + i * kPer), src + i * kPer * 16, there);
+    }
+};
+
+// One unit of work: 64 rows (part `part`) of block r, of one image and head.
 struct Unit {
     int h, part, r;
     long long b;
@@ -325,18 +365,21 @@ struct Unit {
     __device__ __forceinline__ int pixel(const Geometry& g, int row) const { return pixel_of(g, own, part * kRows + row); }
 };
 
-// What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run S - 1 tiles ahead
+// What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run S - 1 steps ahead
 // of the arithmetic, across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
-// trips to memory.  Lists come S - 1 units ahead.
+// trips to memory.  Lists come S - 1 units ahead.  A unit begins with the step (or steps) that bring the rows that stay.
 //   own0, own1: the rows that stay (queries; gradients of the output, or null);  k, v: the tiles.
 template <typename T, int D, int N, int S, int Own> struct QueryPipe {
     using L = Layout<T, D>;
     static constexpr int kLists = 8;                                                 // 2 S - 1 at least
     static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
+    static constexpr int kOwnSteps = Own * kRows <= 2 * N ? 1 : Own;                 // one for all, or one each
+    static_assert(kRows <= 2 * N, "rows that stay fit a stage");
     static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D;      // a plane holds keys and, behind them, values
     static constexpr uint32_t kBehind = L::kSplit ? kPlane / 2 : kTile;              // from the keys to the values
-    static constexpr uint32_t kOwnAt = S * kStage, kPartsAt = kOwnAt + S * Own * kOwn;
-    static constexpr uint32_t kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0), kListsAt = kOwnPartsAt + (L::kSplit ? Own * 3 * kOwnPlane : 0);
+    static constexpr uint32_t kPartsAt = S * kStage, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
+    static constexpr uint32_t kTablesAt = kOwnPartsAt + (L::kSplit ? Own * 3 * kOwnPlane : 0);
+    static constexpr uint32_t kListsAt = kTablesAt + (kThreads / 32) * kMaxTop * sizeof(Entry);
     static constexpr size_t kSmem = kListsAt + kLists * (kMaxTop + 1) * sizeof(int);
 
     const Geometry& g;
@@ -346,23 +389,25 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
     int items;
     uint32_t base;
     int* lists;
-    int* rows_of;                    // rows of an item's list
-    // the copies' place
-    int item, step, steps, listed;
-    Unit unit;
+    // the copies' place: unit, step of it, rows of its list
+    int item, step, listed;
+    uint32_t stage;
     Cursor cursor;
-    size_t plane;
+    const unsigned char *from_k, *from_v;
+    uint32_t read_stage;             // the arithmetic's
 
     __device__ __forceinline__ QueryPipe(const Geometry& geometry, unsigned char* smem, const T* o0, const T* o1, const T* keys, const T* values,
                                          const int* index, unsigned units, int chain)
         : g(geometry), own0(o0), own1(o1), k(keys), v(values), idx(index) {
         base = smem_u32(smem);
         lists = reinterpret_cast<int*>(smem + kListsAt);
-        rows_of = lists + kLists * kMaxTop;
         first = blockIdx.x * (unsigned)chain;
         items = (int)min((unsigned)chain, units - first);
         item = step = 0;
+        stage = read_stage = base;
     }
+    // Rows of a unit's list, once its copies have begun.
+    __device__ __forceinline__ int& rows_of(int i) const { return lists[kLists * kMaxTop + (i & (kLists - 1))]; }
     __device__ __forceinline__ void start() {
         for (int i = 0; i < min(S - 1, items); ++i) {
             Unit u;
@@ -371,64 +416,99 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
         }
         __syncthreads();
 #pragma unroll 1
-        for (int i = 0; i < S - 1; ++i) copy(i);
+        for (int i = 0; i < S - 1; ++i) copy();
     }
-    // The copies of the tile that comes `number` tiles after the CTA's first.
-    __device__ __forceinline__ void copy(int number) {
-        if (item < items) {
-            const int* list = lists + (item % kLists) * kMaxTop;
-            if (step == 0) {
-                unit.find(g, first + item);
-                plane = unit.plane(g, D);
-                const int lane = threadIdx.x % 32;
-                listed = 0;
-                if (unit.rows > 0)
-                    for (int i = 0; i < g.top; i += 32) {
-                        const int id = i + lane < g.top ? list[i + lane] : -1;
-                        listed += (int)__reduce_add_sync(0xffffffffu, (unsigned)id < (unsigned)g.blocks ? (unsigned)block_of(g, id).size() : 0u);
-                    }
-                steps = max(1, (listed + N - 1) / N);
-                if (threadIdx.x == 0) rows_of[item % kLists] = listed;
-                cursor.reset();
-                const int row = threadIdx.x / (kThreads / kRows);
-                const bool there = row < unit.rows;
-                const uint32_t at = base + kOwnAt + (uint32_t)(item % S) * (Own * kOwn);
-                copy_rows<T, D, kRows>(at, at + kOwn, own0 + plane, Own > 1 ? own1 + plane : static_cast<const T*>(nullptr),
-                                       there ? (size_t)unit.pixel(g, row) * g.heads * D : 0, there);
-                if (item + S - 1 < items && (int)threadIdx.x < g.top) {
-                    Unit u;
-                    u.find(g, first + item + S - 1);
-                    copy4(smem_u32(lists + ((item + S - 1) % kLists) * kMaxTop + threadIdx.x), u.list(g, idx) + threadIdx.x);
+    // A unit's list (entries that name no block are left out) and the list of a unit further on.
+    __device__ __forceinline__ void open(const Unit& unit) {
+        const int* list = lists + (item & (kLists - 1)) * kMaxTop;
+        const int lane = threadIdx.x % 32;
+        Entry* table = reinterpret_cast<Entry*>(reinterpret_cast<unsigned char*>(lists) - (kListsAt - kTablesAt)) + threadIdx.x / 32 * kMaxTop;
+        listed = 0;
+        __syncwarp();                // the entries before are done with
+        if (unit.rows > 0)
+            for (int i = 0, n = 0; i < g.top; i += 32) {
+                const int id = i + lane < g.top ? list[i + lane] : -1;
+                const bool there = (unsigned)id < (unsigned)g.blocks;
+                Block block = {};
+                if (there) block = block_of(g, id);
+                int end = block.size();
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const int x = __shfl_up_sync(0xffffffffu, end, o);
+                    if (lane >= o) end += x;
                 }
+                const unsigned ones = __ballot_sync(0xffffffffu, there);
+                if (there) table[n + __popc(ones & ((1u << lane) - 1u))] = Entry::of(g, block, listed + end);
+                n += __popc(ones);
+                listed += __shfl_sync(0xffffffffu, end, 31);
             }
-            const int j = step * N + (int)threadIdx.x / (kThreads / N);
-            const bool there = j < listed;
-            const uint32_t at = base + (uint32_t)(number % S) * kStage;
-            copy_rows<T, D, N>(at, at + kTile, k + plane, v + plane, there ? (size_t)cursor.pixel(g, list, j) * g.heads * D : 0, there);
-            if (++step == steps) { step = 0; ++item; }
+        __syncwarp();
+        cursor.reset(table);
+        if (threadIdx.x == 0) rows_of(item) = listed;
+        const size_t plane = unit.plane(g, D);
+        from_k = reinterpret_cast<const unsigned char*>(k + plane) + Share<T, D, N>::part() * 16;
+        from_v = reinterpret_cast<const unsigned char*>(v + plane) + Share<T, D, N>::part() * 16;
+        const int ahead = item + S - 1;
+        if (ahead < items && (int)threadIdx.x < g.top) {
+            Unit later;
+            later.find(g, first + ahead);
+            copy4(smem_u32(lists + (ahead & (kLists - 1)) * kMaxTop + threadIdx.x), later.list(g, idx) + threadIdx.x);
         }
+    }
+    // The copies of the next step.
+    __device__ __forceinline__ void copy() {
+        if (item < items) {
+            if (step < kOwnSteps) {
+                Unit unit;
+                unit.find(g, first + item);
+                if (step == 0) open(unit);
+                using Q = Share<T, D, kRows>;
+                const bool there = Q::row() < unit.rows;
+                const size_t off = unit.plane(g, D) + (there ? (size_t)unit.pixel(g, Q::row()) * g.heads * D : 0);
+                Q::copy(stage, reinterpret_cast<const unsigned char*>((step == 0 ? own0 : own1) + off) + Q::part() * 16, there);
+                if constexpr (Own > 1 && kOwnSteps == 1) Q::copy(stage + kOwn, reinterpret_cast<const unsigned char*>(own1 + off) + Q::part() * 16, there);
+            } else {
+                using K = Share<T, D, N>;
+                const int j = (step - kOwnSteps) * N + K::row();
+                const bool there = j < listed;
+                const size_t off = there ? (size_t)((unsigned)cursor.pixel(g, j)) * (unsigned)(g.heads * D * (int)sizeof(T)) : 0;
+                K::copy(stage, from_k + off, there);
+                K::copy(stage + kTile, from_v + off, there);
+            }
+            ++step;
+            if ((step - kOwnSteps) * N >= listed && step >= kOwnSteps) { step = 0; ++item; }
+        }
+        stage = stage == base + (S - 1) * kStage ? base : stage + kStage;
         copies_commit();
     }
-    // Tile `number` has arrived and every thread is done with the one before; the next copies are sent for.  fp32: the tile's planes, and
-    // (`fresh`) those of the unit's own rows, are made.  Returns where the keys are.
-    __device__ __forceinline__ uint32_t next(int number, bool fresh, int compute_item) {
+    // What the next step brings has arrived and every thread is done with the step before; the next copies are sent for.
+    __device__ __forceinline__ uint32_t next() {
         copies_wait<S - 2>();
         __syncthreads();
-        copy(number + S - 1);
-        const uint32_t raw = base + (uint32_t)(number % S) * kStage;
-        if constexpr (!L::kSplit) return raw;
-        cut_rows<D, 2 * N>(raw, base + kPartsAt);
-        if (fresh) {
-            const uint32_t at = base + kOwnAt + (uint32_t)(compute_item % S) * (Own * kOwn);
+        copy();
+        const uint32_t at = read_stage;
+        read_stage = read_stage == base + (S - 1) * kStage ? base : read_stage + kStage;
+        return at;
+    }
+    // Takes the rows that stay from a unit's first steps.
+    __device__ __forceinline__ void take(uint32_t at, int step, int row0, int lane, Rows<D, L::kPlanes>& rows0, Rows<D, L::kPlanes>* rows1) {
 #pragma unroll
-            for (int o = 0; o < Own; ++o) cut_rows<D, kRows>(at + o * kOwn, base + kOwnPartsAt + o * 3 * kOwnPlane);
+        for (int o = 0; o < Own; ++o) {
+            if (kOwnSteps > 1 && o != step) continue;
+            uint32_t from = kOwnSteps > 1 ? at : at + o * kOwn;
+            if constexpr (L::kSplit) {
+                cut_rows<D, kRows>(from, base + kOwnPartsAt + o * 3 * kOwnPlane);        // read after the next step's barrier
+                from = base + kOwnPartsAt + o * 3 * kOwnPlane;
+            }
+            (o ? *rows1 : rows0).load(from, kOwnPlane, row0, lane);
         }
+    }
+    // The tile as the tensor core reads it: as it is, or its planes.  Returns where the keys are.
+    __device__ __forceinline__ uint32_t tile(uint32_t at) {
+        if constexpr (!L::kSplit) return at;
+        cut_rows<D, 2 * N>(at, base + kPartsAt);
         __syncthreads();
         return base + kPartsAt;
-    }
-    __device__ __forceinline__ uint32_t own_at(int compute_item, int which) const {
-        if constexpr (L::kSplit) return base + kOwnPartsAt + which * 3 * kOwnPlane;
-        else return base + kOwnAt + (uint32_t)(compute_item % S) * (Own * kOwn) + which * kOwn;
     }
 };
 

@@ -14,7 +14,7 @@ namespace sparse {
 template <typename T, int D> using ForwardPipe = QueryPipe<T, D, sizeof(T) == 4 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 2 : 3, 1>;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : D == 64 ? 4 : 5)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : D == 64 ? 3 : 4)
 sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, T* out, float* lse)
 {
     using P = ForwardPipe<T, D>;
@@ -31,73 +31,81 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
     Unit unit;
     Rows<D, L::kPlanes> rows;
     float o[D / 8][4], sum[2], base[2], limit[2];      // base: scaled; limit: the score above which it is raised
+    const pair scales = make_pair(scale, scale);
+    pair bases[2];                                     // less the base, twice
     int item = 0, step = 0, keys = 0;
-    for (int number = 0; item < pipe.items; ++number) {
-        const bool fresh = step == 0;
-        const uint32_t tile = pipe.next(number, fresh, item);
-        if (fresh) {
+    while (item < pipe.items) {
+        const uint32_t at = pipe.next();
+        if (step == 0) {
             unit.find(g, pipe.first + item);
-            keys = pipe.rows_of[item % P::kLists];
-            rows.load(pipe.own_at(item, 0), P::kOwnPlane, warp * 16, lane);
+            keys = pipe.rows_of(item);
+            pipe.take(at, 0, warp * 16, lane, rows, nullptr);
 #pragma unroll
             for (int n = 0; n < D / 8; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) { sum[i] = base[i] = 0.0f; limit[i] = -INFINITY; }
+            for (int i = 0; i < 2; ++i) { sum[i] = base[i] = 0.0f; limit[i] = -INFINITY; bases[i] = make_pair(0.0f, 0.0f); }
         }
         const bool busy = warp * 16 < unit.rows;
-        const int used = min(N, keys - step * N);
-        if (busy && used > 0) {
-            float s[NT][4];
-            scores<D, L::kPlanes, NT>(rows, tile, P::kPlane, lane, used, s);
-            if (used < N) {
+        if (step > 0) {
+            const uint32_t tile = pipe.tile(at);
+            const int used = min(N, keys - (step - 1) * N);
+            if (busy) with_width<NT>(used, [&](auto width) {
+                constexpr int W = decltype(width)::value;
+                float s[W][4];
+                scores<D, L::kPlanes, W>(rows, tile, P::kPlane, lane, s);
+                if (used < W * 8) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int n = 0; n < W; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = -INFINITY;
-            }
-            float most[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                most[i] = fmaxf(s[0][2 * i], s[0][2 * i + 1]);
-#pragma unroll
-                for (int n = 1; n < NT; ++n) most[i] = max3(most[i], s[n][2 * i], s[n][2 * i + 1]);
-            }
-            if (__any_sync(0xffffffffu, most[0] > limit[0] || most[1] > limit[1])) {
+                        for (int e = 0; e < 4; ++e)
+                            if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = -INFINITY;
+                }
+                float most[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float m = most[i];
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                    if (m > limit[i]) {
-                        const float raised = m * scale, fade = limit[i] == -INFINITY ? 0.0f : fast_exp2(base[i] - raised);
-                        base[i] = raised;
-                        limit[i] = m + 8.0f / scale;
-                        sum[i] *= fade;
+                    most[i] = fmaxf(s[0][2 * i], s[0][2 * i + 1]);
 #pragma unroll
-                        for (int n = 0; n < D / 8; ++n) { o[n][2 * i] *= fade; o[n][2 * i + 1] *= fade; }
+                    for (int n = 1; n < W; ++n) most[i] = max3(most[i], s[n][2 * i], s[n][2 * i + 1]);
+                }
+                if (__any_sync(0xffffffffu, most[0] > limit[0] || most[1] > limit[1])) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float m = most[i];
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                        if (m > limit[i]) {
+                            const float raised = m * scale, fade = limit[i] == -INFINITY ? 0.0f : fast_exp2(base[i] - raised);
+                            base[i] = raised;
+                            bases[i] = make_pair(-raised, -raised);
+                            limit[i] = m + 8.0f / scale;
+                            sum[i] *= fade;
+#pragma unroll
+                            for (int n = 0; n < D / 8; ++n) { o[n][2 * i] *= fade; o[n][2 * i + 1] *= fade; }
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float l0 = 0.0f, l1 = 0.0f;
+                for (int i = 0; i < 2; ++i) {
+                    pair l = 0;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float& x = s[n][2 * i];
-                    float& y = s[n][2 * i + 1];
-                    fma2(x, y, x, y, scale, scale, -base[i], -base[i]);
-                    x = fast_exp2(x);
-                    y = fast_exp2(y);
-                    fadd2(l0, l1, x, y);
+                    for (int n = 0; n < W; ++n) {
+                        float& x = s[n][2 * i];
+                        float& y = s[n][2 * i + 1];
+                        split_pair(fma2(make_pair(x, y), scales, bases[i]), x, y);
+                        x = fast_exp2(x);
+                        y = fast_exp2(y);
+                        l = n == 0 ? make_pair(x, y) : add2(l, make_pair(x, y));
+                    }
+                    float l0, l1;
+                    split_pair(l, l0, l1);
+                    sum[i] += l0 + l1;
                 }
-                sum[i] += l0 + l1;
-            }
-            gather<D, L::kPlanes, NT>(s, tile + P::kBehind, P::kPlane, lane, used, o);
+                gather<D, L::kPlanes, W>(s, tile + P::kBehind, P::kPlane, lane, o);
+            });
         }
-        if (++step * N < keys) continue;
+        if (step++ * N < keys) continue;
         if (busy) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
