@@ -133,9 +133,10 @@ cudaError_t launch_rank(const Geometry& g, long long B, const double* pooled, in
 
 }  // namespace sparse
 
-cudaError_t launch_select(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
+cudaError_t launch_select(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
                           int* idx, cudaStream_t stream) {
     using namespace sparse;
+    g.complete();
     const dim3 grid((unsigned)(B * g.blocks), 2);
     cudaError_t e = dtype == SLIDE_ATTN_BF16
                         ? launch_chained(pool_kernel<__nv_bfloat16>, grid, kPoolThreads, 0, stream, g, head_dim, B, static_cast<const __nv_bfloat16*>(q),

@@ -3,9 +3,9 @@
 //
 //   dS = P (dout v^T - delta),   dq = dS k / sqrt(d),   dk = dS^T q / sqrt(d),   dv = P^T dout
 //
-// Two launches: queries (dq, over the blocks of their list; also writes each query's logarithm and delta side by side) and keys (dk and dv, over
-// the blocks of queries whose lists name the key's block, found by going through the image's lists in their order).  Neither adds to
-// memory that another CTA writes, so results do not depend on which CTA runs first.
+// Three launches: each query's logarithm and delta, side by side; queries (dq, over the blocks of their list); keys (dk and dv, over the blocks of
+// queries whose lists name the key's block, found by going through the image's lists in their order).  None adds to memory that
+// another CTA writes, so results do not depend on which CTA runs first.
 #include "operators.cuh"
 
 namespace slide_attn {
@@ -31,7 +31,7 @@ template <> __device__ __forceinline__ float dot_piece<__nv_bfloat16>(const __nv
     return s;
 }
 
-// Each query's logarithm of the sum (base 2) and delta, a thread a query and head.
+// Less each query's logarithm of the sum (base 2), and less its delta: a thread a query and head.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats)
 {
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* 
     constexpr int kPiece = 16 / sizeof(T);
 #pragma unroll
     for (int e = 0; e < D; e += kPiece) s += dot_piece<T>(dout + i * D + e, out + i * D + e);
-    stats[i] = make_float2(log2_of_sum(lse[i]), s);
+    stats[i] = make_float2(-log2_of_sum(lse[i]), -s);
 }
 
 template <typename T, int D>
@@ -74,10 +74,10 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = warp * 16 + i * 8 + (lane >> 2);
-                float2 stat = make_float2(INFINITY, 0.0f);
-                if (row < unit.rows) stat = stats[((size_t)unit.b * g.H * g.W + unit.pixel(g, row)) * g.heads + unit.h];
-                sums[i] = make_pair(-stat.x, -stat.x);
-                deltas[i] = make_pair(-stat.y, -stat.y);
+                float2 stat = make_float2(-INFINITY, 0.0f);
+                if (row < unit.rows) stat = stats[(unit.image * (unsigned)(g.H * g.W) + unit.pixel(g, row)) * (unsigned)g.heads + (unsigned)unit.h];
+                sums[i] = make_pair(stat.x, stat.x);
+                deltas[i] = make_pair(stat.y, stat.y);
             }
 #pragma unroll
             for (int n = 0; n < D / 8; ++n)
@@ -122,7 +122,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
             for (int i = 0; i < 2; ++i) {
                 const int row = warp * 16 + i * 8 + (lane >> 2);
                 if (row < unit.rows) {
-                    T* dst = dq + unit.plane(g, D) + (size_t)unit.pixel(g, row) * g.heads * D + 2 * (lane & 3);
+                    T* dst = dq + unit.plane(g, D) + (size_t)unit.pixel(g, row) * (unsigned)(g.heads * D) + 2 * (lane & 3);
 #pragma unroll
                     for (int n = 0; n < D / 8; ++n) store2(dst + n * 8, dqs[n][2 * i] * scale, dqs[n][2 * i + 1] * scale);
                 }
@@ -158,7 +158,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     __shared__ unsigned warp_sums[kThreads / 32];
     const uint32_t base = smem_u32(smem);
     Entry* list = reinterpret_cast<Entry*>(smem + K::kListAt);
-    const float2* columns = reinterpret_cast<const float2*>(smem + K::kStatsAt);        // of each stage's queries
+    const float* columns = reinterpret_cast<const float*>(smem + K::kStatsAt);          // of each stage: less the logarithms, then less the deltas
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     constexpr float scale = root<D>();
 
@@ -170,7 +170,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     {
         using Q = Share<T, D, kRows>;
         const bool there = Q::row() < unit.rows;
-        const size_t off = plane + (there ? (size_t)unit.pixel(g, Q::row()) * g.heads * D : 0);
+        const size_t off = plane + (there ? (size_t)unit.pixel(g, Q::row()) * (unsigned)(g.heads * D) : 0);
         Q::copy(base + K::kOwnAt, reinterpret_cast<const unsigned char*>(k + off) + Q::part() * 16, there);
         Q::copy(base + K::kOwnAt + K::kOwn, reinterpret_cast<const unsigned char*>(v + off) + Q::part() * 16, there);
         copies_commit();
@@ -179,7 +179,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     Rows<D, L::kPlanes> rows_k, rows_v;
     float dks[D / 8][4] = {}, dvs[D / 8][4] = {};
     const pair scales = make_pair(scale * kLog2e, scale * kLog2e);
-    const int* lists = idx + (unit.b * g.heads + unit.h) * (size_t)g.blocks * g.top;
+    const int* lists = idx + unit.list * (unsigned)(g.blocks * g.top);
     const int entries = g.blocks * g.top;
     for (int seen = 0; seen < entries; seen += kScan) {
         // the next blocks of queries that see this block, in an order that the lists alone decide
@@ -193,7 +193,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
 #pragma unroll
         for (int e = 0; e < kScanEach; ++e) {
             const bool is = mine[e] == unit.r;
-            mine[e] = is ? (seen + e * kThreads + (int)threadIdx.x) / g.top : -1;
+            mine[e] = is ? (int)g.by_top.quotient((unsigned)(seen + e * kThreads) + threadIdx.x) : -1;
             if (is) sum += (1u << 21) + (unsigned)block_of(g, mine[e]).size();
         }
         unsigned before = sum;
@@ -236,7 +236,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
         uint32_t stage = base, stage_stats = base + K::kStatsAt;
         const unsigned char* from_q = reinterpret_cast<const unsigned char*>(q + plane) + Q::part() * 16;
         const unsigned char* from_g = reinterpret_cast<const unsigned char*>(dout + plane) + Q::part() * 16;
-        const float2* from_stats = stats + (size_t)unit.b * g.H * g.W * g.heads + unit.h;
+        const float2* from_stats = stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
         auto copy = [&](int step) {
             const int j = step * N + Q::row();
             if (step < steps) {
@@ -245,7 +245,8 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
                 const size_t off = (size_t)pixel * (unsigned)(g.heads * D * (int)sizeof(T));
                 Q::copy(stage, from_q + off, there);
                 Q::copy(stage + K::kTile, from_g + off, there);
-                if (there && Q::part() == 0) copy8(stage_stats + Q::row() * 8, from_stats + (size_t)pixel * (unsigned)g.heads);
+                if (there && Q::part() < 2)
+                    copy4(stage_stats + (Q::part() * N + Q::row()) * 4, reinterpret_cast<const float*>(from_stats + (size_t)pixel * (unsigned)g.heads) + Q::part());
             }
             const bool last = stage == base + (S - 1) * K::kStage;
             stage = last ? base : stage + K::kStage;
@@ -253,17 +254,17 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
             copies_commit();
         };
         uint32_t raw = base;
-        const float4* col = reinterpret_cast<const float4*>(columns) + (lane & 3);      // of two queries each
+        const pair* col = reinterpret_cast<const pair*>(columns) + (lane & 3);              // of two queries each
         for (int step = 0; step < S - 1; ++step) copy(step);
         for (int step = 0; step < steps; ++step) {
             copies_wait<S - 2>();
             __syncthreads();
             copy(step + S - 1);
             uint32_t tile = raw;
-            const float4* const stat = col;
+            const pair* const stat = col;
             const bool last = raw == base + (S - 1) * K::kStage;
             raw = last ? base : raw + K::kStage;
-            col = last ? col - (S - 1) * N / 2 : col + N / 2;
+            col = last ? col - (S - 1) * N : col + N;
             if constexpr (L::kSplit) {
                 cut_rows<D, 2 * N>(tile, base + K::kPartsAt);
                 __syncthreads();
@@ -278,8 +279,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
                 scores<D, L::kPlanes, W>(rows_v, tile + K::kBehind, K::kPlane, lane, dp);
 #pragma unroll
                 for (int n = 0; n < W; ++n) {
-                    const float4 c = stat[n * 4];
-                    const pair sums = make_pair(-c.x, -c.z), deltas = make_pair(-c.y, -c.w);
+                    const pair sums = stat[n * 4], deltas = stat[N / 2 + n * 4];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         float& x = s[n][2 * i];
@@ -308,7 +308,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     for (int i = 0; i < 2; ++i) {
         const int row = warp * 16 + i * 8 + (lane >> 2);
         if (row >= unit.rows) continue;
-        const size_t at = plane + (size_t)unit.pixel(g, row) * g.heads * D + 2 * (lane & 3);
+        const size_t at = plane + (size_t)unit.pixel(g, row) * (unsigned)(g.heads * D) + 2 * (lane & 3);
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) {
             store2(dk + at + n * 8, dks[n][2 * i] * scale, dks[n][2 * i + 1] * scale);
@@ -346,9 +346,10 @@ cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& 
 
 }  // namespace sparse
 
-cudaError_t launch_sparse_backward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const sparse::BackwardMaps& m,
+cudaError_t launch_sparse_backward(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const sparse::BackwardMaps& m,
                                    void* workspace, int sms, cudaStream_t stream) {
     using namespace sparse;
+    g.complete();
     float2* stats = static_cast<float2*>(workspace);
     if (dtype == SLIDE_ATTN_BF16) {
         if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, stats, sms, stream);

@@ -25,12 +25,35 @@ constexpr int kMaxEdge = 32;         // of a block
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// Division of numbers below 2^31 by one that is known ahead, by a multiplication (T. Granlund, P. Montgomery, "Division by invariant integers
+// using multiplication", PLDI 1994): with l the least such that 2^l >= d and m = floor(2^32 (2^l - d) / d) + 1, n / d = (m n / 2^32 + n) / 2^l.
+struct Divisor {
+    unsigned d, mul, shift;
+    static Divisor of(unsigned d) {
+        unsigned l = 0;
+        while ((1ull << l) < d) ++l;
+        return {d, (unsigned)(((1ull << 32) * ((1ull << l) - d)) / d + 1), l};
+    }
+    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
+    // n / d, and n becomes n % d
+    __device__ __forceinline__ unsigned divide(unsigned& n) const {
+        const unsigned q = quotient(n);
+        n -= q * d;
+        return q;
+    }
+};
+
 struct Geometry {
     int H, W, heads;
     int bh, bw;                      // block of pixels
     int across, blocks;              // blocks in a row of the map, and in all
     int top;                         // entries of a list
     int tiles;                       // tiles of 64 rows that a whole block takes
+    Divisor by_heads, by_tiles, by_blocks, by_across, by_top;      // set by complete()
+    void complete() {
+        by_heads = Divisor::of(heads); by_tiles = Divisor::of(tiles); by_blocks = Divisor::of(blocks);
+        by_across = Divisor::of(across); by_top = Divisor::of(top);
+    }
 };
 
 struct Block {
@@ -39,8 +62,9 @@ struct Block {
 };
 __device__ __forceinline__ Block block_of(const Geometry& g, int id) {
     Block b;
-    const int by = id / g.across, bx = id - by * g.across;
-    b.y0 = by * g.bh; b.x0 = bx * g.bw;
+    unsigned bx = (unsigned)id;
+    const unsigned by = g.by_across.divide(bx);
+    b.y0 = (int)by * g.bh; b.x0 = (int)bx * g.bw;
     b.h = min(g.bh, g.H - b.y0); b.w = min(g.bw, g.W - b.x0);
     return b;
 }
@@ -97,9 +121,6 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -348,21 +369,35 @@ template <typename T, int D, int N> struct Share {
 
 // One unit of work: 64 rows (part `part`) of block r, of one image and head.
 struct Unit {
-    int h, part, r;
-    long long b;
+    int row0, r;                     // the first row within the block
+    size_t list, image;              // (image, head) number, image number
+    int h;
     Block own;
+    float inv;                       // 1 / width
     int rows;                        // rows of this part, or none
     __device__ __forceinline__ void find(const Geometry& g, unsigned u) {
-        h = u % g.heads; u /= g.heads;
-        part = u % g.tiles; u /= g.tiles;
-        r = u % g.blocks;
-        b = u / g.blocks;
+        unsigned rest = u;
+        unsigned next = g.by_heads.divide(rest);
+        h = (int)rest;
+        rest = next;
+        next = g.by_tiles.divide(rest);
+        row0 = (int)rest * kRows;
+        rest = next;
+        next = g.by_blocks.divide(rest);
+        r = (int)rest;
+        image = next;
+        list = (size_t)next * (unsigned)g.heads + (unsigned)h;
         own = block_of(g, r);
-        rows = min(own.size() - part * kRows, kRows);
+        inv = __fdividef(1.0f, (float)own.w);
+        rows = min(own.size() - row0, kRows);
     }
-    __device__ __forceinline__ size_t plane(const Geometry& g, int d) const { return ((size_t)b * g.H * g.W * g.heads + h) * d; }
-    __device__ __forceinline__ const int* list(const Geometry& g, const int* idx) const { return idx + ((b * g.heads + h) * (size_t)g.blocks + r) * g.top; }
-    __device__ __forceinline__ int pixel(const Geometry& g, int row) const { return pixel_of(g, own, part * kRows + row); }
+    // the first element of the image's head; elements from pixel to pixel: heads d
+    __device__ __forceinline__ size_t plane(const Geometry& g, int d) const { return (image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)h) * (unsigned)d; }
+    __device__ __forceinline__ const int* entries(const Geometry& g, const int* idx) const { return idx + (list * (unsigned)g.blocks + (unsigned)r) * (unsigned)g.top; }
+    __device__ __forceinline__ unsigned pixel(const Geometry& g, int row) const {
+        const int at = row0 + row, y = (int)(((float)at + 0.5f) * inv);
+        return (unsigned)((own.y0 + y) * g.W + own.x0 + (at - y * own.w));
+    }
 };
 
 // What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run S - 1 steps ahead
@@ -379,7 +414,7 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
     static constexpr uint32_t kBehind = L::kSplit ? kPlane / 2 : kTile;              // from the keys to the values
     static constexpr uint32_t kPartsAt = S * kStage, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
     static constexpr uint32_t kTablesAt = kOwnPartsAt + (L::kSplit ? Own * 3 * kOwnPlane : 0);
-    static constexpr uint32_t kListsAt = kTablesAt + (kThreads / 32) * kMaxTop * sizeof(Entry);
+    static constexpr uint32_t kListsAt = kTablesAt + kMaxTop * sizeof(Entry);
     static constexpr size_t kSmem = kListsAt + kLists * (kMaxTop + 1) * sizeof(int);
 
     const Geometry& g;
@@ -406,25 +441,27 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
         item = step = 0;
         stage = read_stage = base;
     }
-    // Rows of a unit's list, once its copies have begun.
+    // Rows of a unit's list, from the step behind its first copies on.
     __device__ __forceinline__ int& rows_of(int i) const { return lists[kLists * kMaxTop + (i & (kLists - 1))]; }
+    __device__ __forceinline__ Entry* table() const { return reinterpret_cast<Entry*>(reinterpret_cast<unsigned char*>(lists) - (kListsAt - kTablesAt)); }
     __device__ __forceinline__ void start() {
         for (int i = 0; i < min(S - 1, items); ++i) {
             Unit u;
             u.find(g, first + i);
-            if ((int)threadIdx.x < g.top) lists[i * kMaxTop + threadIdx.x] = u.list(g, idx)[threadIdx.x];
+            if ((int)threadIdx.x < g.top) lists[i * kMaxTop + threadIdx.x] = u.entries(g, idx)[threadIdx.x];
         }
-        __syncthreads();
 #pragma unroll 1
-        for (int i = 0; i < S - 1; ++i) copy();
+        for (int i = 0; i < S - 1; ++i) {
+            __syncthreads();
+            copy();
+        }
     }
-    // A unit's list (entries that name no block are left out) and the list of a unit further on.
+    // A unit's list, by the first warp while the rows that stay are sent for (the others read it a step later; entries that name no block are
+    // left out), and the list of a unit further on.
     __device__ __forceinline__ void open(const Unit& unit) {
         const int* list = lists + (item & (kLists - 1)) * kMaxTop;
-        const int lane = threadIdx.x % 32;
-        Entry* table = reinterpret_cast<Entry*>(reinterpret_cast<unsigned char*>(lists) - (kListsAt - kTablesAt)) + threadIdx.x / 32 * kMaxTop;
-        listed = 0;
-        __syncwarp();                // the entries before are done with
+        const int lane = threadIdx.x;
+        int total = 0;
         if (unit.rows > 0)
             for (int i = 0, n = 0; i < g.top; i += 32) {
                 const int id = i + lane < g.top ? list[i + lane] : -1;
@@ -438,35 +475,41 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
                     if (lane >= o) end += x;
                 }
                 const unsigned ones = __ballot_sync(0xffffffffu, there);
-                if (there) table[n + __popc(ones & ((1u << lane) - 1u))] = Entry::of(g, block, listed + end);
+                if (there) table()[n + __popc(ones & ((1u << lane) - 1u))] = Entry::of(g, block, total + end);
                 n += __popc(ones);
-                listed += __shfl_sync(0xffffffffu, end, 31);
+                total += __shfl_sync(0xffffffffu, end, 31);
             }
-        __syncwarp();
-        cursor.reset(table);
-        if (threadIdx.x == 0) rows_of(item) = listed;
-        const size_t plane = unit.plane(g, D);
-        from_k = reinterpret_cast<const unsigned char*>(k + plane) + Share<T, D, N>::part() * 16;
-        from_v = reinterpret_cast<const unsigned char*>(v + plane) + Share<T, D, N>::part() * 16;
+        if (lane == 0) rows_of(item) = total;
         const int ahead = item + S - 1;
-        if (ahead < items && (int)threadIdx.x < g.top) {
+        if (ahead < items) {
             Unit later;
             later.find(g, first + ahead);
-            copy4(smem_u32(lists + (ahead & (kLists - 1)) * kMaxTop + threadIdx.x), later.list(g, idx) + threadIdx.x);
+            const int* from = later.entries(g, idx);
+            for (int i = lane; i < g.top; i += 32) copy4(smem_u32(lists + (ahead & (kLists - 1)) * kMaxTop + i), from + i);
         }
     }
     // The copies of the next step.
     __device__ __forceinline__ void copy() {
+        if (step == kOwnSteps) {
+            listed = rows_of(item);
+            cursor.reset(table());
+        }
+        if (step >= kOwnSteps && (step - kOwnSteps) * N >= listed) { step = 0; ++item; }
         if (item < items) {
             if (step < kOwnSteps) {
                 Unit unit;
                 unit.find(g, first + item);
-                if (step == 0) open(unit);
                 using Q = Share<T, D, kRows>;
                 const bool there = Q::row() < unit.rows;
-                const size_t off = unit.plane(g, D) + (there ? (size_t)unit.pixel(g, Q::row()) * g.heads * D : 0);
+                const size_t plane = unit.plane(g, D);
+                const size_t off = plane + (there ? (size_t)unit.pixel(g, Q::row()) * (unsigned)(g.heads * D) : 0);
                 Q::copy(stage, reinterpret_cast<const unsigned char*>((step == 0 ? own0 : own1) + off) + Q::part() * 16, there);
                 if constexpr (Own > 1 && kOwnSteps == 1) Q::copy(stage + kOwn, reinterpret_cast<const unsigned char*>(own1 + off) + Q::part() * 16, there);
+                if (step == 0) {
+                    from_k = reinterpret_cast<const unsigned char*>(k + plane) + Share<T, D, N>::part() * 16;
+                    from_v = reinterpret_cast<const unsigned char*>(v + plane) + Share<T, D, N>::part() * 16;
+                    if (threadIdx.x < 32) open(unit);
+                }
             } else {
                 using K = Share<T, D, N>;
                 const int j = (step - kOwnSteps) * N + K::row();
@@ -476,7 +519,6 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
                 K::copy(stage + kTile, from_v + off, there);
             }
             ++step;
-            if ((step - kOwnSteps) * N >= listed && step >= kOwnSteps) { step = 0; ++item; }
         }
         stage = stage == base + (S - 1) * kStage ? base : stage + kStage;
         copies_commit();

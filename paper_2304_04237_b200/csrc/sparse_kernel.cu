@@ -115,12 +115,12 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                 const int row = warp * 16 + i * 8 + (lane >> 2);
                 if (row < unit.rows) {
                     const float inv = l == 0.0f ? 0.0f : 1.0f / l;      // no keys, or none that is not -inf: zeros
-                    const int pixel = unit.pixel(g, row);
-                    T* dst = out + unit.plane(g, D) + (size_t)pixel * g.heads * D + 2 * (lane & 3);
+                    const size_t at_row = (unit.image * (unsigned)(g.H * g.W) + unit.pixel(g, row)) * (unsigned)g.heads + (unsigned)unit.h;
+                    T* dst = out + at_row * D + 2 * (lane & 3);
 #pragma unroll
                     for (int n = 0; n < D / 8; ++n) store2(dst + n * 8, o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
                     if ((lane & 3) == 0)
-                        lse[((size_t)unit.b * g.H * g.W + pixel) * g.heads + unit.h] = l == 0.0f ? -INFINITY : base[i] * kLn2 + logf(l);
+                        lse[at_row] = l == 0.0f ? -INFINITY : base[i] * kLn2 + logf(l);
                 }
             }
         }
@@ -150,9 +150,10 @@ cudaError_t launch_forward(const Geometry& g, long long B, const void* q, const 
 
 }  // namespace sparse
 
-cudaError_t launch_sparse_forward(const sparse::Geometry& g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k,
+cudaError_t launch_sparse_forward(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k,
                                   const void* v, const int* idx, void* out, float* lse, int sms, cudaStream_t stream) {
     using namespace sparse;
+    g.complete();
     if (dtype == SLIDE_ATTN_BF16) {
         if (head_dim == 16) return launch_forward<__nv_bfloat16, 16>(g, B, q, k, v, idx, out, lse, sms, stream);
         if (head_dim == 32) return launch_forward<__nv_bfloat16, 32>(g, B, q, k, v, idx, out, lse, sms, stream);
