@@ -12,7 +12,7 @@ namespace slide_attn {
 
 namespace sparse {
 
-template <typename T, int D> using BackwardPipe = QueryPipe<T, D, sizeof(T) == 4 || D == 64 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 2 : 3, 2>;
+template <typename T, int D> using BackwardPipe = QueryPipe<T, D, sizeof(T) == 4 || D == 64 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 3 : 4, 2>;
 
 // The logarithm to base 2 of a row's sum.  A row that has none (no keys, or none but -inf) has no weights: exp2 of less infinity.
 __device__ __forceinline__ float log2_of_sum(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
@@ -46,19 +46,22 @@ __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 2 : 3)
 sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, const T* dout, const float2* stats, T* dq)
 {
     using P = BackwardPipe<T, D>;
     using L = Layout<T, D>;
-    constexpr int N = (int)(P::kTile / L::kRowBytes), NT = N / 8;
+    constexpr int N = P::N, NT = N / 8;
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     constexpr float scale = root<D>();
 
     grid_dependency_wait();
-    P pipe(g, smem, q, dout, k, v, idx, units, chain);
-    pipe.start();
+    P pipe(smem, units, chain);
+    if (warp == kThreads / 32) {
+        pipe.copy_all(g, q, dout, k, v, idx);
+        return;
+    }
 
     Unit unit;
     Rows<D, L::kPlanes> rows_q, rows_g;
@@ -115,6 +118,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                 gather<D, L::kPlanes, W>(s, tile, P::kPlane, lane, dqs);
             });
         }
+        pipe.release();
         ++step;
         if (step < P::kOwnSteps || (step - P::kOwnSteps) * N < keys) continue;
         if (busy) {
@@ -134,21 +138,22 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
 }
 
 constexpr int kScanEach = 8, kScan = kScanEach * kThreads;      // entries of the image's lists that the keys' kernel looks at in one go
+constexpr int kListed = kScan + 512;                            // entries that it lists before it goes through them
 
 template <typename T, int D> struct KeysPlan {
     using L = Layout<T, D>;
-    static constexpr int N = BackwardPipe<T, D>::kTile / L::kRowBytes, S = sizeof(T) == 4 && D == 64 ? 2 : 3;
+    static constexpr int N = BackwardPipe<T, D>::N, S = BackwardPipe<T, D>::S;
     static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
     static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D, kBehind = L::kSplit ? kPlane / 2 : kTile;
     // fp32: the rows that stay arrive where the stages are, and what stays are their planes
     static constexpr uint32_t kPartsAt = S * kStage, kOwnAt = L::kSplit ? 0 : kPartsAt, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
-    static constexpr uint32_t kListAt = kOwnPartsAt + (L::kSplit ? 6 * kOwnPlane : 2 * kOwn), kStatsAt = kListAt + kScan * sizeof(Entry);
+    static constexpr uint32_t kListAt = kOwnPartsAt + (L::kSplit ? 6 * kOwnPlane : 2 * kOwn), kStatsAt = kListAt + kListed * sizeof(Entry);
     static constexpr size_t kSmem = kStatsAt + S * N * sizeof(float2);
     static_assert(!L::kSplit || 2 * kOwn <= kPartsAt, "room for the rows that stay");
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 && D == 64 ? 1 : 2)
 sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const int* idx, const float2* stats, const T* dout, T* dk, T* dv)
 {
     using K = KeysPlan<T, D>;
@@ -160,6 +165,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     Entry* list = reinterpret_cast<Entry*>(smem + K::kListAt);
     const float* columns = reinterpret_cast<const float*>(smem + K::kStatsAt);          // of each stage: less the logarithms, then less the deltas
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const bool copying = warp == kThreads / 32;
     constexpr float scale = root<D>();
 
     grid_dependency_wait();
@@ -167,12 +173,13 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     unit.find(g, blockIdx.x);
     if (unit.rows <= 0) return;
     const size_t plane = unit.plane(g, D);
-    {
-        using Q = Share<T, D, kRows>;
-        const bool there = Q::row() < unit.rows;
-        const size_t off = plane + (there ? (size_t)unit.pixel(g, Q::row()) * (unsigned)(g.heads * D) : 0);
-        Q::copy(base + K::kOwnAt, reinterpret_cast<const unsigned char*>(k + off) + Q::part() * 16, there);
-        Q::copy(base + K::kOwnAt + K::kOwn, reinterpret_cast<const unsigned char*>(v + off) + Q::part() * 16, there);
+    const unsigned pixel_bytes = (unsigned)(g.heads * D * (int)sizeof(T));
+    if (copying) {
+        unsigned pixels[kRows / 32];
+#pragma unroll
+        for (int i = 0; i < kRows / 32; ++i) pixels[i] = unit.pixel(g, lane + 32 * i);
+        Sender<T, D, kRows>::send(base + K::kOwnAt, reinterpret_cast<const unsigned char*>(k + plane), pixel_bytes, pixels, unit.rows, lane);
+        Sender<T, D, kRows>::send(base + K::kOwnAt + K::kOwn, reinterpret_cast<const unsigned char*>(v + plane), pixel_bytes, pixels, unit.rows, lane);
         copies_commit();
     }
     const bool busy = warp * 16 < unit.rows;
@@ -181,129 +188,138 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     const pair scales = make_pair(scale * kLog2e, scale * kLog2e);
     const int* lists = idx + unit.list * (unsigned)(g.blocks * g.top);
     const int entries = g.blocks * g.top;
-    for (int seen = 0; seen < entries; seen += kScan) {
+    for (int seen = 0; seen < entries;) {
         // the next blocks of queries that see this block, in an order that the lists alone decide
-        int mine[kScanEach];
+        const bool start = seen == 0;
+        unsigned listed = 0;                                 // blocks << 21 | rows: at most 1536 blocks of 1024
+        do {
+            int mine[kScanEach];
+            unsigned sum = 0;
+            if (!copying) {
 #pragma unroll
-        for (int e = 0; e < kScanEach; ++e) {
-            const int i = seen + e * kThreads + (int)threadIdx.x;
-            mine[e] = i < entries ? lists[i] : -1;
-        }
-        unsigned sum = 0;                                    // blocks << 21 | rows: 1024 blocks of 1024 at most
+                for (int e = 0; e < kScanEach; ++e) {
+                    const int i = seen + e * kThreads + (int)threadIdx.x;
+                    mine[e] = i < entries ? lists[i] : -1;
+                }
 #pragma unroll
-        for (int e = 0; e < kScanEach; ++e) {
-            const bool is = mine[e] == unit.r;
-            mine[e] = is ? (int)g.by_top.quotient((unsigned)(seen + e * kThreads) + threadIdx.x) : -1;
-            if (is) sum += (1u << 21) + (unsigned)block_of(g, mine[e]).size();
-        }
-        unsigned before = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const unsigned x = __shfl_up_sync(0xffffffffu, before, o);
-            if (lane >= o) before += x;
-        }
-        if (lane == 31) warp_sums[warp] = before;
-        if (seen == 0) copies_wait<0>();
-        __syncthreads();
-        if (seen == 0) {                                     // the rows that stay have arrived
-            if constexpr (L::kSplit)
-#pragma unroll
-                for (int o = 0; o < 2; ++o) cut_rows<D, kRows>(base + K::kOwnAt + o * K::kOwn, base + K::kOwnPartsAt + o * 3 * K::kOwnPlane);
-            rows_k.load(L::kSplit ? base + K::kOwnPartsAt : base + K::kOwnAt, K::kOwnPlane, warp * 16, lane);
-            rows_v.load(L::kSplit ? base + K::kOwnPartsAt + 3 * K::kOwnPlane : base + K::kOwnAt + K::kOwn, K::kOwnPlane, warp * 16, lane);
-        }
-        before -= sum;
-        unsigned all = 0;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += warp_sums[w];
-            all += warp_sums[w];
-        }
-#pragma unroll
-        for (int e = 0; e < kScanEach; ++e)
-            if (mine[e] >= 0) {
-                const Block block = block_of(g, mine[e]);
-                const unsigned slot = before >> 21;
-                before += (1u << 21) + (unsigned)block.size();
-                list[slot] = Entry::of(g, block, (int)(before & 0x1FFFFFu));
+                for (int e = 0; e < kScanEach; ++e) {
+                    const bool is = mine[e] == unit.r;
+                    mine[e] = is ? (int)g.by_top.quotient((unsigned)(seen + e * kThreads) + threadIdx.x) : -1;
+                    if (is) sum += (1u << 21) + (unsigned)block_of(g, mine[e]).size();
+                }
             }
-        __syncthreads();
-
-        const int total = (int)(all & 0x1FFFFFu), steps = (total + N - 1) / N;
-        using Q = Share<T, D, N>;
-        Cursor cursor;
-        cursor.reset(list);
-        uint32_t stage = base, stage_stats = base + K::kStatsAt;
-        const unsigned char* from_q = reinterpret_cast<const unsigned char*>(q + plane) + Q::part() * 16;
-        const unsigned char* from_g = reinterpret_cast<const unsigned char*>(dout + plane) + Q::part() * 16;
-        const float2* from_stats = stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
-        auto copy = [&](int step) {
-            const int j = step * N + Q::row();
-            if (step < steps) {
-                const bool there = j < total;
-                const unsigned pixel = there ? (unsigned)cursor.pixel(g, j) : 0u;
-                const size_t off = (size_t)pixel * (unsigned)(g.heads * D * (int)sizeof(T));
-                Q::copy(stage, from_q + off, there);
-                Q::copy(stage + K::kTile, from_g + off, there);
-                if (there && Q::part() < 2)
-                    copy4(stage_stats + (Q::part() * N + Q::row()) * 4, reinterpret_cast<const float*>(from_stats + (size_t)pixel * (unsigned)g.heads) + Q::part());
+            unsigned before = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const unsigned x = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += x;
             }
-            const bool last = stage == base + (S - 1) * K::kStage;
-            stage = last ? base : stage + K::kStage;
-            stage_stats = last ? base + K::kStatsAt : stage_stats + N * (uint32_t)sizeof(float2);
-            copies_commit();
-        };
-        uint32_t raw = base;
-        const pair* col = reinterpret_cast<const pair*>(columns) + (lane & 3);              // of two queries each
-        for (int step = 0; step < S - 1; ++step) copy(step);
-        for (int step = 0; step < steps; ++step) {
-            copies_wait<S - 2>();
+            if (lane == 31 && !copying) warp_sums[warp] = before;
             __syncthreads();
-            copy(step + S - 1);
-            uint32_t tile = raw;
-            const pair* const stat = col;
-            const bool last = raw == base + (S - 1) * K::kStage;
-            raw = last ? base : raw + K::kStage;
-            col = last ? col - (S - 1) * N : col + N;
-            if constexpr (L::kSplit) {
-                cut_rows<D, 2 * N>(tile, base + K::kPartsAt);
-                __syncthreads();
-                tile = base + K::kPartsAt;
+            before += listed - sum;
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) {
+                if (w < warp) before += warp_sums[w];
+                listed += warp_sums[w];
             }
-            if (!busy) continue;
-            const int used = min(N, total - step * N);
-            with_width<NT>(used, [&](auto width) {
-                constexpr int W = decltype(width)::value;
-                float s[W][4], dp[W][4];
-                scores<D, L::kPlanes, W>(rows_k, tile, K::kPlane, lane, s);
-                scores<D, L::kPlanes, W>(rows_v, tile + K::kBehind, K::kPlane, lane, dp);
+            if (!copying) {
 #pragma unroll
-                for (int n = 0; n < W; ++n) {
-                    const pair sums = stat[n * 4], deltas = stat[N / 2 + n * 4];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float& x = s[n][2 * i];
-                        float& y = s[n][2 * i + 1];
-                        split_pair(fma2(make_pair(x, y), scales, sums), x, y);
-                        x = fast_exp2(x);
-                        y = fast_exp2(y);
-                        split_pair(mul2(make_pair(x, y), add2(make_pair(dp[n][2 * i], dp[n][2 * i + 1]), deltas)), dp[n][2 * i], dp[n][2 * i + 1]);
+                for (int e = 0; e < kScanEach; ++e)
+                    if (mine[e] >= 0) {
+                        const Block block = block_of(g, mine[e]);
+                        const unsigned place = before >> 21;
+                        before += (1u << 21) + (unsigned)block.size();
+                        list[place] = Entry::of(g, block, (int)(before & 0x1FFFFFu));
                     }
-                }
-                if (used < W * 8) {                              // (a key that is not finite makes a NaN of rows that hold nothing)
+            }
+            seen += kScan;
+            if (start && copying) copies_wait<0>();
+            __syncthreads();
+        } while (seen < entries && (int)(listed >> 21) + kScan <= kListed);
+        if (start) {                                         // the rows that stay have arrived
+            if (!copying) {
+                if constexpr (L::kSplit)
 #pragma unroll
-                    for (int n = 0; n < W; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = dp[n][e] = 0.0f;
-                }
-                gather<D, L::kPlanes, W>(s, tile + K::kBehind, K::kPlane, lane, dvs);
-                gather<D, L::kPlanes, W>(dp, tile, K::kPlane, lane, dks);
-            });
+                    for (int o = 0; o < 2; ++o) cut_rows<D, kRows>(base + K::kOwnAt + o * K::kOwn, base + K::kOwnPartsAt + o * 3 * K::kOwnPlane);
+                rows_k.load(L::kSplit ? base + K::kOwnPartsAt : base + K::kOwnAt, K::kOwnPlane, warp * 16, lane);
+                rows_v.load(L::kSplit ? base + K::kOwnPartsAt + 3 * K::kOwnPlane : base + K::kOwnAt + K::kOwn, K::kOwnPlane, warp * 16, lane);
+            }
+            if constexpr (L::kSplit) __syncthreads();        // the stages are free
         }
-        __syncthreads();                                     // the list and the tiles are free again
+        const int total = (int)(listed & 0x1FFFFFu);
+        if (copying) {
+            Ring<S> ring;
+            Cursor cursor;
+            cursor.reset(list);
+            const float2* from_stats = stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
+#pragma unroll 1
+            for (int done = 0; done < total; done += N) {
+                unsigned pixels[N / 32];
+#pragma unroll
+                for (int i = 0; i < N / 32; ++i) pixels[i] = done + 32 * i + lane < total ? cursor.pixel(g, done + 32 * i + lane) : 0u;
+                ring.claim();
+                const uint32_t stage = base + (uint32_t)ring.slot * K::kStage, at = base + K::kStatsAt + (uint32_t)(ring.slot * 2 * N * 4);
+                Sender<T, D, N>::send(stage, reinterpret_cast<const unsigned char*>(q + plane), pixel_bytes, pixels, total - done, lane);
+                Sender<T, D, N>::send(stage + K::kTile, reinterpret_cast<const unsigned char*>(dout + plane), pixel_bytes, pixels, total - done, lane);
+#pragma unroll
+                for (int i = 0; i < N / 32; ++i)
+                    if (done + 32 * i + lane < total) {
+                        const float* from = reinterpret_cast<const float*>(from_stats + (size_t)pixels[i] * (unsigned)g.heads);
+                        copy4(at + (32 * i + lane) * 4, from);
+                        copy4(at + (N + 32 * i + lane) * 4, from + 1);
+                    }
+                ring.commit();
+            }
+            ring.finish();
+        } else {
+            int slot = 0;
+#pragma unroll 1
+            for (int done = 0; done < total; done += N) {
+                bar_sync<kBlock>(Ring<S>::full(slot));
+                uint32_t tile = base + (uint32_t)slot * K::kStage;
+                if constexpr (L::kSplit) {
+                    compute_sync();
+                    cut_rows<D, 2 * N>(tile, base + K::kPartsAt);
+                    compute_sync();
+                    tile = base + K::kPartsAt;
+                }
+                const pair* stat = reinterpret_cast<const pair*>(columns + slot * 2 * N) + (lane & 3);       // of two queries each
+                const int used = min(N, total - done);
+                if (busy) with_width<NT>(used, [&](auto width) {
+                    constexpr int W = decltype(width)::value;
+                    float s[W][4], dp[W][4];
+                    scores<D, L::kPlanes, W>(rows_k, tile, K::kPlane, lane, s);
+                    scores<D, L::kPlanes, W>(rows_v, tile + K::kBehind, K::kPlane, lane, dp);
+#pragma unroll
+                    for (int n = 0; n < W; ++n) {
+                        const pair sums = stat[n * 4], deltas = stat[N / 2 + n * 4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float& x = s[n][2 * i];
+                            float& y = s[n][2 * i + 1];
+                            split_pair(fma2(make_pair(x, y), scales, sums), x, y);
+                            x = fast_exp2(x);
+                            y = fast_exp2(y);
+                            split_pair(mul2(make_pair(x, y), add2(make_pair(dp[n][2 * i], dp[n][2 * i + 1]), deltas)), dp[n][2 * i], dp[n][2 * i + 1]);
+                        }
+                    }
+                    if (used < W * 8) {                          // (a key that is not finite makes a NaN of rows that hold nothing)
+#pragma unroll
+                        for (int n = 0; n < W; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = dp[n][e] = 0.0f;
+                    }
+                    gather<D, L::kPlanes, W>(s, tile + K::kBehind, K::kPlane, lane, dvs);
+                    gather<D, L::kPlanes, W>(dp, tile, K::kPlane, lane, dks);
+                });
+                bar_arrive<kBlock>(Ring<S>::empty(slot));
+                slot = Ring<S>::after(slot);
+            }
+        }
+        __syncthreads();                                     // the list is free again
     }
-    if (!busy) return;
+    if (copying || !busy) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int row = warp * 16 + i * 8 + (lane >> 2);
@@ -331,16 +347,16 @@ cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& 
         if (dev < 64) ready[dev] = true;
     }
     const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads);
-    const int chain = chain_of(g, units, sms, BackwardPipe<T, D>::kTile / Layout<T, D>::kRowBytes);
+    const int chain = chain_of(g, units, sms, BackwardPipe<T, D>::N);
     const long long n = B * g.H * g.W * g.heads;
     auto in = [](const void* p) { return static_cast<const T*>(p); };
     auto to = [](void* p) { return static_cast<T*>(p); };
     e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + 255) / 256)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats);
     if (e != cudaSuccess) return e;
-    e = launch_chained(sparse_queries_kernel<T, D>, dim3((units + chain - 1) / chain), kThreads, smem_q, stream, g, units, chain, in(m.q), in(m.k),
+    e = launch_chained(sparse_queries_kernel<T, D>, dim3((units + chain - 1) / chain), kBlock, smem_q, stream, g, units, chain, in(m.q), in(m.k),
                        in(m.v), m.idx, in(m.dout), static_cast<const float2*>(stats), to(m.dq));
     if (e != cudaSuccess) return e;
-    return launch_chained(sparse_keys_kernel<T, D>, dim3(units), kThreads, smem_k, stream, g, in(m.q), in(m.k), in(m.v), m.idx,
+    return launch_chained(sparse_keys_kernel<T, D>, dim3(units), kBlock, smem_k, stream, g, in(m.q), in(m.k), in(m.v), m.idx,
                           static_cast<const float2*>(stats), in(m.dout), to(m.dk), to(m.dv));
 }
 

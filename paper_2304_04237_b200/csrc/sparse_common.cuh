@@ -3,7 +3,8 @@
 // The map of an image is cut into blocks of bh x bw pixels (smaller at its right and lower edges); a list of blocks says which pixels a
 // block of queries attends to.  A CTA keeps 64 rows (queries of one block, or keys of one block in the gradient of keys and values) and
 // takes the pixels of the listed blocks one after the other, packed into tiles without gaps whatever the blocks' sizes: each row of a
-// tile is looked up by itself and copied in pieces of 16 bytes.
+// tile is looked up by itself and copied in pieces of 16 bytes.  A fifth warp does that for the four that compute, through a ring of stages: the
+// looking up would be a third of their instructions.  Warps wait for one another at named barriers only.
 //
 // bf16: mma.sync m16n8k16 on the tiles as they are.  fp32: every tile is cut into three bf16 planes in shared memory, once for the four
 // warps (split.cuh: exact), and a product is six bf16 products, down to 2^-24 of it.
@@ -17,7 +18,8 @@
 namespace slide_attn {
 namespace sparse {
 
-constexpr int kThreads = 128;        // four warps of 16 rows
+constexpr int kThreads = 128;        // four warps of 16 rows ...
+constexpr int kBlock = 160;          // ... and one that sends for what they need
 constexpr int kRows = 64;
 constexpr int kMaxBlocks = 1024;     // of a map
 constexpr int kMaxTop = 64;          // entries of a list
@@ -123,6 +125,18 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Named barriers of `Count` threads, by whole warps: a wait, or an arrival only.
+template <int Count> __device__ __forceinline__ void bar_sync(int id) {
+    __syncwarp();
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(Count) : "memory");
+}
+template <int Count> __device__ __forceinline__ void bar_arrive(int id) {
+    __syncwarp();
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(Count) : "memory");
+}
+constexpr int kComputeBarrier = 15;  // among the warps that compute
+__device__ __forceinline__ void compute_sync() { bar_sync<kThreads>(kComputeBarrier); }
+
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t (&r)[4]) {
@@ -228,9 +242,9 @@ __device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t til
     const int row = (lane & 7) + ((lane >> 4) << 3), piece = (lane >> 3) & 1;
     if constexpr (Planes == 1) {
 #pragma unroll
-        for (int n = 0; n < NT; n += 2)
+        for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
+            for (int n = 0; n < NT; n += 2) {
                 uint32_t b[4];
                 ldmatrix4(tile + n * 8 * 2 * D + plane_at<D>(row, 2 * ks + piece), b);
                 if (ks == 0) {
@@ -328,45 +342,6 @@ struct __align__(8) Entry {
     }
 };
 
-// The row that a thread copies next; rows are asked for in rising order and lie within the list.
-struct Cursor {
-    const Entry* next;
-    int start, end;
-    int pixel0, skip;                // the block's first pixel, and what a row of the map has beside the block's
-    float inv;                       // 1 / width
-    __device__ __forceinline__ void reset(const Entry* table) { next = table; start = end = 0; }
-    __device__ __forceinline__ int pixel(const Geometry& g, int j) {
-        if (j >= end) {
-            Entry at;
-            do {
-                at = *next++;
-                start = end;
-                end = at.end;
-            } while (j >= end);
-            const int width = (int)(at.where >> 21);
-            pixel0 = (int)(at.where & 0x1FFFFFu);
-            skip = g.W - width;
-            inv = __fdividef(1.0f, (float)width);
-        }
-        const int r = j - start, y = (int)(((float)r + 0.5f) * inv);      // exact: see pixel_of
-        return pixel0 + y * skip + r;
-    }
-};
-
-// Sixteen-byte pieces of a row that a thread of a tile of N rows copies: thread t row t / kPer, pieces t % kPer and every kPer-th after it.
-template <typename T, int D, int N> struct Share {
-    using L = Layout<T, D>;
-    static constexpr int kPer = kThreads / N, kEach = L::kPieces / kPer;
-    static_assert(kEach >= 1 && kEach * kPer == L::kPieces, "whole pieces for each thread");
-    static __device__ __forceinline__ int row() { return (int)threadIdx.x / kPer; }
-    static __device__ __forceinline__ int part() { return (int)threadIdx.x % kPer; }
-    // from `src`, which points at the thread's first piece, or zeros
-    static __device__ __forceinline__ void copy(uint32_t tile, const unsigned char* src, bool there) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) copy16(tile + L::at(row(), part() + i * kPer), src + i * kPer * 16, there);
-    }
-};
-
 // One unit of work: 64 rows (part `part`) of block r, of one image and head.
 struct Unit {
     int row0, r;                     // the first row within the block
@@ -400,146 +375,218 @@ struct Unit {
     }
 };
 
-// What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run S - 1 steps ahead
-// of the arithmetic, across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
-// trips to memory.  Lists come S - 1 units ahead.  A unit begins with the step (or steps) that bring the rows that stay.
-//   own0, own1: the rows that stay (queries; gradients of the output, or null);  k, v: the tiles.
-template <typename T, int D, int N, int S, int Own> struct QueryPipe {
+// The pixels of a list, row by row; rows are asked for in rising order and lie within the list.
+struct Cursor {
+    const Entry* next;
+    int start, end;
+    int pixel0, skip;                // the block's first pixel, and what a row of the map has beside the block's
+    float inv;                       // 1 / width
+    __device__ __forceinline__ void reset(const Entry* table) { next = table; start = end = 0; }
+    __device__ __forceinline__ unsigned pixel(const Geometry& g, int j) {
+        if (j >= end) {
+            Entry at;
+            do {
+                at = *next++;
+                start = end;
+                end = at.end;
+            } while (j >= end);
+            const int width = (int)(at.where >> 21);
+            pixel0 = (int)(at.where & 0x1FFFFFu);
+            skip = g.W - width;
+            inv = __fdividef(1.0f, (float)width);
+        }
+        const int r = j - start, y = (int)(((float)r + 0.5f) * inv);      // exact: see pixel_of
+        return (unsigned)(pixel0 + y * skip + r);
+    }
+};
+
+// The ring of S stages between the warp that copies and those that compute.  Two barriers a stage: full, empty.  The copies of three steps
+// (S = 4) may be on their way; a step is handed over when the next but one has been sent for, so that the computing warps find
+// the next step there when they are done with one.
+template <int S> struct Ring {
+    static constexpr int kLate = S - 2;                          // steps between sending for one and handing it over
+    int sent = 0, slot = 0, late_slot = 0;
+    static __device__ __forceinline__ int full(int slot) { return 1 + slot; }
+    static __device__ __forceinline__ int empty(int slot) { return 1 + S + slot; }
+    static __device__ __forceinline__ int after(int slot) { return slot == S - 1 ? 0 : slot + 1; }
+    // the copying warp: before the copies of a step ...
+    __device__ __forceinline__ void claim() { if (sent >= S) bar_sync<kBlock>(empty(slot)); }
+    // ... behind them ...
+    __device__ __forceinline__ void commit() {
+        copies_commit();
+        if (sent >= kLate) {
+            copies_wait<kLate>();
+            bar_arrive<kBlock>(full(late_slot));
+            late_slot = after(late_slot);
+        }
+        slot = after(slot);
+        ++sent;
+    }
+    // ... and at the end: the last steps are handed over, and the barriers are left as they were found.
+    __device__ __forceinline__ void finish() {
+        copies_wait<0>();
+        for (int i = min(sent, kLate); i > 0; --i) {
+            bar_arrive<kBlock>(full(late_slot));
+            late_slot = after(late_slot);
+        }
+        slot = sent >= S ? slot : 0;
+        for (int i = min(sent, S); i > 0; --i) {
+            bar_sync<kBlock>(empty(slot));
+            slot = after(slot);
+        }
+    }
+};
+
+// Copies of the copying warp: N rows, a row by as many neighbouring lanes as it has pieces.  Lane l has looked up rows l, l + 32, ...
+template <typename T, int D, int N> struct Sender {
     using L = Layout<T, D>;
-    static constexpr int kLists = 8;                                                 // 2 S - 1 at least
+    static constexpr int kRowsAtOnce = 32 / L::kPieces, kPasses = N / kRowsAtOnce, kLookups = N / 32;
+    static_assert(N % 32 == 0 && kRowsAtOnce >= 1, "rows by lanes");
+    // pixels[i]: of row lane + 32 i, anything where there is none; rows from `count` on are zeros
+    static __device__ __forceinline__ void send(uint32_t tile, const unsigned char* plane, unsigned pixel_bytes, const unsigned (&pixels)[kLookups], int count,
+                                                int lane) {
+        const int row0 = lane / L::kPieces, piece = lane % L::kPieces;
+        const unsigned char* src = plane + piece * 16;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int row = i * kRowsAtOnce + row0;
+            const unsigned pixel = __shfl_sync(0xffffffffu, pixels[i * kRowsAtOnce / 32], row & 31);
+            const bool there = row < count;
+            copy16(tile + L::at(row, piece), src + (there ? (size_t)pixel * pixel_bytes : 0), there);
+        }
+    }
+};
+
+// What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run ahead of the
+// arithmetic across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
+// trips to memory.  A unit begins with the step (or steps) that bring the rows that stay.
+//   own0, own1: the rows that stay (queries; gradients of the output, or null);  k, v: the tiles.
+template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
+    using L = Layout<T, D>;
+    static constexpr int N = N_, S = S_;
+    static constexpr int kTotals = 8;                                                // more than units that may be under way: S + 1
     static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
     static constexpr int kOwnSteps = Own * kRows <= 2 * N ? 1 : Own;                 // one for all, or one each
     static_assert(kRows <= 2 * N, "rows that stay fit a stage");
     static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D;      // a plane holds keys and, behind them, values
     static constexpr uint32_t kBehind = L::kSplit ? kPlane / 2 : kTile;              // from the keys to the values
     static constexpr uint32_t kPartsAt = S * kStage, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
-    static constexpr uint32_t kTablesAt = kOwnPartsAt + (L::kSplit ? Own * 3 * kOwnPlane : 0);
-    static constexpr uint32_t kListsAt = kTablesAt + kMaxTop * sizeof(Entry);
-    static constexpr size_t kSmem = kListsAt + kLists * (kMaxTop + 1) * sizeof(int);
+    static constexpr uint32_t kTableAt = kOwnPartsAt + (L::kSplit ? Own * 3 * kOwnPlane : 0);
+    static constexpr uint32_t kTotalsAt = kTableAt + kMaxTop * sizeof(Entry);
+    static constexpr size_t kSmem = kTotalsAt + kTotals * sizeof(int);
 
-    const Geometry& g;
-    const T *own0, *own1, *k, *v;
-    const int* idx;
+    unsigned char* smem;
+    uint32_t base;
     unsigned first;
     int items;
-    uint32_t base;
-    int* lists;
-    // the copies' place: unit, step of it, rows of its list
-    int item, step, listed;
-    uint32_t stage;
-    Cursor cursor;
-    const unsigned char *from_k, *from_v;
-    uint32_t read_stage;             // the arithmetic's
+    int slot;                                                                        // the computing warps' stage
 
-    __device__ __forceinline__ QueryPipe(const Geometry& geometry, unsigned char* smem, const T* o0, const T* o1, const T* keys, const T* values,
-                                         const int* index, unsigned units, int chain)
-        : g(geometry), own0(o0), own1(o1), k(keys), v(values), idx(index) {
-        base = smem_u32(smem);
-        lists = reinterpret_cast<int*>(smem + kListsAt);
+    __device__ __forceinline__ QueryPipe(unsigned char* memory, unsigned units, int chain) : smem(memory) {
+        base = smem_u32(memory);
         first = blockIdx.x * (unsigned)chain;
         items = (int)min((unsigned)chain, units - first);
-        item = step = 0;
-        stage = read_stage = base;
+        slot = 0;
     }
-    // Rows of a unit's list, from the step behind its first copies on.
-    __device__ __forceinline__ int& rows_of(int i) const { return lists[kLists * kMaxTop + (i & (kLists - 1))]; }
-    __device__ __forceinline__ Entry* table() const { return reinterpret_cast<Entry*>(reinterpret_cast<unsigned char*>(lists) - (kListsAt - kTablesAt)); }
-    __device__ __forceinline__ void start() {
-        for (int i = 0; i < min(S - 1, items); ++i) {
-            Unit u;
-            u.find(g, first + i);
-            if ((int)threadIdx.x < g.top) lists[i * kMaxTop + threadIdx.x] = u.entries(g, idx)[threadIdx.x];
-        }
-#pragma unroll 1
-        for (int i = 0; i < S - 1; ++i) {
-            __syncthreads();
-            copy();
-        }
-    }
-    // A unit's list, by the first warp while the rows that stay are sent for (the others read it a step later; entries that name no block are
-    // left out), and the list of a unit further on.
-    __device__ __forceinline__ void open(const Unit& unit) {
-        const int* list = lists + (item & (kLists - 1)) * kMaxTop;
-        const int lane = threadIdx.x;
-        int total = 0;
-        if (unit.rows > 0)
-            for (int i = 0, n = 0; i < g.top; i += 32) {
-                const int id = i + lane < g.top ? list[i + lane] : -1;
-                const bool there = (unsigned)id < (unsigned)g.blocks;
-                Block block = {};
-                if (there) block = block_of(g, id);
-                int end = block.size();
+    // Rows of a unit's list, known when its first step has arrived.
+    __device__ __forceinline__ int& rows_of(int i) const { return reinterpret_cast<int*>(smem + kTotalsAt)[i & (kTotals - 1)]; }
+
+    // All that the copying warp does.
+    __device__ __forceinline__ void copy_all(const Geometry& g, const T* own0, const T* own1, const T* k, const T* v, const int* idx) {
+        const int lane = threadIdx.x % 32;
+        Entry* table = reinterpret_cast<Entry*>(smem + kTableAt);
+        const unsigned pixel_bytes = (unsigned)(g.heads * D * (int)sizeof(T));
+        Ring<S> ring;
+        Unit unit;
+        unit.find(g, first);
+        int ids[kMaxTop / 32];
+        auto read = [&]() {
 #pragma unroll
-                for (int o = 1; o < 32; o *= 2) {
-                    const int x = __shfl_up_sync(0xffffffffu, end, o);
-                    if (lane >= o) end += x;
+            for (int i = 0; i < kMaxTop / 32; ++i) ids[i] = i * 32 + lane < g.top ? unit.entries(g, idx)[i * 32 + lane] : -1;
+        };
+        read();
+#pragma unroll 1
+        for (int item = 0; item < items; ++item) {
+            // the rows that stay
+            const size_t plane = unit.plane(g, D);
+            {
+                unsigned pixels[kRows / 32];
+#pragma unroll
+                for (int i = 0; i < kRows / 32; ++i) pixels[i] = unit.pixel(g, lane + 32 * i);
+#pragma unroll
+                for (int o = 0; o < kOwnSteps; ++o) {
+                    ring.claim();
+                    if (o == 0) {
+                        // the list: entries that name no block are left out
+                        int n = 0, total = 0;
+#pragma unroll
+                        for (int i = 0; i < kMaxTop / 32; ++i) {
+                            if (i * 32 >= g.top) break;
+                            const bool there = unit.rows > 0 && (unsigned)ids[i] < (unsigned)g.blocks;
+                            Block block = {};
+                            if (there) block = block_of(g, ids[i]);
+                            int end = block.size();
+#pragma unroll
+                            for (int d = 1; d < 32; d *= 2) {
+                                const int x = __shfl_up_sync(0xffffffffu, end, d);
+                                if (lane >= d) end += x;
+                            }
+                            const unsigned ones = __ballot_sync(0xffffffffu, there);
+                            if (there) table[n + __popc(ones & ((1u << lane) - 1u))] = Entry::of(g, block, total + end);
+                            n += __popc(ones);
+                            total += __shfl_sync(0xffffffffu, end, 31);
+                        }
+                        if (lane == 0) rows_of(item) = total;
+                        __syncwarp();
+                    }
+                    const uint32_t stage = base + (uint32_t)ring.slot * kStage;
+                    Sender<T, D, kRows>::send(stage, reinterpret_cast<const unsigned char*>((o ? own1 : own0) + plane), pixel_bytes, pixels, unit.rows, lane);
+                    if constexpr (Own > 1 && kOwnSteps == 1)
+                        Sender<T, D, kRows>::send(stage + kOwn, reinterpret_cast<const unsigned char*>(own1 + plane), pixel_bytes, pixels, unit.rows, lane);
+                    ring.commit();
                 }
-                const unsigned ones = __ballot_sync(0xffffffffu, there);
-                if (there) table()[n + __popc(ones & ((1u << lane) - 1u))] = Entry::of(g, block, total + end);
-                n += __popc(ones);
-                total += __shfl_sync(0xffffffffu, end, 31);
             }
-        if (lane == 0) rows_of(item) = total;
-        const int ahead = item + S - 1;
-        if (ahead < items) {
-            Unit later;
-            later.find(g, first + ahead);
-            const int* from = later.entries(g, idx);
-            for (int i = lane; i < g.top; i += 32) copy4(smem_u32(lists + (ahead & (kLists - 1)) * kMaxTop + i), from + i);
-        }
-    }
-    // The copies of the next step.
-    __device__ __forceinline__ void copy() {
-        if (step == kOwnSteps) {
-            listed = rows_of(item);
-            cursor.reset(table());
-        }
-        if (step >= kOwnSteps && (step - kOwnSteps) * N >= listed) { step = 0; ++item; }
-        if (item < items) {
-            if (step < kOwnSteps) {
-                Unit unit;
-                unit.find(g, first + item);
-                using Q = Share<T, D, kRows>;
-                const bool there = Q::row() < unit.rows;
-                const size_t plane = unit.plane(g, D);
-                const size_t off = plane + (there ? (size_t)unit.pixel(g, Q::row()) * (unsigned)(g.heads * D) : 0);
-                Q::copy(stage, reinterpret_cast<const unsigned char*>((step == 0 ? own0 : own1) + off) + Q::part() * 16, there);
-                if constexpr (Own > 1 && kOwnSteps == 1) Q::copy(stage + kOwn, reinterpret_cast<const unsigned char*>(own1 + off) + Q::part() * 16, there);
-                if (step == 0) {
-                    from_k = reinterpret_cast<const unsigned char*>(k + plane) + Share<T, D, N>::part() * 16;
-                    from_v = reinterpret_cast<const unsigned char*>(v + plane) + Share<T, D, N>::part() * 16;
-                    if (threadIdx.x < 32) open(unit);
-                }
-            } else {
-                using K = Share<T, D, N>;
-                const int j = (step - kOwnSteps) * N + K::row();
-                const bool there = j < listed;
-                const size_t off = there ? (size_t)((unsigned)cursor.pixel(g, j)) * (unsigned)(g.heads * D * (int)sizeof(T)) : 0;
-                K::copy(stage, from_k + off, there);
-                K::copy(stage + kTile, from_v + off, there);
+            const int total = rows_of(item);
+            if (item + 1 < items) {
+                unit.find(g, first + item + 1);
+                read();                                          // on its way while this unit's tiles are sent for
             }
-            ++step;
+            Cursor cursor;
+            cursor.reset(table);
+#pragma unroll 1
+            for (int done = 0; done < total; done += N) {
+                unsigned pixels[N / 32];
+#pragma unroll
+                for (int i = 0; i < N / 32; ++i) pixels[i] = done + 32 * i + lane < total ? cursor.pixel(g, done + 32 * i + lane) : 0u;
+                ring.claim();
+                const uint32_t stage = base + (uint32_t)ring.slot * kStage;
+                Sender<T, D, N>::send(stage, reinterpret_cast<const unsigned char*>(k + plane), pixel_bytes, pixels, total - done, lane);
+                Sender<T, D, N>::send(stage + kTile, reinterpret_cast<const unsigned char*>(v + plane), pixel_bytes, pixels, total - done, lane);
+                ring.commit();
+            }
+            __syncwarp();                                        // the table is free again
         }
-        stage = stage == base + (S - 1) * kStage ? base : stage + kStage;
-        copies_commit();
+        ring.finish();
     }
-    // What the next step brings has arrived and every thread is done with the step before; the next copies are sent for.
+
+    // The computing warps: what the next step brings has arrived ...
     __device__ __forceinline__ uint32_t next() {
-        copies_wait<S - 2>();
-        __syncthreads();
-        copy();
-        const uint32_t at = read_stage;
-        read_stage = read_stage == base + (S - 1) * kStage ? base : read_stage + kStage;
-        return at;
+        bar_sync<kBlock>(Ring<S>::full(slot));
+        return base + (uint32_t)slot * kStage;
+    }
+    // ... and is not needed any more.
+    __device__ __forceinline__ void release() {
+        bar_arrive<kBlock>(Ring<S>::empty(slot));
+        slot = Ring<S>::after(slot);
     }
     // Takes the rows that stay from a unit's first steps.
     __device__ __forceinline__ void take(uint32_t at, int step, int row0, int lane, Rows<D, L::kPlanes>& rows0, Rows<D, L::kPlanes>* rows1) {
+        if constexpr (L::kSplit) compute_sync();                 // nobody reads the planes of the unit before any more
 #pragma unroll
         for (int o = 0; o < Own; ++o) {
             if (kOwnSteps > 1 && o != step) continue;
             uint32_t from = kOwnSteps > 1 ? at : at + o * kOwn;
             if constexpr (L::kSplit) {
-                cut_rows<D, kRows>(from, base + kOwnPartsAt + o * 3 * kOwnPlane);        // read after the next step's barrier
+                cut_rows<D, kRows>(from, base + kOwnPartsAt + o * 3 * kOwnPlane);        // read behind a later barrier
                 from = base + kOwnPartsAt + o * 3 * kOwnPlane;
             }
             (o ? *rows1 : rows0).load(from, kOwnPlane, row0, lane);
@@ -548,8 +595,9 @@ template <typename T, int D, int N, int S, int Own> struct QueryPipe {
     // The tile as the tensor core reads it: as it is, or its planes.  Returns where the keys are.
     __device__ __forceinline__ uint32_t tile(uint32_t at) {
         if constexpr (!L::kSplit) return at;
+        compute_sync();                                          // nobody reads the planes of the tile before any more
         cut_rows<D, 2 * N>(at, base + kPartsAt);
-        __syncthreads();
+        compute_sync();
         return base + kPartsAt;
     }
 };

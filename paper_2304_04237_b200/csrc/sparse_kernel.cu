@@ -11,22 +11,25 @@ namespace slide_attn {
 
 namespace sparse {
 
-template <typename T, int D> using ForwardPipe = QueryPipe<T, D, sizeof(T) == 4 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 2 : 3, 1>;
+template <typename T, int D> using ForwardPipe = QueryPipe<T, D, sizeof(T) == 4 || D == 64 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 3 : 4, 1>;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : D == 64 ? 3 : 4)
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 || D == 64 ? 3 : 4)
 sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, T* out, float* lse)
 {
     using P = ForwardPipe<T, D>;
     using L = Layout<T, D>;
-    constexpr int N = (int)(P::kTile / L::kRowBytes), NT = N / 8;
+    constexpr int N = P::N, NT = N / 8;
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     constexpr float scale = root<D>() * kLog2e;
 
     grid_dependency_wait();
-    P pipe(g, smem, q, nullptr, k, v, idx, units, chain);
-    pipe.start();
+    P pipe(smem, units, chain);
+    if (warp == kThreads / 32) {
+        pipe.copy_all(g, q, nullptr, k, v, idx);
+        return;
+    }
 
     Unit unit;
     Rows<D, L::kPlanes> rows;
@@ -105,6 +108,7 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                 gather<D, L::kPlanes, W>(s, tile + P::kBehind, P::kPlane, lane, o);
             });
         }
+        pipe.release();
         if (step++ * N < keys) continue;
         if (busy) {
 #pragma unroll
@@ -143,8 +147,8 @@ cudaError_t launch_forward(const Geometry& g, long long B, const void* q, const 
         if (dev < 64) ready[dev] = true;
     }
     const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads);
-    const int chain = chain_of(g, units, sms, sizeof(T) == 4 ? 32 : 64);
-    return launch_chained(sparse_forward_kernel<T, D>, dim3((units + chain - 1) / chain), kThreads, smem, stream, g, units, chain,
+    const int chain = chain_of(g, units, sms, ForwardPipe<T, D>::N);
+    return launch_chained(sparse_forward_kernel<T, D>, dim3((units + chain - 1) / chain), kBlock, smem, stream, g, units, chain,
                           static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), idx, static_cast<T*>(out), lse);
 }
 
