@@ -12,6 +12,7 @@
 #include <cooperative_groups.h>
 
 #include "operators.cuh"
+#include "packed.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -23,12 +24,12 @@ constexpr int kMaxCluster = 16;
 constexpr int kMaxSmem = 227 * 1024;
 constexpr int kMostSms = 160;
 
-// How a call is cut up: slabs of `width` channels, clusters of `cluster` CTAs, of whose pixels `cached` rows stay in shared memory.
+// How a call is cut up: slabs of `width` channels, clusters of `cluster` CTAs, of whose pixels `cached` rounds of `rows` stay in shared memory.
 struct NormPlan {
     int P, C, groups, per_group;       // per_group: channels of a group
-    int width, slabs, cluster;
+    int width, slabs, cluster, log_cluster;
     int columns, rows, threads;        // 16-byte columns of a slab; pixel rows that a CTA takes at a time
-    int cached;                        // rows x this many rounds of pixels stay in shared memory
+    int cached;
     size_t smem;
     long long blocks;
 };
@@ -45,40 +46,89 @@ struct NormArgs {
     float eps;
 };
 
+// Sixteen bytes of channels as pairs of fp32 values.
 template <typename T> struct Vec;
 template <> struct Vec<float> {
-    static constexpr int n = 4;
-    static __device__ __forceinline__ void get(const uint4& r, float (&v)[4]) {
-        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    static constexpr int pairs = 2;
+    static __device__ __forceinline__ void get(const uint4& r, pair (&v)[2]) {
+        v[0] = make_pair(__uint_as_float(r.x), __uint_as_float(r.y));
+        v[1] = make_pair(__uint_as_float(r.z), __uint_as_float(r.w));
     }
-    static __device__ __forceinline__ uint4 put(const float (&v)[4]) {
-        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    static __device__ __forceinline__ uint4 put(const pair (&v)[2]) {
+        float a, b, c, d;
+        split_pair(v[0], a, b);
+        split_pair(v[1], c, d);
+        return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
     }
 };
 template <> struct Vec<__nv_bfloat16> {
-    static constexpr int n = 8;
-    static __device__ __forceinline__ void get(const uint4& r, float (&v)[8]) {
-        v[0] = bf16_lo(r.x); v[1] = bf16_hi(r.x); v[2] = bf16_lo(r.y); v[3] = bf16_hi(r.y);
-        v[4] = bf16_lo(r.z); v[5] = bf16_hi(r.z); v[6] = bf16_lo(r.w); v[7] = bf16_hi(r.w);
+    static constexpr int pairs = 4;
+    static __device__ __forceinline__ void get(const uint4& r, pair (&v)[4]) {
+        v[0] = make_pair(bf16_lo(r.x), bf16_hi(r.x));
+        v[1] = make_pair(bf16_lo(r.y), bf16_hi(r.y));
+        v[2] = make_pair(bf16_lo(r.z), bf16_hi(r.z));
+        v[3] = make_pair(bf16_lo(r.w), bf16_hi(r.w));
     }
-    static __device__ __forceinline__ uint4 put(const float (&v)[8]) {
-        return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    static __device__ __forceinline__ uint32_t word(pair v) {
+        float a, b;
+        split_pair(v, a, b);
+        return pack_bf16(a, b);
     }
+    static __device__ __forceinline__ uint4 put(const pair (&v)[4]) { return make_uint4(word(v[0]), word(v[1]), word(v[2]), word(v[3])); }
 };
 
-template <int Act> __device__ __forceinline__ float act_value(float z) {
-    if constexpr (Act == SLIDE_ATTN_ACT_SILU) return z / (1.0f + __expf(-z));
-    else if constexpr (Act == SLIDE_ATTN_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    else return z;
+__device__ __forceinline__ pair exp2_2(pair x) {
+    float a, b;
+    split_pair(x, a, b);
+    return make_pair(fast_exp2(a), fast_exp2(b));
 }
-template <int Act> __device__ __forceinline__ float act_slope(float z) {
+__device__ __forceinline__ pair rcp_2(pair x) {
+    float a, b;
+    split_pair(x, a, b);
+    return make_pair(rcp_approx(a), rcp_approx(b));
+}
+
+// The normal distribution's integral up to z and, from the same exponential, its density.  erfc by M. Abramowitz, I. Stegun, Handbook of
+// Mathematical Functions, 7.1.26 (error below 1.5e-7): erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + p x), x = |z| / sqrt 2.  An
+// infinity gives 0 or 1 and a NaN a NaN.
+__device__ __forceinline__ void normal_2(pair z, pair& cdf, pair& density) {
+    float z0, z1;
+    split_pair(z, z0, z1);
+    const pair a = make_pair(fabsf(z0), fabsf(z1));
+    const pair t = rcp_2(fma2(a, both(0.3275911f * 0.70710678f), both(1.0f)));
+    pair p = fma2(t, both(0.5f * 1.061405429f), both(-0.5f * 1.453152027f));      // half of the polynomial
+    p = fma2(p, t, both(0.5f * 1.421413741f));
+    p = fma2(p, t, both(-0.5f * 0.284496736f));
+    p = fma2(p, t, both(0.5f * 0.254829592f));
+    const pair e = exp2_2(mul2(mul2(z, both(-0.72134752f)), z));                 // exp(-z^2 / 2)
+    const pair d = fma2(mul2(p, t), mul2(e, both(-1.0f)), both(0.5f));           // 1/2 - integral up to -|z|
+    float d0, d1;
+    split_pair(d, d0, d1);
+    cdf = add2(make_pair(copysignf(d0, z0), copysignf(d1, z1)), both(0.5f));
+    density = mul2(e, both(0.39894228f));
+}
+
+template <int Act> __device__ __forceinline__ pair act_value(pair z) {
     if constexpr (Act == SLIDE_ATTN_ACT_SILU) {
-        const float g = 1.0f / (1.0f + __expf(-z));
-        return g * (1.0f + z * (1.0f - g));
+        return mul2(z, rcp_2(add2(exp2_2(mul2(z, both(-1.44269504f))), both(1.0f))));
     } else if constexpr (Act == SLIDE_ATTN_ACT_GELU) {
-        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
+        pair cdf, density;
+        normal_2(z, cdf, density);
+        return mul2(z, cdf);
     } else {
-        return 1.0f;
+        return z;
+    }
+}
+template <int Act> __device__ __forceinline__ pair act_slope(pair z) {
+    if constexpr (Act == SLIDE_ATTN_ACT_SILU) {
+        const pair g = rcp_2(add2(exp2_2(mul2(z, both(-1.44269504f))), both(1.0f)));
+        return mul2(g, fma2(z, fma2(g, both(-1.0f), both(1.0f)), both(1.0f)));    // g (1 + z (1 - g))
+    } else if constexpr (Act == SLIDE_ATTN_ACT_GELU) {
+        pair cdf, density;
+        normal_2(z, cdf, density);
+        return fma2(z, density, cdf);
+    } else {
+        return both(1.0f);
     }
 }
 
@@ -88,257 +138,314 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// out[i] = sum over rows r and unit's columns c of red[r][i * unit + c], i < n, by `lanes` lanes of a warp each (a power of two).
-__device__ __forceinline__ void reduce_units(const float* red, int rows, int width, int unit, int n, int lanes, float* out) {
-    const int per_round = blockDim.x / lanes, lane = threadIdx.x % lanes;
-    const int count = rows * unit;
-    for (int first = 0; first < n; first += per_round) {
-        const int i = first + threadIdx.x / lanes;
+// Where a thread works: a 16-byte column of the slab and every `rows`-th of the CTA's pixels.
+struct Place {
+    int column, first;
+    int mine, held;                    // how many pixels, and how many of them in shared memory
+    bool active;
+};
+__device__ __forceinline__ Place find_place(const NormPlan& pl, int pixels) {
+    Place p;
+    p.active = (int)threadIdx.x < pl.rows * pl.columns;
+    p.first = (int)threadIdx.x / pl.columns;
+    p.column = (int)threadIdx.x - p.first * pl.columns;
+    p.mine = p.active && p.first < pixels ? (pixels - p.first + pl.rows - 1) / pl.rows : 0;
+    p.held = min(p.mine, pl.cached);
+    return p;
+}
+// The groups (within the slab) of a column's channels.
+template <int V> __device__ __forceinline__ void find_groups(const NormPlan& pl, int column, int (&group)[V]) {
+    int g = column * V / pl.per_group, left = (g + 1) * pl.per_group - column * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        group[e] = g;
+        if (--left == 0) { ++g; left = pl.per_group; }
+    }
+}
+// V channels of gamma or beta, or a constant.
+template <int V> __device__ __forceinline__ void get_weights(const float* w, int c, float otherwise, pair (&v)[V / 2]) {
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+        const float4 x = w ? *reinterpret_cast<const float4*>(w + c + e) : make_float4(otherwise, otherwise, otherwise, otherwise);
+        v[e / 2] = make_pair(x.x, x.y);
+        v[e / 2 + 1] = make_pair(x.z, x.w);
+    }
+}
+
+// out[i] = sum over rows r < `rows` and columns c < `unit` of in[r][i unit + c], i < n, by `lanes` neighbouring threads each (a power of two up
+// to 32), who share the rows or, of a single row, the columns.
+__device__ __forceinline__ int lanes_for(int n) {
+    int lanes = 32;
+    while (lanes > 1 && n * lanes > (int)blockDim.x) lanes /= 2;
+    return lanes;
+}
+__device__ __forceinline__ void sum_cells(const float* in, int rows, int width, int unit, int n, int lanes, float* out) {
+    const int lane = threadIdx.x & (lanes - 1), at_once = (int)blockDim.x / lanes;
+    for (int first = 0; first < n; first += at_once) {
+        const int i = first + (int)threadIdx.x / lanes;
         float s = 0.0f;
         if (i < n) {
-            int r = lane / unit, c = lane - r * unit;
-            for (int e = lane; e < count; e += lanes) {
-                s += red[r * width + i * unit + c];
-                c += lanes;
-                while (c >= unit) { c -= unit; ++r; }
+            const float* cell = in + i * unit;
+            if (rows > 1) {
+                if (unit == 1) {
+#pragma unroll 4
+                    for (int r = lane; r < rows; r += lanes) s += cell[r * width];
+                } else {
+#pragma unroll 2
+                    for (int r = lane; r < rows; r += lanes)
+                        for (int c = 0; c < unit; ++c) s += cell[r * width + c];
+                }
+            } else {
+                for (int c = lane; c < unit; c += lanes) s += cell[c];
             }
         }
         for (int o = lanes / 2; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (i < n && lane == 0) out[i] = s;
     }
+    __syncthreads();
 }
-__device__ __forceinline__ int lanes_for(int n) { return n * 32 <= (int)blockDim.x ? 32 : 8; }
-
-// What a thread works on.
-struct Place {
-    int column, first, step;           // column of 16 bytes; its first pixel within the CTA's, and the step to the next
-    int mine, held;                    // how many pixels, and how many of them in shared memory
-    bool active;
-};
-
-template <int V>
-__device__ __forceinline__ Place find_place(const NormPlan& pl, int pixels) {
-    Place p;
-    p.active = (int)threadIdx.x < pl.rows * pl.columns;
-    p.column = threadIdx.x % pl.columns;
-    p.first = threadIdx.x / pl.columns;
-    p.step = pl.rows;
-    p.mine = p.active && p.first < pixels ? (pixels - p.first + pl.rows - 1) / pl.rows : 0;
-    p.held = p.mine < pl.cached ? p.mine : pl.cached;
-    return p;
+template <int V> __device__ __forceinline__ void leave(float* red, const pair (&v)[V / 2]) {
+#pragma unroll
+    for (int e = 0; e < V / 4; ++e) {
+        float4 x;
+        split_pair(v[2 * e], x.x, x.y);
+        split_pair(v[2 * e + 1], x.z, x.w);
+        reinterpret_cast<float4*>(red)[threadIdx.x * (V / 4) + e] = x;               // [row][channel of the slab]
+    }
 }
+
+constexpr int kCopyGroups = 4;         // groups that a thread's copies come in, so that the sums begin with the first
+template <int G> __device__ __forceinline__ void wait_for_group() { copies_wait<kCopyGroups - 1 - G>(); }
 
 template <typename T, int Act>
 __global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a, const NormPlan pl)
 {
-    constexpr int V = Vec<T>::n;
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
     extern __shared__ __align__(16) unsigned char smem[];
     cg::cluster_group cluster = cg::this_cluster();
     const int K = pl.cluster, rank = (int)cluster.block_rank();
-    const long long unit = blockIdx.x / K;
-    const long long b = unit / pl.slabs;
-    const int slab = (int)(unit % pl.slabs);
-    const long long p0 = (long long)pl.P * rank / K, p1 = (long long)pl.P * (rank + 1) / K;
-    const int pixels = (int)(p1 - p0), slab_groups = pl.width / pl.per_group;
-    const Place at = find_place<V>(pl, pixels);
+    const unsigned unit = blockIdx.x / (unsigned)K;
+    const size_t b = unit / (unsigned)pl.slabs;
+    const int slab = (int)(unit - (unsigned)b * (unsigned)pl.slabs);
+    auto cut = [&](int r) { return (int)((long long)pl.P * r >> pl.log_cluster); };      // the first pixel of a CTA
+    const int p0 = cut(rank), pixels = cut(rank + 1) - p0;
+    const int slab_groups = pl.width / pl.per_group;
+    const Place at = find_place(pl, pixels);
     const int active = pl.rows * pl.columns;
 
-    uint4* cache = reinterpret_cast<uint4*>(smem);
+    uint4* cache = reinterpret_cast<uint4*>(smem) + threadIdx.x;                     // [round][active thread]
     float* red = reinterpret_cast<float*>(smem + (size_t)pl.cached * active * 16);
-    float* local = red + pl.threads * V;              // mean and sum of squares of this CTA's pixels, by group
+    float* local = red + pl.threads * V;              // sums of this CTA's pixels and of the squares about their mean, by group
     float* total = local + 2 * slab_groups;           // mean and rstd of the image
-    const size_t row_bytes = (size_t)pl.C * sizeof(T);
-    const size_t start = ((size_t)b * pl.P + p0 + at.first) * row_bytes + (size_t)slab * pl.width * sizeof(T) + (size_t)at.column * 16;
+    const size_t row_bytes = (size_t)pl.C * sizeof(T), step = (size_t)pl.rows * row_bytes;
+    const size_t start = (b * (size_t)pl.P + (size_t)(p0 + at.first)) * row_bytes + (size_t)slab * pl.width * sizeof(T) + (size_t)at.column * 16;
     const unsigned char* src = static_cast<const unsigned char*>(a.x) + start;
-    const size_t step = (size_t)at.step * row_bytes;
 
     grid_dependency_wait();
-    // four groups of copies, so that the sums begin with the first
-    constexpr int kGroups = 4;
-    int ends[kGroups];
+    auto round_of = [&](int group) { return at.held * group / kCopyGroups; };
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        ends[g] = at.held * (g + 1) / kGroups;
-        for (int i = g ? ends[g - 1] : 0; i < ends[g]; ++i) copy16(smem_u32(cache + i * active + threadIdx.x), src + i * step);
+    for (int g = 0; g < kCopyGroups; ++g) {
+        for (int i = round_of(g); i < round_of(g + 1); ++i) copy16(smem_u32(cache + i * active), src + i * step);
         copies_end_group();
     }
-    float gamma[V], beta[V];
     int group[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = at.column * V + e;
-        group[e] = c / pl.per_group;
-        gamma[e] = a.gamma ? a.gamma[slab * pl.width + c] : 1.0f;
-        beta[e] = a.beta ? a.beta[slab * pl.width + c] : 0.0f;
-    }
+    find_groups<V>(pl, at.column, group);
 
     // the CTA's own mean ...
-    float sum[V] = {};
+    pair sum[Q] = {};
     auto add = [&](const uint4& r) {
-        float v[V];
+        pair v[Q];
         Vec<T>::get(r, v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] += v[e];
+        for (int e = 0; e < Q; ++e) sum[e] = add2(sum[e], v[e]);
     };
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        if (g == 0) copies_wait<3>(); else if (g == 1) copies_wait<2>(); else if (g == 2) copies_wait<1>(); else copies_wait<0>();
-        for (int i = g ? ends[g - 1] : 0; i < ends[g]; ++i) add(cache[i * active + threadIdx.x]);
-    }
+    auto add_group = [&](int g) {
+        for (int i = round_of(g); i < round_of(g + 1); ++i) add(cache[i * active]);
+    };
+    wait_for_group<0>(); add_group(0);
+    wait_for_group<1>(); add_group(1);
+    wait_for_group<2>(); add_group(2);
+    wait_for_group<3>(); add_group(3);
 #pragma unroll 4
     for (int i = at.held; i < at.mine; ++i) add(*reinterpret_cast<const uint4*>(src + i * step));
     const int lanes = lanes_for(slab_groups);
-    auto fold = [&](const float (&v)[V], float* out) {
-        if (at.active)
-#pragma unroll
-            for (int e = 0; e < V; ++e) red[threadIdx.x * V + e] = v[e];       // [row][channel of the slab]
+    auto fold = [&](const pair (&v)[Q], float* out) {
+        if (at.active) leave<V>(red, v);
         __syncthreads();
-        reduce_units(red, pl.rows, pl.width, pl.per_group, slab_groups, lanes, out);
-        __syncthreads();
+        sum_cells(red, pl.rows, pl.width, pl.per_group, slab_groups, lanes, out);
     };
     fold(sum, local);
-    const float inv_own = 1.0f / ((float)pixels * (float)pl.per_group);        // no CTA is without pixels
+    const float inv_own = 1.0f / ((float)pixels * (float)pl.per_group);               // no CTA is without pixels
     // ... and the squares about it, which lose nothing however far the mean is from zero
-    float mean[V], square[V] = {};
+    pair mean[Q], square[Q] = {};                      // less the mean
 #pragma unroll
-    for (int e = 0; e < V; ++e) mean[e] = at.active ? local[group[e]] * inv_own : 0.0f;
+    for (int e = 0; e < Q; ++e) mean[e] = make_pair(-local[group[2 * e]] * inv_own, -local[group[2 * e + 1]] * inv_own);
     auto add_square = [&](const uint4& r) {
-        float v[V];
+        pair v[Q];
         Vec<T>::get(r, v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) { const float d = v[e] - mean[e]; square[e] = fmaf(d, d, square[e]); }
+        for (int e = 0; e < Q; ++e) {
+            const pair d = add2(v[e], mean[e]);
+            square[e] = fma2(d, d, square[e]);
+        }
     };
-    for (int i = 0; i < at.held; ++i) add_square(cache[i * active + threadIdx.x]);
+#pragma unroll 2
+    for (int i = 0; i < at.held; ++i) add_square(cache[i * active]);
 #pragma unroll 4
     for (int i = at.held; i < at.mine; ++i) add_square(*reinterpret_cast<const uint4*>(src + i * step));
     fold(square, local + slab_groups);
 
     // the cluster's: deviations from the first CTA's mean, so that nothing large cancels
     cluster.sync();
-    for (int g = threadIdx.x; g < slab_groups; g += blockDim.x) {
-        const float n = (float)pl.P, m0 = cluster.map_shared_rank(local, 0)[g] / ((float)((long long)pl.P / K) * (float)pl.per_group);
-        float shift = 0.0f, m2 = 0.0f;
-        for (int r = 0; r < K; ++r) {
-            const float own = (float)((long long)pl.P * (r + 1) / K - (long long)pl.P * r / K);
-            shift += own * (cluster.map_shared_rank(local, r)[g] / (own * (float)pl.per_group) - m0);
-        }
-        const float m = m0 + shift / n;
-        for (int r = 0; r < K; ++r) {
-            const float own = (float)((long long)pl.P * (r + 1) / K - (long long)pl.P * r / K);
-            const float* there = cluster.map_shared_rank(local, r);
-            const float d = there[g] / (own * (float)pl.per_group) - m;
-            m2 += there[slab_groups + g] + own * (float)pl.per_group * d * d;
-        }
-        const float rstd = 1.0f / sqrtf(m2 / (n * (float)pl.per_group) + a.eps);
-        total[g] = m;
-        total[slab_groups + g] = rstd;
-        if (rank == 0) {
-            const size_t o = (size_t)b * pl.groups + slab * slab_groups + g;
-            a.mean[o] = m;
-            a.rstd[o] = rstd;
+    // a lane for each CTA of the cluster (a power of two)
+    for (int first = 0; first < slab_groups; first += (int)blockDim.x >> pl.log_cluster) {
+        const int g = first + ((int)threadIdx.x >> pl.log_cluster), r = (int)threadIdx.x & (K - 1);
+        const bool there = g < slab_groups;
+        const float* theirs = cluster.map_shared_rank(local, r);
+        const float per = (float)pl.per_group, n = (float)pl.P * per;
+        const float own = (float)(cut(r + 1) - cut(r)) * per;
+        const float mine = there ? theirs[g] / own : 0.0f;
+        const float m0 = __shfl_sync(0xffffffffu, mine, (int)threadIdx.x & 31 & ~(K - 1));
+        float shift = own * (mine - m0);
+        for (int o = K / 2; o > 0; o /= 2) shift += __shfl_xor_sync(0xffffffffu, shift, o);
+        const float m = m0 + shift / n, d = mine - m;
+        float m2 = there ? fmaf(own * d, d, theirs[slab_groups + g]) : 0.0f;
+        for (int o = K / 2; o > 0; o /= 2) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+        if (there && r == 0) {
+            const float rstd = 1.0f / sqrtf(m2 / n + a.eps);
+            total[g] = m;
+            total[slab_groups + g] = rstd;
+            if (rank == 0) {
+                const size_t o = b * pl.groups + slab * slab_groups + g;
+                a.mean[o] = m;
+                a.rstd[o] = rstd;
+            }
         }
     }
     cluster.sync();          // `total` is complete, and nobody reads another CTA's shared memory any more
     if (!at.active) return;
 
-    float scale[V];
+    pair scale[Q], beta[Q];
+    get_weights<V>(a.gamma, slab * pl.width + at.column * V, 1.0f, scale);
+    get_weights<V>(a.beta, slab * pl.width + at.column * V, 0.0f, beta);
 #pragma unroll
-    for (int e = 0; e < V; ++e) { mean[e] = total[group[e]]; scale[e] = total[slab_groups + group[e]] * gamma[e]; }
+    for (int e = 0; e < Q; ++e) {
+        mean[e] = make_pair(-total[group[2 * e]], -total[group[2 * e + 1]]);
+        scale[e] = mul2(scale[e], make_pair(total[slab_groups + group[2 * e]], total[slab_groups + group[2 * e + 1]]));
+    }
     unsigned char* dst = static_cast<unsigned char*>(a.y) + start;
     auto apply = [&](const uint4& r) {
-        float v[V];
+        pair v[Q];
         Vec<T>::get(r, v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = act_value<Act>(fmaf(v[e] - mean[e], scale[e], beta[e]));
+        for (int e = 0; e < Q; ++e) v[e] = act_value<Act>(fma2(add2(v[e], mean[e]), scale[e], beta[e]));
         return Vec<T>::put(v);
     };
-    for (int i = 0; i < at.held; ++i) *reinterpret_cast<uint4*>(dst + i * step) = apply(cache[i * active + threadIdx.x]);
+    for (int i = 0; i < at.held; ++i) *reinterpret_cast<uint4*>(dst + i * step) = apply(cache[i * active]);
 #pragma unroll 4
     for (int i = at.held; i < at.mine; ++i)
         *reinterpret_cast<uint4*>(dst + i * step) = apply(*reinterpret_cast<const uint4*>(src + i * step));
 }
 
+// Shared memory holds x and, in the place of dy, dz in fp32 (bf16: twice the room): act' is not computed twice.
 template <typename T, int Act>
 __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a, const NormPlan pl)
 {
-    constexpr int V = Vec<T>::n;
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
     extern __shared__ __align__(16) unsigned char smem[];
     cg::cluster_group cluster = cg::this_cluster();
     const int K = pl.cluster, rank = (int)cluster.block_rank();
-    const long long unit = blockIdx.x / K;
-    const long long b = unit / pl.slabs;
-    const int slab = (int)(unit % pl.slabs);
-    const long long p0 = (long long)pl.P * rank / K, p1 = (long long)pl.P * (rank + 1) / K;
-    const int pixels = (int)(p1 - p0), slab_groups = pl.width / pl.per_group;
-    const Place at = find_place<V>(pl, pixels);
+    const unsigned unit = blockIdx.x / (unsigned)K;
+    const size_t b = unit / (unsigned)pl.slabs;
+    const int slab = (int)(unit - (unsigned)b * (unsigned)pl.slabs);
+    auto cut = [&](int r) { return (int)((long long)pl.P * r >> pl.log_cluster); };      // the first pixel of a CTA
+    const int p0 = cut(rank), pixels = cut(rank + 1) - p0;
+    const int slab_groups = pl.width / pl.per_group;
+    const Place at = find_place(pl, pixels);
     const int active = pl.rows * pl.columns;
 
-    uint4* cache_x = reinterpret_cast<uint4*>(smem);
-    uint4* cache_g = cache_x + (size_t)pl.cached * active;
-    float* red = reinterpret_cast<float*>(smem + (size_t)pl.cached * active * 32);
+    uint4* cache_x = reinterpret_cast<uint4*>(smem) + threadIdx.x;
+    uint4* cache_g = cache_x + (size_t)pl.cached * active;                            // dy; then dz, of bf16 the first half
+    uint4* cache_h = cache_g + (size_t)pl.cached * active;                            // bf16: the second half of dz
+    float* red = reinterpret_cast<float*>(smem + (size_t)pl.cached * active * (16 + 4 * V));
     float* channel = red + pl.threads * V;            // sums of dz, then of dz u, by channel: this CTA's
     float* weighted = channel + 2 * pl.width;         // the same times gamma
     float* local = weighted + 2 * pl.width;           // sums of du, then of du u, by group: this CTA's
     float* total = local + 2 * slab_groups;           // their means over the image
-    const size_t row_bytes = (size_t)pl.C * sizeof(T);
-    const size_t start = ((size_t)b * pl.P + p0 + at.first) * row_bytes + (size_t)slab * pl.width * sizeof(T) + (size_t)at.column * 16;
+    const size_t row_bytes = (size_t)pl.C * sizeof(T), step = (size_t)pl.rows * row_bytes;
+    const size_t start = (b * (size_t)pl.P + (size_t)(p0 + at.first)) * row_bytes + (size_t)slab * pl.width * sizeof(T) + (size_t)at.column * 16;
     const unsigned char* src_x = static_cast<const unsigned char*>(a.x) + start;
     const unsigned char* src_g = static_cast<const unsigned char*>(a.dy) + start;
-    const size_t step = (size_t)at.step * row_bytes;
 
     grid_dependency_wait();
-    constexpr int kGroups = 4;
-    int ends[kGroups];
+    auto round_of = [&](int group) { return at.held * group / kCopyGroups; };
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        ends[g] = at.held * (g + 1) / kGroups;
-        for (int i = g ? ends[g - 1] : 0; i < ends[g]; ++i) {
-            copy16(smem_u32(cache_x + i * active + threadIdx.x), src_x + i * step);
-            copy16(smem_u32(cache_g + i * active + threadIdx.x), src_g + i * step);
+    for (int g = 0; g < kCopyGroups; ++g) {
+        for (int i = round_of(g); i < round_of(g + 1); ++i) {
+            copy16(smem_u32(cache_x + i * active), src_x + i * step);
+            copy16(smem_u32(cache_g + i * active), src_g + i * step);
         }
         copies_end_group();
     }
-    float gamma[V], beta[V], mean[V], rstd[V];
     int group[V];
+    find_groups<V>(pl, at.column, group);
+    pair gamma[Q], beta[Q], mean[Q], rstd[Q];          // less the mean
+    get_weights<V>(a.gamma, slab * pl.width + at.column * V, 1.0f, gamma);
+    get_weights<V>(a.beta, slab * pl.width + at.column * V, 0.0f, beta);
+    {
+        const float* m = a.mean + b * pl.groups + slab * slab_groups;
+        const float* r = a.rstd + b * pl.groups + slab * slab_groups;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = at.column * V + e;
-        group[e] = c / pl.per_group;
-        gamma[e] = a.gamma ? a.gamma[slab * pl.width + c] : 1.0f;
-        beta[e] = a.beta ? a.beta[slab * pl.width + c] : 0.0f;
-        const size_t o = (size_t)b * pl.groups + slab * slab_groups + group[e];
-        mean[e] = a.mean[o];
-        rstd[e] = a.rstd[o];
+        for (int e = 0; e < Q; ++e) {
+            mean[e] = make_pair(-m[group[2 * e]], -m[group[2 * e + 1]]);
+            rstd[e] = make_pair(r[group[2 * e]], r[group[2 * e + 1]]);
+        }
     }
-    float s1[V] = {}, s2[V] = {};
-    auto add = [&](const uint4& rx, const uint4& rg) {
-        float x[V], g[V];
-        Vec<T>::get(rx, x);
-        Vec<T>::get(rg, g);
+    pair s1[Q] = {}, s2[Q] = {};
+    // dz of a column of 16 bytes
+    auto slopes = [&](const uint4& rx, const uint4& rg, pair (&u)[Q], pair (&dz)[Q]) {
+        Vec<T>::get(rx, u);
+        Vec<T>::get(rg, dz);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float u = (x[e] - mean[e]) * rstd[e];
-            const float dz = g[e] * act_slope<Act>(fmaf(u, gamma[e], beta[e]));
-            s1[e] += dz;
-            s2[e] = fmaf(dz, u, s2[e]);
+        for (int e = 0; e < Q; ++e) {
+            u[e] = mul2(add2(u[e], mean[e]), rstd[e]);
+            if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<Act>(fma2(u[e], gamma[e], beta[e])));
         }
     };
+    auto add = [&](const pair (&u)[Q], const pair (&dz)[Q]) {
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        if (g == 0) copies_wait<3>(); else if (g == 1) copies_wait<2>(); else if (g == 2) copies_wait<1>(); else copies_wait<0>();
-        for (int i = g ? ends[g - 1] : 0; i < ends[g]; ++i) add(cache_x[i * active + threadIdx.x], cache_g[i * active + threadIdx.x]);
-    }
+        for (int e = 0; e < Q; ++e) {
+            s1[e] = add2(s1[e], dz[e]);
+            s2[e] = fma2(dz[e], u[e], s2[e]);
+        }
+    };
+    auto add_group = [&](int g) {
+        for (int i = round_of(g); i < round_of(g + 1); ++i) {
+            pair u[Q], dz[Q];
+            slopes(cache_x[i * active], cache_g[i * active], u, dz);
+            add(u, dz);
+            const pair lower[2] = {dz[0], dz[1]};
+            cache_g[i * active] = Vec<float>::put(lower);
+            if constexpr (Q == 4) {
+                const pair upper[2] = {dz[2], dz[3]};
+                cache_h[i * active] = Vec<float>::put(upper);
+            }
+        }
+    };
+    wait_for_group<0>(); add_group(0);
+    wait_for_group<1>(); add_group(1);
+    wait_for_group<2>(); add_group(2);
+    wait_for_group<3>(); add_group(3);
 #pragma unroll 2
-    for (int i = at.held; i < at.mine; ++i)
-        add(*reinterpret_cast<const uint4*>(src_x + i * step), *reinterpret_cast<const uint4*>(src_g + i * step));
-    const int lanes_c = lanes_for(pl.width), lanes_g = lanes_for(slab_groups);
-    auto fold = [&](const float (&v)[V], float* out) {
-        if (at.active)
-#pragma unroll
-            for (int e = 0; e < V; ++e) red[threadIdx.x * V + e] = v[e];
+    for (int i = at.held; i < at.mine; ++i) {
+        pair u[Q], dz[Q];
+        slopes(*reinterpret_cast<const uint4*>(src_x + i * step), *reinterpret_cast<const uint4*>(src_g + i * step), u, dz);
+        add(u, dz);
+    }
+    auto fold = [&](const pair (&v)[Q], float* out) {
+        if (at.active) leave<V>(red, v);
         __syncthreads();
-        reduce_units(red, pl.rows, pl.width, 1, pl.width, lanes_c, out);
-        __syncthreads();
+        sum_cells(red, pl.rows, pl.width, 1, pl.width, lanes_for(pl.width), out);
     };
     fold(s1, channel);
     fold(s2, channel + pl.width);
@@ -347,49 +454,60 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a, co
         weighted[c] = channel[c] * (a.gamma ? a.gamma[slab * pl.width + ch] : 1.0f);
     }
     __syncthreads();
-    reduce_units(weighted, 1, pl.width, pl.per_group, slab_groups, lanes_g, local);
-    reduce_units(weighted + pl.width, 1, pl.width, pl.per_group, slab_groups, lanes_g, local + slab_groups);
+    sum_cells(weighted, 1, 0, pl.per_group, 2 * slab_groups, lanes_for(2 * slab_groups), local);
     cluster.sync();
+    // a lane for each CTA of the cluster (a power of two)
     const float inv = 1.0f / ((float)pl.P * (float)pl.per_group);
-    for (int g = threadIdx.x; g < 2 * slab_groups; g += blockDim.x) {
-        float s = 0.0f;
-        for (int r = 0; r < K; ++r) s += cluster.map_shared_rank(local, r)[g];
-        total[g] = s * inv;
+    for (int first = 0; first < 2 * slab_groups; first += (int)blockDim.x >> pl.log_cluster) {
+        const int g = first + ((int)threadIdx.x >> pl.log_cluster), r = (int)threadIdx.x & (K - 1);
+        float s = g < 2 * slab_groups ? cluster.map_shared_rank(local, r)[g] : 0.0f;
+        for (int o = K / 2; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (g < 2 * slab_groups && r == 0) total[g] = s * inv;
     }
     if (a.sums) {
-        const long long images = (long long)gridDim.x / K / pl.slabs;
+        const size_t images = gridDim.x / (unsigned)K / (unsigned)pl.slabs;
         for (int c = rank * (int)blockDim.x + (int)threadIdx.x; c < 2 * pl.width; c += K * (int)blockDim.x) {
             float s = 0.0f;
             for (int r = 0; r < K; ++r) s += cluster.map_shared_rank(channel, r)[c];
             const int which = c / pl.width, ch = c - which * pl.width;
-            a.sums[((size_t)which * images + b) * pl.C + slab * pl.width + ch] = s;
+            a.sums[(which * images + b) * pl.C + slab * pl.width + ch] = s;
         }
     }
     cluster.sync();
     if (!at.active) return;
 
-    float m1[V], m2[V];
+    // dx = rstd (gamma dz - m1 - u m2)
+    pair m1[Q], m2[Q];                                 // less the means
 #pragma unroll
-    for (int e = 0; e < V; ++e) { m1[e] = total[group[e]]; m2[e] = total[slab_groups + group[e]]; }
+    for (int e = 0; e < Q; ++e) {
+        m1[e] = make_pair(-total[group[2 * e]], -total[group[2 * e + 1]]);
+        m2[e] = make_pair(-total[slab_groups + group[2 * e]], -total[slab_groups + group[2 * e + 1]]);
+    }
     unsigned char* dst = static_cast<unsigned char*>(a.y) + start;
-    auto apply = [&](const uint4& rx, const uint4& rg) {
-        float x[V], g[V];
-        Vec<T>::get(rx, x);
-        Vec<T>::get(rg, g);
+    auto finish = [&](const pair (&u)[Q], pair (&dz)[Q]) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float u = (x[e] - mean[e]) * rstd[e];
-            const float du = g[e] * act_slope<Act>(fmaf(u, gamma[e], beta[e])) * gamma[e];
-            g[e] = rstd[e] * (du - m1[e] - u * m2[e]);
-        }
-        return Vec<T>::put(g);
+        for (int e = 0; e < Q; ++e) dz[e] = mul2(rstd[e], fma2(u[e], m2[e], fma2(dz[e], gamma[e], m1[e])));
+        return Vec<T>::put(dz);
     };
-    for (int i = 0; i < at.held; ++i)
-        *reinterpret_cast<uint4*>(dst + i * step) = apply(cache_x[i * active + threadIdx.x], cache_g[i * active + threadIdx.x]);
+    for (int i = 0; i < at.held; ++i) {
+        pair u[Q], dz[Q], half[2];
+        Vec<T>::get(cache_x[i * active], u);
+#pragma unroll
+        for (int e = 0; e < Q; ++e) u[e] = mul2(add2(u[e], mean[e]), rstd[e]);
+        Vec<float>::get(cache_g[i * active], half);
+        dz[0] = half[0]; dz[1] = half[1];
+        if constexpr (Q == 4) {
+            Vec<float>::get(cache_h[i * active], half);
+            dz[2] = half[0]; dz[3] = half[1];
+        }
+        *reinterpret_cast<uint4*>(dst + i * step) = finish(u, dz);
+    }
 #pragma unroll 2
-    for (int i = at.held; i < at.mine; ++i)
-        *reinterpret_cast<uint4*>(dst + i * step) =
-            apply(*reinterpret_cast<const uint4*>(src_x + i * step), *reinterpret_cast<const uint4*>(src_g + i * step));
+    for (int i = at.held; i < at.mine; ++i) {
+        pair u[Q], dz[Q];
+        slopes(*reinterpret_cast<const uint4*>(src_x + i * step), *reinterpret_cast<const uint4*>(src_g + i * step), u, dz);
+        *reinterpret_cast<uint4*>(dst + i * step) = finish(u, dz);
+    }
 }
 
 // dbeta and dgamma: the images' sums, added up in the images' order.  32 channels of one of the two a block, eight rows at a time.
@@ -413,42 +531,43 @@ __global__ void norm_weight_kernel(const float* sums, long long images, int C, f
 
 long long gcd(long long a, long long b) { return b ? gcd(b, a % b) : a; }
 
-// False where no slab fits a block.
+// maps: 1 forward, 2 backward.  False where no slab fits a block, or no grid the call.
 bool make_plan(long long B, long long P, int C, int groups, int size, int maps, int num_sms, NormPlan* out) {
     NormPlan p = {};
     const int V = 16 / size;
     p.P = (int)P; p.C = C; p.groups = groups; p.per_group = C / groups;
     const int narrow = (int)((long long)p.per_group / gcd(p.per_group, V) * V);   // the narrowest slab: whole groups and 16-byte columns
     const int most_slabs = C / narrow;
-    constexpr long long kShare = 72 * 1024;            // three CTAs share an SM
-    auto bytes = [&](int slabs) { return P * (C / slabs) * size * maps; };
-    // Wider slabs read longer runs of memory; narrower ones give more CTAs and may be held whole.
-    int slabs = 1;
+    if (B * most_slabs > 0x7fffffffLL / kMaxCluster) return false;
+    const int held = maps == 1 ? size : size + 4;      // bytes that stay of an element
+    // A slab as wide as may be reads the longest runs of memory; narrower ones take smaller clusters, give more CTAs and may be held whole.
+    // A CTA's share of 72 KB lets three share an SM.
+    constexpr long long kShare = 72 * 1024;
+    int best_slabs = 0, best_cluster = 0;
     for (int s = 1; s <= most_slabs; ++s) {
-        if (most_slabs % s) continue;
-        const bool fits = C / s / V <= 512;
-        if (s > 1 && (slabs > 0 && C / slabs / V <= 512) && (C / s) * size < 64) break;
-        slabs = s;
-        if (fits && bytes(s) <= kMaxCluster * kShare && (B * s * kMaxCluster >= 2 * num_sms || bytes(s) <= 16 * 1024)) break;
+        if (most_slabs % s || C / s / V > 512) continue;
+        if (best_slabs && C / s * size < 64) break;
+        const long long bytes = P * (C / s) * held;
+        int K = 1;
+        while (K < kMaxCluster && 2 * K <= P && (bytes > K * kShare || (B * s * K < 2 * num_sms && bytes > K * 8 * 1024))) K *= 2;
+        best_slabs = s;
+        best_cluster = K;
+        if (bytes <= K * kShare && K <= 8 && (B * s * K >= 2 * num_sms || bytes <= K * 16 * 1024)) break;
     }
-    p.slabs = slabs; p.width = C / slabs;
+    if (!best_slabs) return false;
+    p.slabs = best_slabs; p.width = C / best_slabs; p.cluster = best_cluster;
+    while ((1 << p.log_cluster) < p.cluster) ++p.log_cluster;
     p.columns = p.width / V;
-    if (p.columns > 512) return false;
     p.threads = p.columns > 256 ? 512 : 256;
     p.rows = p.threads / p.columns;
-    int K = 1;
-    while (K < kMaxCluster && 2 * K <= P && (bytes(slabs) > K * kShare || (B * slabs * K < 2 * num_sms && bytes(slabs) > K * 8 * 1024))) K *= 2;
-    p.cluster = K;
-    const int active = p.rows * p.columns;
-    const long long most = (P + K - 1) / K;
-    const long long rounds = (most + p.rows - 1) / p.rows;
-    const int slab_groups = p.width / p.per_group;
-    const size_t rest = (size_t)p.threads * 16 / size * 4 + (size_t)(4 * slab_groups + (maps > 1 ? 4 * p.width : 0)) * 4;
-    const long long fit = (long long)(kMaxSmem - 1024 - rest) / ((long long)active * 16 * maps);
+    const int active = p.rows * p.columns, slab_groups = p.width / p.per_group;
+    const long long rounds = ((P + p.cluster - 1) / p.cluster + p.rows - 1) / p.rows;
+    const size_t rest = (size_t)p.threads * V * 4 + (size_t)(4 * slab_groups + (maps > 1 ? 4 * p.width : 0)) * 4;
+    const long long round_bytes = (long long)active * V * held;
+    const long long fit = (long long)(kMaxSmem - 1024 - rest) / round_bytes;
     p.cached = (int)(rounds < fit ? rounds : fit);
-    p.smem = (size_t)p.cached * active * 16 * maps + rest;
-    p.blocks = B * slabs * K;
-    if (B * most_slabs > 0x7fffffffLL / kMaxCluster) return false;
+    p.smem = (size_t)p.cached * round_bytes + rest;
+    p.blocks = B * p.slabs * p.cluster;
     *out = p;
     return true;
 }

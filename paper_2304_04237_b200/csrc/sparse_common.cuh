@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "common.cuh"
+#include "packed.cuh"
 #include "ptx.cuh"
 #include "split.cuh"
 
@@ -88,29 +89,6 @@ struct BackwardMaps {
 
 template <int D> __device__ __forceinline__ constexpr float root() { return D == 16 ? 0.25f : D == 32 ? 0.17677669529663688f : 0.125f; }
 
-// Two fp32 values in a pair of registers, and packed operations on such pairs.  A pair of one value twice is built once, outside of the loops.
-using pair = unsigned long long;
-__device__ __forceinline__ pair make_pair(float x, float y) {
-    pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
-    return p;
-}
-__device__ __forceinline__ void split_pair(pair p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
-__device__ __forceinline__ pair fma2(pair a, pair b, pair c) {
-    pair d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ pair add2(pair a, pair b) {
-    pair d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ pair mul2(pair a, pair b) {
-    pair d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
