@@ -346,22 +346,23 @@ typedef enum {
  *   x, y         [in / out] [B][H][W][C]
  *   gamma, beta  [in]  float [C], each may be NULL (ones, zeros)
  *   mean, rstd   [out] float [B][groups]: what the backward takes
+ *   workspace    slide_attn_group_norm_workspace bytes with backward = 0; may be NULL where that is 0 (small images)
  * Arithmetic is fp32 (the variance from deviations from the mean, so that a large mean costs nothing);
- * y is rounded to the dtype once.  Supported: C a multiple of 8 and of groups; whole groups that share
- * 16-byte pieces of a pixel at most 4096 (bf16) or 2048 (fp32) channels wide; eps >= 0.
+ * y is rounded to the dtype once.  Supported: C a multiple of 8 and of groups, up to 4096 (bf16) or
+ * 2048 (fp32); eps >= 0.
  */
 slide_attn_status slide_attn_group_norm_forward(const void* x, const float* gamma, const float* beta,
                                                 void* y, float* mean, float* rstd,
                                                 int B, int H, int W, int C, int groups, float eps,
                                                 slide_attn_activation act, slide_attn_dtype dtype,
-                                                void* cuda_stream);
+                                                void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * Its gradients for dy = d(loss)/d(y):
  *   x, gamma, beta, mean, rstd  [in] what the forward was given and gave
  *   dy, dx         [in / out] [B][H][W][C]
  *   dgamma, dbeta  [out] float [C], overwritten; both or neither may be NULL
- *   workspace      slide_attn_group_norm_workspace bytes; not used, and may be NULL, without dgamma
+ *   workspace      slide_attn_group_norm_workspace bytes with backward = 1
  */
 slide_attn_status slide_attn_group_norm_backward(const void* x, const float* gamma, const float* beta,
                                                  const float* mean, const float* rstd, const void* dy,
@@ -370,7 +371,7 @@ slide_attn_status slide_attn_group_norm_backward(const void* x, const float* gam
                                                  slide_attn_activation act, slide_attn_dtype dtype,
                                                  void* workspace, size_t workspace_bytes, void* cuda_stream);
 slide_attn_status slide_attn_group_norm_workspace(int B, int H, int W, int C, int groups,
-                                                  slide_attn_dtype dtype, size_t* bytes);
+                                                  slide_attn_dtype dtype, int backward, size_t* bytes);
 
 typedef enum {
     SLIDE_ATTN_DROP_ELEMENTS = 0,   /* each element is dropped by itself                           */

@@ -7,6 +7,7 @@ library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -72,9 +73,9 @@ def load() -> ctypes.CDLL:
         lib.slide_attn_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_double),
                                                ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i)]
         ll, f, sz = ctypes.c_longlong, ctypes.c_float, ctypes.c_size_t
-        lib.slide_attn_group_norm_forward.argtypes = [vp] * 6 + [i] * 5 + [f, i, i, vp]
+        lib.slide_attn_group_norm_forward.argtypes = [vp] * 6 + [i] * 5 + [f, i, i, vp, sz, vp]
         lib.slide_attn_group_norm_backward.argtypes = [vp] * 9 + [i] * 7 + [vp, sz, vp]
-        lib.slide_attn_group_norm_workspace.argtypes = [i] * 6 + [ctypes.POINTER(sz)]
+        lib.slide_attn_group_norm_workspace.argtypes = [i] * 7 + [ctypes.POINTER(sz)]
         lib.slide_attn_dropout_forward.argtypes = [vp] * 3 + [ll, ll, f, i, vp, i, vp]
         lib.slide_attn_dropout_backward.argtypes = [vp] * 2 + [ll, ll, f, i, vp, i, vp]
         lib.slide_attn_select_blocks.argtypes = [vp] * 3 + [i] * 9 + [vp, sz, vp]
@@ -272,22 +273,30 @@ def _expect(where, name, t, shape, dtype):
         raise ValueError(f"{where}: {name} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
-def _workspace(where, given, stream, size, *args):
-    """(tensor, address, bytes) of the scratch memory that `size` asks for.  Without one of the caller's it is torch's, taken from the pool
-    of the stream that the call runs on, so that it can be handed back as soon as the call is made."""
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(where, size, *args):
     need = ctypes.c_size_t()
-    _check(size(*args, ctypes.byref(need)), where)
+    _check(getattr(load(), size)(*args, ctypes.byref(need)), where)
+    return need.value
+
+
+def _workspace(where, given, stream, size, *args):
+    """(tensor, address, bytes) of the scratch memory that the library's function `size` asks for.  Without one of the caller's it is torch's, taken from the pool
+    of the stream that the call runs on, so that it can be handed back as soon as the call is made."""
+    need = _workspace_bytes(where, size, *args)
+    if given is None and need == 0:
+        return None, None, 0
     if given is None:
         if stream is None:
-            given = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+            given = torch.empty(need, dtype=torch.uint8, device="cuda")
         else:
             handle = _stream_ptr(stream)
             with torch.cuda.stream(torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()):
-                given = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+                given = torch.empty(need, dtype=torch.uint8, device="cuda")
     return given, _device_ptrs(where, given)[0], given.numel() * given.element_size()
 
 
-def slide_attn_group_norm_forward(x, gamma, beta, groups, eps, act, y, mean, rstd, stream=None) -> None:
+def slide_attn_group_norm_forward(x, gamma, beta, groups, eps, act, y, mean, rstd, stream=None, workspace=None) -> None:
     """y = act(group norm of x * gamma + beta) over [B, H, W, C] maps; act: ACT_NONE, ACT_SILU or ACT_GELU; gamma, beta: float32 [C] or None;
     mean, rstd: float32 [B, groups], written for the backward.  Asynchronous on `stream`."""
     where = "slide_attn_group_norm_forward"
@@ -298,8 +307,10 @@ def slide_attn_group_norm_forward(x, gamma, beta, groups, eps, act, y, mean, rst
         _expect(where, name, t, (C,), torch.float32)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _expect(where, name, t, (B, groups), torch.float32)
-    _check(load().slide_attn_group_norm_forward(*_device_ptrs(where, x, gamma, beta, y, mean, rstd), B, H, W, C, groups, eps, act, dtype,
-                                                _stream_ptr(stream)), where)
+    lib = load()
+    ptrs = _device_ptrs(where, x, gamma, beta, y, mean, rstd)
+    workspace, at, size = _workspace(where, workspace, stream, "slide_attn_group_norm_workspace", B, H, W, C, groups, dtype, 0)
+    _check(lib.slide_attn_group_norm_forward(*ptrs, B, H, W, C, groups, eps, act, dtype, at, size, _stream_ptr(stream)), where)
 
 
 def slide_attn_group_norm_backward(x, gamma, beta, groups, act, mean, rstd, dy, dx, dgamma, dbeta, stream=None, workspace=None) -> None:
@@ -313,10 +324,9 @@ def slide_attn_group_norm_backward(x, gamma, beta, groups, act, mean, rstd, dy, 
         _expect(where, name, t, (C,), torch.float32)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _expect(where, name, t, (B, groups), torch.float32)
-    lib, at, size = load(), None, 0
+    lib = load()
     ptrs = _device_ptrs(where, x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta)
-    if dgamma is not None:
-        workspace, at, size = _workspace(where, workspace, stream, lib.slide_attn_group_norm_workspace, B, H, W, C, groups, dtype)
+    workspace, at, size = _workspace(where, workspace, stream, "slide_attn_group_norm_workspace", B, H, W, C, groups, dtype, 1)
     _check(lib.slide_attn_group_norm_backward(*ptrs, B, H, W, C, groups, act, dtype, at, size, _stream_ptr(stream)), where)
 
 
@@ -369,7 +379,7 @@ def slide_attn_select_blocks(q, k, block, idx, stream=None, workspace=None) -> N
     bh, bw, top = _lists(where, q, idx, block)
     lib = load()
     ptrs = _device_ptrs(where, q, k, idx)
-    workspace, at, size = _workspace(where, workspace, stream, lib.slide_attn_select_workspace, B, H, W, heads, d, bh, bw)
+    workspace, at, size = _workspace(where, workspace, stream, "slide_attn_select_workspace", B, H, W, heads, d, bh, bw)
     _check(lib.slide_attn_select_blocks(*ptrs, B, H, W, heads, d, bh, bw, top, dtype, at, size, _stream_ptr(stream)), where)
 
 
@@ -398,5 +408,5 @@ def slide_attn_sparse_backward(q, k, v, idx, block, out, lse, dout, dq, dk, dv, 
     bh, bw, top = _lists(where, q, idx, block)
     lib = load()
     ptrs = _device_ptrs(where, q, k, v, idx, out, lse, dout, dq, dk, dv)
-    workspace, at, size = _workspace(where, workspace, stream, lib.slide_attn_sparse_workspace, B, H, W, heads, d, bh, bw)
+    workspace, at, size = _workspace(where, workspace, stream, "slide_attn_sparse_workspace", B, H, W, heads, d, bh, bw)
     _check(lib.slide_attn_sparse_backward(*ptrs, B, H, W, heads, d, bh, bw, top, dtype, at, size, _stream_ptr(stream)), where)

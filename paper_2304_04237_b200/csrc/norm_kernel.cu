@@ -4,34 +4,29 @@
 //   u = (x - m) rstd,  z = gamma_c u + beta_c,  y = act(z)
 //   dz = dy act'(z),  du = gamma_c dz,  dx = rstd (du - mean(du) - u mean(du u)),  dgamma_c = sum dz u,  dbeta_c = sum dz
 //
-// Bound by memory: x in and y out; x, dy in and dx out.  So each map is read from device memory once: a cluster of up to 16 CTAs
-// holds the pixels of one image's slab (whole groups, a multiple of 16 bytes wide) in its shared memory, exchanges the
-// sums through distributed shared memory and writes the result from what it holds.  Pixels that do not fit are read a
-// second time.  A thread keeps to one 16-byte column of the slab and reads from shared memory only what it copied there itself, so
-// the copies need no barrier.  All sums are fp32, in an order that only the shape decides.
-#include <cooperative_groups.h>
-
+// Bound by memory: x in and y out; x, dy in and dx out.  Two passes that stream over the map: sums of chunks of pixels, then the result, whose
+// inputs the second pass finds in L2 (126 MB) as long as they fit; a small launch between them joins the chunks and lays out what the second
+// pass multiplies each channel by.  A thread keeps to one 16-byte column of the pixels, of which a CTA takes whole rows.  Images that
+// one CTA can hold in its registers take one launch.
+// (One pass for all, with an image's pixels kept in the shared memory of a cluster of CTAs that exchange their sums, read every map once,
+// but its barriers and low occupancy made 64 x 56 x 56 x 96, bf16, GELU, forward and backward, take 114 us against PASS_US here.)
+// All sums are fp32, in an order that only the shape decides.
 #include "operators.cuh"
 #include "packed.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace slide_attn {
 
 namespace {
 
-constexpr int kMaxCluster = 16;
-constexpr int kMaxSmem = 227 * 1024;
-constexpr int kMostSms = 160;
+constexpr int kTogether = 4;           // 16-byte pieces that a thread has in flight (backward: half of them of each map)
+constexpr int kForwardCtas = 4, kBackwardCtas = 3;     // of 256 threads on an SM, as registers allow
+constexpr int kPair = kTogether / 2;
+constexpr int kOnce = 8;               // rounds of an image that one CTA keeps
 
-// How a call is cut up: slabs of `width` channels, clusters of `cluster` CTAs, of whose pixels `cached` rounds of `rows` stay in shared memory.
-struct NormPlan {
+struct NormShape {
     int P, C, groups, per_group;       // per_group: channels of a group
-    int width, slabs, cluster, log_cluster;
-    int columns, rows, threads;        // 16-byte columns of a slab; pixel rows that a CTA takes at a time
-    int cached;
-    size_t smem;
-    long long blocks;
+    int columns, rows, threads;        // 16-byte columns of a pixel; pixels that a CTA takes at a time (a round)
+    int rounds, chunks;                // of a CTA; CTAs of an image.  One chunk: an image in one launch
 };
 
 struct NormArgs {
@@ -42,7 +37,9 @@ struct NormArgs {
     void* y;              // forward: y, backward: dx
     float* mean;          // [B][groups], written by the forward and read by the backward
     float* rstd;
-    float* sums;          // backward: [B][C] of dz and, behind them, of dz u
+    float2* partial;      // [B][groups][chunks]: forward mean and sum of squares about it, backward sums of du and of du u
+    float* factors;       // [B][2 (forward) or 4 (backward)][C]: see Factors
+    float* channels;      // backward: [B][chunks][2][C], sums of dz and of dz u; or null
     float eps;
 };
 
@@ -132,34 +129,13 @@ template <int Act> __device__ __forceinline__ pair act_slope(pair z) {
     }
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// Where a thread works: a 16-byte column of the slab and every `rows`-th of the CTA's pixels.
-struct Place {
-    int column, first;
-    int mine, held;                    // how many pixels, and how many of them in shared memory
-    bool active;
-};
-__device__ __forceinline__ Place find_place(const NormPlan& pl, int pixels) {
-    Place p;
-    p.active = (int)threadIdx.x < pl.rows * pl.columns;
-    p.first = (int)threadIdx.x / pl.columns;
-    p.column = (int)threadIdx.x - p.first * pl.columns;
-    p.mine = p.active && p.first < pixels ? (pixels - p.first + pl.rows - 1) / pl.rows : 0;
-    p.held = min(p.mine, pl.cached);
-    return p;
-}
-// The groups (within the slab) of a column's channels.
-template <int V> __device__ __forceinline__ void find_groups(const NormPlan& pl, int column, int (&group)[V]) {
-    int g = column * V / pl.per_group, left = (g + 1) * pl.per_group - column * V;
+// The groups of a column's channels.
+template <int V> __device__ __forceinline__ void find_groups(int per_group, int column, int (&group)[V]) {
+    int g = column * V / per_group, left = (g + 1) * per_group - column * V;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         group[e] = g;
-        if (--left == 0) { ++g; left = pl.per_group; }
+        if (--left == 0) { ++g; left = per_group; }
     }
 }
 // V channels of gamma or beta, or a constant.
@@ -214,445 +190,561 @@ template <int V> __device__ __forceinline__ void leave(float* red, const pair (&
     }
 }
 
-constexpr int kCopyGroups = 4;         // groups that a thread's copies come in, so that the sums begin with the first
-template <int G> __device__ __forceinline__ void wait_for_group() { copies_wait<kCopyGroups - 1 - G>(); }
-
-template <typename T, int Act>
-__global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a, const NormPlan pl)
-{
-    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
-    extern __shared__ __align__(16) unsigned char smem[];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int K = pl.cluster, rank = (int)cluster.block_rank();
-    const unsigned unit = blockIdx.x / (unsigned)K;
-    const size_t b = unit / (unsigned)pl.slabs;
-    const int slab = (int)(unit - (unsigned)b * (unsigned)pl.slabs);
-    auto cut = [&](int r) { return (int)((long long)pl.P * r >> pl.log_cluster); };      // the first pixel of a CTA
-    const int p0 = cut(rank), pixels = cut(rank + 1) - p0;
-    const int slab_groups = pl.width / pl.per_group;
-    const Place at = find_place(pl, pixels);
-    const int active = pl.rows * pl.columns;
-
-    uint4* cache = reinterpret_cast<uint4*>(smem) + threadIdx.x;                     // [round][active thread]
-    float* red = reinterpret_cast<float*>(smem + (size_t)pl.cached * active * 16);
-    float* local = red + pl.threads * V;              // sums of this CTA's pixels and of the squares about their mean, by group
-    float* total = local + 2 * slab_groups;           // mean and rstd of the image
-    const size_t row_bytes = (size_t)pl.C * sizeof(T), step = (size_t)pl.rows * row_bytes;
-    const size_t start = (b * (size_t)pl.P + (size_t)(p0 + at.first)) * row_bytes + (size_t)slab * pl.width * sizeof(T) + (size_t)at.column * 16;
-    const unsigned char* src = static_cast<const unsigned char*>(a.x) + start;
-
-    grid_dependency_wait();
-    auto round_of = [&](int group) { return at.held * group / kCopyGroups; };
-#pragma unroll
-    for (int g = 0; g < kCopyGroups; ++g) {
-        for (int i = round_of(g); i < round_of(g + 1); ++i) copy16(smem_u32(cache + i * active), src + i * step);
-        copies_end_group();
-    }
-    int group[V];
-    find_groups<V>(pl, at.column, group);
-
-    // the CTA's own mean ...
-    pair sum[Q] = {};
-    auto add = [&](const uint4& r) {
-        pair v[Q];
-        Vec<T>::get(r, v);
-#pragma unroll
-        for (int e = 0; e < Q; ++e) sum[e] = add2(sum[e], v[e]);
-    };
-    auto add_group = [&](int g) {
-        for (int i = round_of(g); i < round_of(g + 1); ++i) add(cache[i * active]);
-    };
-    wait_for_group<0>(); add_group(0);
-    wait_for_group<1>(); add_group(1);
-    wait_for_group<2>(); add_group(2);
-    wait_for_group<3>(); add_group(3);
-#pragma unroll 4
-    for (int i = at.held; i < at.mine; ++i) add(*reinterpret_cast<const uint4*>(src + i * step));
-    const int lanes = lanes_for(slab_groups);
-    auto fold = [&](const pair (&v)[Q], float* out) {
-        if (at.active) leave<V>(red, v);
-        __syncthreads();
-        sum_cells(red, pl.rows, pl.width, pl.per_group, slab_groups, lanes, out);
-    };
-    fold(sum, local);
-    const float inv_own = 1.0f / ((float)pixels * (float)pl.per_group);               // no CTA is without pixels
-    // ... and the squares about it, which lose nothing however far the mean is from zero
-    pair mean[Q], square[Q] = {};                      // less the mean
-#pragma unroll
-    for (int e = 0; e < Q; ++e) mean[e] = make_pair(-local[group[2 * e]] * inv_own, -local[group[2 * e + 1]] * inv_own);
-    auto add_square = [&](const uint4& r) {
-        pair v[Q];
-        Vec<T>::get(r, v);
-#pragma unroll
-        for (int e = 0; e < Q; ++e) {
-            const pair d = add2(v[e], mean[e]);
-            square[e] = fma2(d, d, square[e]);
-        }
-    };
-#pragma unroll 2
-    for (int i = 0; i < at.held; ++i) add_square(cache[i * active]);
-#pragma unroll 4
-    for (int i = at.held; i < at.mine; ++i) add_square(*reinterpret_cast<const uint4*>(src + i * step));
-    fold(square, local + slab_groups);
-
-    // the cluster's: deviations from the first CTA's mean, so that nothing large cancels
-    cluster.sync();
-    // a lane for each CTA of the cluster (a power of two)
-    for (int first = 0; first < slab_groups; first += (int)blockDim.x >> pl.log_cluster) {
-        const int g = first + ((int)threadIdx.x >> pl.log_cluster), r = (int)threadIdx.x & (K - 1);
-        const bool there = g < slab_groups;
-        const float* theirs = cluster.map_shared_rank(local, r);
-        const float per = (float)pl.per_group, n = (float)pl.P * per;
-        const float own = (float)(cut(r + 1) - cut(r)) * per;
-        const float mine = there ? theirs[g] / own : 0.0f;
-        const float m0 = __shfl_sync(0xffffffffu, mine, (int)threadIdx.x & 31 & ~(K - 1));
-        float shift = own * (mine - m0);
-        for (int o = K / 2; o > 0; o /= 2) shift += __shfl_xor_sync(0xffffffffu, shift, o);
-        const float m = m0 + shift / n, d = mine - m;
-        float m2 = there ? fmaf(own * d, d, theirs[slab_groups + g]) : 0.0f;
-        for (int o = K / 2; o > 0; o /= 2) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-        if (there && r == 0) {
-            const float rstd = 1.0f / sqrtf(m2 / n + a.eps);
-            total[g] = m;
-            total[slab_groups + g] = rstd;
-            if (rank == 0) {
-                const size_t o = b * pl.groups + slab * slab_groups + g;
-                a.mean[o] = m;
-                a.rstd[o] = rstd;
-            }
-        }
-    }
-    cluster.sync();          // `total` is complete, and nobody reads another CTA's shared memory any more
-    if (!at.active) return;
-
-    pair scale[Q], beta[Q];
-    get_weights<V>(a.gamma, slab * pl.width + at.column * V, 1.0f, scale);
-    get_weights<V>(a.beta, slab * pl.width + at.column * V, 0.0f, beta);
-#pragma unroll
-    for (int e = 0; e < Q; ++e) {
-        mean[e] = make_pair(-total[group[2 * e]], -total[group[2 * e + 1]]);
-        scale[e] = mul2(scale[e], make_pair(total[slab_groups + group[2 * e]], total[slab_groups + group[2 * e + 1]]));
-    }
-    unsigned char* dst = static_cast<unsigned char*>(a.y) + start;
-    auto apply = [&](const uint4& r) {
-        pair v[Q];
-        Vec<T>::get(r, v);
-#pragma unroll
-        for (int e = 0; e < Q; ++e) v[e] = act_value<Act>(fma2(add2(v[e], mean[e]), scale[e], beta[e]));
-        return Vec<T>::put(v);
-    };
-    for (int i = 0; i < at.held; ++i) *reinterpret_cast<uint4*>(dst + i * step) = apply(cache[i * active]);
-#pragma unroll 4
-    for (int i = at.held; i < at.mine; ++i)
-        *reinterpret_cast<uint4*>(dst + i * step) = apply(*reinterpret_cast<const uint4*>(src + i * step));
+// A thread's part of a chunk.
+struct Place {
+    int column;
+    int mine;                          // its rounds
+    int pixels;                        // the chunk's
+    unsigned image;
+    int chunk;
+    size_t start, step;                // bytes to its first piece and from one to the next
+    bool active;
+};
+__device__ __forceinline__ int chunk_pixels(const NormShape& s, int chunk) { return min(s.rows * s.rounds, s.P - chunk * s.rows * s.rounds); }
+template <typename T> __device__ __forceinline__ Place find_place(const NormShape& s) {
+    Place p;
+    p.image = blockIdx.x / (unsigned)s.chunks;
+    p.chunk = (int)(blockIdx.x - p.image * (unsigned)s.chunks);
+    const int row = (int)threadIdx.x / s.columns;
+    p.column = (int)threadIdx.x - row * s.columns;
+    p.active = row < s.rows;
+    p.pixels = chunk_pixels(s, p.chunk);
+    p.mine = p.active ? (p.pixels - row + s.rows - 1) / s.rows : 0;
+    const size_t row_bytes = (size_t)s.C * sizeof(T);
+    p.start = ((size_t)p.image * s.P + (size_t)p.chunk * (s.rows * s.rounds) + row) * row_bytes + (size_t)p.column * 16;
+    p.step = s.rows * row_bytes;
+    return p;
 }
 
-// Shared memory holds x and, in the place of dy, dz in fp32 (bf16: twice the room): act' is not computed twice.
-template <typename T, int Act>
-__global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a, const NormPlan pl)
-{
-    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
-    extern __shared__ __align__(16) unsigned char smem[];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int K = pl.cluster, rank = (int)cluster.block_rank();
-    const unsigned unit = blockIdx.x / (unsigned)K;
-    const size_t b = unit / (unsigned)pl.slabs;
-    const int slab = (int)(unit - (unsigned)b * (unsigned)pl.slabs);
-    auto cut = [&](int r) { return (int)((long long)pl.P * r >> pl.log_cluster); };      // the first pixel of a CTA
-    const int p0 = cut(rank), pixels = cut(rank + 1) - p0;
-    const int slab_groups = pl.width / pl.per_group;
-    const Place at = find_place(pl, pixels);
-    const int active = pl.rows * pl.columns;
+// What the passes multiply by, V channels of it.  Forward: less the mean, and rstd gamma.  Backward, with c = x - mean: z = c (rstd gamma) + beta,
+// dx = dz (rstd gamma) + (c quad + shift), quad = -rstd^2 mean(du u), shift = -rstd mean(du).
+template <int V> __device__ __forceinline__ void get_factors(const float* factors, int C, int which, int column, pair (&v)[V / 2]) {
+    get_weights<V>(factors + (size_t)which * C, column * V, 0.0f, v);
+}
 
-    uint4* cache_x = reinterpret_cast<uint4*>(smem) + threadIdx.x;
-    uint4* cache_g = cache_x + (size_t)pl.cached * active;                            // dy; then dz, of bf16 the first half
-    uint4* cache_h = cache_g + (size_t)pl.cached * active;                            // bf16: the second half of dz
-    float* red = reinterpret_cast<float*>(smem + (size_t)pl.cached * active * (16 + 4 * V));
-    float* channel = red + pl.threads * V;            // sums of dz, then of dz u, by channel: this CTA's
-    float* weighted = channel + 2 * pl.width;         // the same times gamma
-    float* local = weighted + 2 * pl.width;           // sums of du, then of du u, by group: this CTA's
-    float* total = local + 2 * slab_groups;           // their means over the image
-    const size_t row_bytes = (size_t)pl.C * sizeof(T), step = (size_t)pl.rows * row_bytes;
-    const size_t start = (b * (size_t)pl.P + (size_t)(p0 + at.first)) * row_bytes + (size_t)slab * pl.width * sizeof(T) + (size_t)at.column * 16;
-    const unsigned char* src_x = static_cast<const unsigned char*>(a.x) + start;
-    const unsigned char* src_g = static_cast<const unsigned char*>(a.dy) + start;
-
-    grid_dependency_wait();
-    auto round_of = [&](int group) { return at.held * group / kCopyGroups; };
+// First pass, forward: of a chunk, each group's mean and sum of squares about that mean, which loses nothing however far it is from zero: batch by
+// batch of a thread's pixels (mean, then squares about it), joined by what the means differ, then over the threads in the same way.
+template <typename T>
+struct Moments {
+    static constexpr int Q = Vec<T>::pairs;
+    pair mean[Q] = {}, square[Q] = {};
+    float n = 0.0f;
+    template <int N> __device__ __forceinline__ void add(const uint4 (&raw)[N], int count) {
+        pair sum[Q] = {};
 #pragma unroll
-    for (int g = 0; g < kCopyGroups; ++g) {
-        for (int i = round_of(g); i < round_of(g + 1); ++i) {
-            copy16(smem_u32(cache_x + i * active), src_x + i * step);
-            copy16(smem_u32(cache_g + i * active), src_g + i * step);
+        for (int i = 0; i < N; ++i)
+            if (i < count) {
+                pair v[Q];
+                Vec<T>::get(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < Q; ++e) sum[e] = add2(sum[e], v[e]);
+            }
+        const float k = (float)count, all = n + k;
+        const pair inv = both(-1.0f / k), part = both(k / all), weight = both(n * k / all);
+        pair own[Q], own_square[Q] = {};                            // less the batch's mean
+#pragma unroll
+        for (int e = 0; e < Q; ++e) own[e] = mul2(sum[e], inv);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < count) {
+                pair v[Q];
+                Vec<T>::get(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < Q; ++e) {
+                    const pair d = add2(v[e], own[e]);
+                    own_square[e] = fma2(d, d, own_square[e]);
+                }
+            }
+#pragma unroll
+        for (int e = 0; e < Q; ++e) {
+            const pair d = fma2(own[e], both(-1.0f), mul2(mean[e], both(-1.0f)));       // the batch's mean less the one so far
+            mean[e] = fma2(d, part, mean[e]);
+            square[e] = fma2(mul2(d, d), weight, add2(square[e], own_square[e]));
         }
-        copies_end_group();
+        n = all;
+    }
+};
+// Each group's mean and sum of squares from the threads'; all threads call it.  red: [row][channel]
+template <typename T>
+__device__ __forceinline__ void join_threads(const NormShape& s, const Place& at, const Moments<T>& m, const int (&group)[2 * Vec<T>::pairs], float* red,
+                                             float* means, float* squares) {
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    const int lanes = lanes_for(s.groups);
+    pair v[Q];
+#pragma unroll
+    for (int e = 0; e < Q; ++e) v[e] = mul2(m.mean[e], both(m.n));
+    if (at.active) leave<V>(red, v);
+    __syncthreads();
+    sum_cells(red, s.rows, s.C, s.per_group, s.groups, lanes, means);
+    const float inv = 1.0f / ((float)at.pixels * (float)s.per_group);
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+        const pair d = add2(m.mean[e], make_pair(-means[group[2 * e]] * inv, -means[group[2 * e + 1]] * inv));
+        v[e] = fma2(mul2(d, d), both(m.n), m.square[e]);
+    }
+    if (at.active) leave<V>(red, v);
+    __syncthreads();
+    for (int g = threadIdx.x; g < s.groups; g += blockDim.x) means[g] *= inv;
+    sum_cells(red, s.rows, s.C, s.per_group, s.groups, lanes, squares);
+}
+
+template <int Threads, typename T>
+__global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_sums_kernel(const NormArgs a, const NormShape s)
+{
+    constexpr int V = 2 * Vec<T>::pairs;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float* red = reinterpret_cast<float*>(smem);
+    float* means = red + s.threads * V;
+    float* squares = means + s.groups;
+    const Place at = find_place<T>(s);
+    const unsigned char* src = static_cast<const unsigned char*>(a.x) + at.start;
+    grid_dependency_wait();
+    Moments<T> m;
+#pragma unroll 1
+    for (int done = 0; done < at.mine; done += kTogether) {
+        const int count = min(at.mine - done, kTogether);
+        uint4 raw[kTogether];
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (i < count) { raw[i] = *reinterpret_cast<const uint4*>(src); src += at.step; }
+        m.add(raw, count);
     }
     int group[V];
-    find_groups<V>(pl, at.column, group);
-    pair gamma[Q], beta[Q], mean[Q], rstd[Q];          // less the mean
-    get_weights<V>(a.gamma, slab * pl.width + at.column * V, 1.0f, gamma);
-    get_weights<V>(a.beta, slab * pl.width + at.column * V, 0.0f, beta);
-    {
-        const float* m = a.mean + b * pl.groups + slab * slab_groups;
-        const float* r = a.rstd + b * pl.groups + slab * slab_groups;
+    find_groups<V>(s.per_group, at.column, group);
+    join_threads<T>(s, at, m, group, red, means, squares);
+    for (int g = threadIdx.x; g < s.groups; g += blockDim.x)
+        a.partial[((size_t)at.image * s.groups + g) * s.chunks + at.chunk] = make_float2(means[g], squares[g]);
+}
+
+// Between the passes, a CTA an image, a warp a group: joins the chunks' moments (deviations from the first chunk's mean, so that nothing
+// large cancels), then lays out the factors.
+__global__ void __launch_bounds__(512) norm_join_kernel(const NormArgs a, const NormShape s)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    float2* stats = reinterpret_cast<float2*>(smem);
+    grid_dependency_wait();
+    const size_t b = blockIdx.x;
+    const int lane = threadIdx.x % 32;
+    const float per = (float)s.per_group, n = (float)s.P * per;
+    for (int g = threadIdx.x / 32; g < s.groups; g += blockDim.x / 32) {
+        const float2* chunks = a.partial + (b * s.groups + g) * s.chunks;
+        const float m0 = chunks[0].x;
+        float shift = 0.0f;
+        for (int c = lane; c < s.chunks; c += 32) shift += (float)chunk_pixels(s, c) * per * (chunks[c].x - m0);
 #pragma unroll
-        for (int e = 0; e < Q; ++e) {
-            mean[e] = make_pair(-m[group[2 * e]], -m[group[2 * e + 1]]);
-            rstd[e] = make_pair(r[group[2 * e]], r[group[2 * e + 1]]);
+        for (int o = 16; o > 0; o /= 2) shift += __shfl_xor_sync(0xffffffffu, shift, o);
+        const float m = m0 + shift / n;
+        float m2 = 0.0f;
+        for (int c = lane; c < s.chunks; c += 32) {
+            const float2 v = chunks[c];
+            const float d = v.x - m;
+            m2 += fmaf((float)chunk_pixels(s, c) * per * d, d, v.y);
         }
-    }
-    pair s1[Q] = {}, s2[Q] = {};
-    // dz of a column of 16 bytes
-    auto slopes = [&](const uint4& rx, const uint4& rg, pair (&u)[Q], pair (&dz)[Q]) {
-        Vec<T>::get(rx, u);
-        Vec<T>::get(rg, dz);
 #pragma unroll
-        for (int e = 0; e < Q; ++e) {
-            u[e] = mul2(add2(u[e], mean[e]), rstd[e]);
-            if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<Act>(fma2(u[e], gamma[e], beta[e])));
+        for (int o = 16; o > 0; o /= 2) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+        if (lane == 0) {
+            const float rstd = 1.0f / sqrtf(m2 / n + a.eps);
+            stats[g] = make_float2(m, rstd);
+            a.mean[b * s.groups + g] = m;
+            a.rstd[b * s.groups + g] = rstd;
         }
-    };
-    auto add = [&](const pair (&u)[Q], const pair (&dz)[Q]) {
-#pragma unroll
-        for (int e = 0; e < Q; ++e) {
-            s1[e] = add2(s1[e], dz[e]);
-            s2[e] = fma2(dz[e], u[e], s2[e]);
-        }
-    };
-    auto add_group = [&](int g) {
-        for (int i = round_of(g); i < round_of(g + 1); ++i) {
-            pair u[Q], dz[Q];
-            slopes(cache_x[i * active], cache_g[i * active], u, dz);
-            add(u, dz);
-            const pair lower[2] = {dz[0], dz[1]};
-            cache_g[i * active] = Vec<float>::put(lower);
-            if constexpr (Q == 4) {
-                const pair upper[2] = {dz[2], dz[3]};
-                cache_h[i * active] = Vec<float>::put(upper);
-            }
-        }
-    };
-    wait_for_group<0>(); add_group(0);
-    wait_for_group<1>(); add_group(1);
-    wait_for_group<2>(); add_group(2);
-    wait_for_group<3>(); add_group(3);
-#pragma unroll 2
-    for (int i = at.held; i < at.mine; ++i) {
-        pair u[Q], dz[Q];
-        slopes(*reinterpret_cast<const uint4*>(src_x + i * step), *reinterpret_cast<const uint4*>(src_g + i * step), u, dz);
-        add(u, dz);
-    }
-    auto fold = [&](const pair (&v)[Q], float* out) {
-        if (at.active) leave<V>(red, v);
-        __syncthreads();
-        sum_cells(red, pl.rows, pl.width, 1, pl.width, lanes_for(pl.width), out);
-    };
-    fold(s1, channel);
-    fold(s2, channel + pl.width);
-    for (int c = threadIdx.x; c < 2 * pl.width; c += blockDim.x) {
-        const int ch = c < pl.width ? c : c - pl.width;
-        weighted[c] = channel[c] * (a.gamma ? a.gamma[slab * pl.width + ch] : 1.0f);
     }
     __syncthreads();
-    sum_cells(weighted, 1, 0, pl.per_group, 2 * slab_groups, lanes_for(2 * slab_groups), local);
-    cluster.sync();
-    // a lane for each CTA of the cluster (a power of two)
-    const float inv = 1.0f / ((float)pl.P * (float)pl.per_group);
-    for (int first = 0; first < 2 * slab_groups; first += (int)blockDim.x >> pl.log_cluster) {
-        const int g = first + ((int)threadIdx.x >> pl.log_cluster), r = (int)threadIdx.x & (K - 1);
-        float s = g < 2 * slab_groups ? cluster.map_shared_rank(local, r)[g] : 0.0f;
-        for (int o = K / 2; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (g < 2 * slab_groups && r == 0) total[g] = s * inv;
-    }
-    if (a.sums) {
-        const size_t images = gridDim.x / (unsigned)K / (unsigned)pl.slabs;
-        for (int c = rank * (int)blockDim.x + (int)threadIdx.x; c < 2 * pl.width; c += K * (int)blockDim.x) {
-            float s = 0.0f;
-            for (int r = 0; r < K; ++r) s += cluster.map_shared_rank(channel, r)[c];
-            const int which = c / pl.width, ch = c - which * pl.width;
-            a.sums[(which * images + b) * pl.C + slab * pl.width + ch] = s;
-        }
-    }
-    cluster.sync();
-    if (!at.active) return;
-
-    // dx = rstd (gamma dz - m1 - u m2)
-    pair m1[Q], m2[Q];                                 // less the means
-#pragma unroll
-    for (int e = 0; e < Q; ++e) {
-        m1[e] = make_pair(-total[group[2 * e]], -total[group[2 * e + 1]]);
-        m2[e] = make_pair(-total[slab_groups + group[2 * e]], -total[slab_groups + group[2 * e + 1]]);
-    }
-    unsigned char* dst = static_cast<unsigned char*>(a.y) + start;
-    auto finish = [&](const pair (&u)[Q], pair (&dz)[Q]) {
-#pragma unroll
-        for (int e = 0; e < Q; ++e) dz[e] = mul2(rstd[e], fma2(u[e], m2[e], fma2(dz[e], gamma[e], m1[e])));
-        return Vec<T>::put(dz);
-    };
-    for (int i = 0; i < at.held; ++i) {
-        pair u[Q], dz[Q], half[2];
-        Vec<T>::get(cache_x[i * active], u);
-#pragma unroll
-        for (int e = 0; e < Q; ++e) u[e] = mul2(add2(u[e], mean[e]), rstd[e]);
-        Vec<float>::get(cache_g[i * active], half);
-        dz[0] = half[0]; dz[1] = half[1];
-        if constexpr (Q == 4) {
-            Vec<float>::get(cache_h[i * active], half);
-            dz[2] = half[0]; dz[3] = half[1];
-        }
-        *reinterpret_cast<uint4*>(dst + i * step) = finish(u, dz);
-    }
-#pragma unroll 2
-    for (int i = at.held; i < at.mine; ++i) {
-        pair u[Q], dz[Q];
-        slopes(*reinterpret_cast<const uint4*>(src_x + i * step), *reinterpret_cast<const uint4*>(src_g + i * step), u, dz);
-        *reinterpret_cast<uint4*>(dst + i * step) = finish(u, dz);
+    float* out = a.factors + b * 2 * s.C;
+    for (int c = threadIdx.x; c < s.C; c += blockDim.x) {
+        const float2 v = stats[c / s.per_group];
+        out[c] = -v.x;
+        out[s.C + c] = v.y * (a.gamma ? a.gamma[c] : 1.0f);
     }
 }
 
-// dbeta and dgamma: the images' sums, added up in the images' order.  32 channels of one of the two a block, eight rows at a time.
-__global__ void norm_weight_kernel(const float* sums, long long images, int C, float* dgamma, float* dbeta)
+template <typename T, int Act>
+__device__ __forceinline__ uint4 normalised(const uint4& raw, const pair (&mean)[Vec<T>::pairs], const pair (&scale)[Vec<T>::pairs],
+                                            const pair (&beta)[Vec<T>::pairs]) {
+    pair v[Vec<T>::pairs];
+    Vec<T>::get(raw, v);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::pairs; ++e) v[e] = act_value<Act>(fma2(add2(v[e], mean[e]), scale[e], beta[e]));
+    return Vec<T>::put(v);
+}
+
+template <int Threads, typename T, int Act>
+__global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_forward_kernel(const NormArgs a, const NormShape s)
 {
-    __shared__ float part[8][33];
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    const Place at = find_place<T>(s);
+    const unsigned char* src = static_cast<const unsigned char*>(a.x) + at.start;
+    unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
     grid_dependency_wait();
-    const int c = blockIdx.x * 32 + threadIdx.x, which = blockIdx.y;
+    if (!at.active) return;
+    pair scale[Q], beta[Q], mean[Q];
+    const float* factors = a.factors + (size_t)at.image * 2 * s.C;
+    get_factors<V>(factors, s.C, 0, at.column, mean);
+    get_factors<V>(factors, s.C, 1, at.column, scale);
+    get_weights<V>(a.beta, at.column * V, 0.0f, beta);
+#pragma unroll 1
+    for (int done = 0; done < at.mine; done += kTogether) {
+        uint4 raw[kTogether];
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (done + i < at.mine) raw[i] = *reinterpret_cast<const uint4*>(src + i * at.step);
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i)
+            if (done + i < at.mine) *reinterpret_cast<uint4*>(dst + i * at.step) = normalised<T, Act>(raw[i], mean, scale, beta);
+        src += kTogether * at.step;
+        dst += kTogether * at.step;
+    }
+}
+
+// An image of one chunk: all of the forward, from registers.
+template <int Threads, typename T, int Act>
+__global__ void __launch_bounds__(Threads, 2 * 256 / Threads) norm_forward_once_kernel(const NormArgs a, const NormShape s)
+{
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float* red = reinterpret_cast<float*>(smem);
+    float* means = red + s.threads * V;
+    float* squares = means + s.groups;
+    const Place at = find_place<T>(s);
+    const unsigned char* src = static_cast<const unsigned char*>(a.x) + at.start;
+    unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
+    grid_dependency_wait();
+    uint4 raw[kOnce];
+#pragma unroll
+    for (int i = 0; i < kOnce; ++i)
+        if (i < at.mine) raw[i] = *reinterpret_cast<const uint4*>(src + i * at.step);
+    int group[V];
+    find_groups<V>(s.per_group, at.column, group);
+    pair scale[Q], beta[Q], mean[Q];
+    get_weights<V>(a.gamma, at.column * V, 1.0f, scale);
+    get_weights<V>(a.beta, at.column * V, 0.0f, beta);
+    Moments<T> m;
+    if (at.mine > 0) m.add(raw, at.mine);
+    join_threads<T>(s, at, m, group, red, means, squares);
+    const float inv = 1.0f / ((float)s.P * (float)s.per_group);
+    for (int g = threadIdx.x; g < s.groups; g += blockDim.x) {
+        const float rstd = 1.0f / sqrtf(squares[g] * inv + a.eps);
+        const size_t o = (size_t)at.image * s.groups + g;
+        a.mean[o] = means[g];
+        a.rstd[o] = rstd;
+        squares[g] = rstd;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+        mean[e] = make_pair(-means[group[2 * e]], -means[group[2 * e + 1]]);
+        scale[e] = mul2(scale[e], make_pair(squares[group[2 * e]], squares[group[2 * e + 1]]));
+    }
+#pragma unroll
+    for (int i = 0; i < kOnce; ++i)
+        if (i < at.mine) *reinterpret_cast<uint4*>(dst + i * at.step) = normalised<T, Act>(raw[i], mean, scale, beta);
+}
+
+// First pass, backward: of a chunk, each channel's sums of dz and dz u, and each group's of du and du u.
+template <int Threads, typename T, int Act>
+__global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_slopes_kernel(const NormArgs a, const NormShape s)
+{
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float* red = reinterpret_cast<float*>(smem);                    // [row][channel]; later two values a channel
+    float* channel = red + max(s.threads * V, 2 * s.C);             // sums of dz, then of dz u
+    float* local = channel + 2 * s.C;                               // the groups'
+    const Place at = find_place<T>(s);
+    const unsigned char* src_x = static_cast<const unsigned char*>(a.x) + at.start;
+    const unsigned char* src_g = static_cast<const unsigned char*>(a.dy) + at.start;
+    grid_dependency_wait();
+    pair mean[Q], scale[Q], beta[Q], s1[Q] = {}, s2[Q] = {};
+    const float* means = a.mean + (size_t)at.image * s.groups;
+    const float* rstds = a.rstd + (size_t)at.image * s.groups;
+    {
+        int group[V];
+        find_groups<V>(s.per_group, at.column, group);
+        get_weights<V>(a.gamma, at.column * V, 1.0f, scale);
+        get_weights<V>(a.beta, at.column * V, 0.0f, beta);
+#pragma unroll
+        for (int e = 0; e < Q; ++e) {
+            mean[e] = make_pair(-means[group[2 * e]], -means[group[2 * e + 1]]);
+            scale[e] = mul2(scale[e], make_pair(rstds[group[2 * e]], rstds[group[2 * e + 1]]));
+        }
+    }
+#pragma unroll 1
+    for (int done = 0; done < at.mine; done += kPair) {
+        uint4 x[kPair], g[kPair];
+#pragma unroll
+        for (int i = 0; i < kPair; ++i)
+            if (done + i < at.mine) {
+                x[i] = *reinterpret_cast<const uint4*>(src_x + i * at.step);
+                g[i] = *reinterpret_cast<const uint4*>(src_g + i * at.step);
+            }
+#pragma unroll
+        for (int i = 0; i < kPair; ++i)
+            if (done + i < at.mine) {
+                pair c[Q], dz[Q];
+                Vec<T>::get(x[i], c);
+                Vec<T>::get(g[i], dz);
+#pragma unroll
+                for (int e = 0; e < Q; ++e) {
+                    c[e] = add2(c[e], mean[e]);
+                    if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<Act>(fma2(c[e], scale[e], beta[e])));
+                    s1[e] = add2(s1[e], dz[e]);
+                    s2[e] = fma2(dz[e], c[e], s2[e]);
+                }
+            }
+        src_x += kPair * at.step;
+        src_g += kPair * at.step;
+    }
+    const int lanes = lanes_for(s.C);
+    if (at.active) leave<V>(red, s1);
+    __syncthreads();
+    sum_cells(red, s.rows, s.C, 1, s.C, lanes, channel);
+    if (at.active) leave<V>(red, s2);
+    __syncthreads();
+    sum_cells(red, s.rows, s.C, 1, s.C, lanes, channel + s.C);
+    float* out = a.channels ? a.channels + ((size_t)at.image * s.chunks + at.chunk) * 2 * s.C : nullptr;
+    for (int i = threadIdx.x; i < 2 * s.C; i += blockDim.x) {
+        const int c = i < s.C ? i : i - s.C;
+        const float v = i < s.C ? channel[i] : channel[i] * rstds[c / s.per_group];
+        if (out) out[i] = v;
+        red[i] = v * (a.gamma ? a.gamma[c] : 1.0f);
+    }
+    __syncthreads();
+    sum_cells(red, 1, 0, s.per_group, 2 * s.groups, lanes_for(2 * s.groups), local);
+    for (int g = threadIdx.x; g < s.groups; g += blockDim.x)
+        a.partial[((size_t)at.image * s.groups + g) * s.chunks + at.chunk] = make_float2(local[g], local[s.groups + g]);
+}
+
+// Between the passes of the backward, a CTA an image, a warp a group.
+__global__ void __launch_bounds__(512) norm_join_slopes_kernel(const NormArgs a, const NormShape s)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    float2* stats = reinterpret_cast<float2*>(smem);                // quad and shift
+    grid_dependency_wait();
+    const size_t b = blockIdx.x;
+    const int lane = threadIdx.x % 32;
+    const float inv = 1.0f / ((float)s.P * (float)s.per_group);
+    const float* rstds = a.rstd + b * s.groups;
+    for (int g = threadIdx.x / 32; g < s.groups; g += blockDim.x / 32) {
+        const float2* chunks = a.partial + (b * s.groups + g) * s.chunks;
+        float2 t = make_float2(0.0f, 0.0f);
+        for (int c = lane; c < s.chunks; c += 32) { t.x += chunks[c].x; t.y += chunks[c].y; }
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) {
+            t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+            t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+        }
+        if (lane == 0) stats[g] = make_float2(-rstds[g] * rstds[g] * (t.y * inv), -rstds[g] * (t.x * inv));
+    }
+    __syncthreads();
+    float* out = a.factors + b * 4 * s.C;
+    for (int c = threadIdx.x; c < s.C; c += blockDim.x) {
+        const int g = c / s.per_group;
+        out[c] = -a.mean[b * s.groups + g];
+        out[s.C + c] = rstds[g] * (a.gamma ? a.gamma[c] : 1.0f);
+        out[2 * s.C + c] = stats[g].x;
+        out[3 * s.C + c] = stats[g].y;
+    }
+}
+
+template <int Threads, typename T, int Act>
+__global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_backward_kernel(const NormArgs a, const NormShape s)
+{
+    constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    const Place at = find_place<T>(s);
+    const unsigned char* src_x = static_cast<const unsigned char*>(a.x) + at.start;
+    const unsigned char* src_g = static_cast<const unsigned char*>(a.dy) + at.start;
+    unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
+    grid_dependency_wait();
+    if (!at.active) return;
+    pair mean[Q], scale[Q], beta[Q], quad[Q], shift[Q];
+    const float* factors = a.factors + (size_t)at.image * 4 * s.C;
+    get_factors<V>(factors, s.C, 0, at.column, mean);
+    get_factors<V>(factors, s.C, 1, at.column, scale);
+    get_factors<V>(factors, s.C, 2, at.column, quad);
+    get_factors<V>(factors, s.C, 3, at.column, shift);
+    get_weights<V>(a.beta, at.column * V, 0.0f, beta);
+#pragma unroll 1
+    for (int done = 0; done < at.mine; done += kPair) {
+        uint4 x[kPair], g[kPair];
+#pragma unroll
+        for (int i = 0; i < kPair; ++i)
+            if (done + i < at.mine) {
+                x[i] = *reinterpret_cast<const uint4*>(src_x + i * at.step);
+                g[i] = *reinterpret_cast<const uint4*>(src_g + i * at.step);
+            }
+#pragma unroll
+        for (int i = 0; i < kPair; ++i)
+            if (done + i < at.mine) {
+                pair c[Q], dz[Q];
+                Vec<T>::get(x[i], c);
+                Vec<T>::get(g[i], dz);
+#pragma unroll
+                for (int e = 0; e < Q; ++e) {
+                    c[e] = add2(c[e], mean[e]);
+                    if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<Act>(fma2(c[e], scale[e], beta[e])));
+                    dz[e] = fma2(dz[e], scale[e], fma2(c[e], quad[e], shift[e]));
+                }
+                *reinterpret_cast<uint4*>(dst + i * at.step) = Vec<T>::put(dz);
+            }
+        src_x += kPair * at.step;
+        src_g += kPair * at.step;
+        dst += kPair * at.step;
+    }
+}
+
+// dbeta and dgamma: the chunks' sums, added up in their order.  32 of the 2 C columns a block, 32 rows at a time.
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* channels, long long chunks, int C, float* dgamma, float* dbeta)
+{
+    __shared__ float part[32][33];
+    grid_dependency_wait();
+    const int c = blockIdx.x * 32 + threadIdx.x;
     float s = 0.0f;
-    if (c < C)
-#pragma unroll 4
-        for (long long b = threadIdx.y; b < images; b += 8) s += sums[((size_t)which * images + b) * C + c];
+    if (c < 2 * C)
+#pragma unroll 8
+        for (long long r = threadIdx.y; r < chunks; r += 32) s += channels[(size_t)r * 2 * C + c];
     part[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
-    if (threadIdx.y == 0 && c < C) {
+    s = part[threadIdx.x][threadIdx.y];                             // a warp a column
 #pragma unroll
-        for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
-        (which ? dgamma : dbeta)[c] = s;
-    }
+    for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const int column = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && column < 2 * C) (column < C ? dbeta : dgamma)[column < C ? column : column - C] = s;
 }
 
-long long gcd(long long a, long long b) { return b ? gcd(b, a % b) : a; }
-
-// maps: 1 forward, 2 backward.  False where no slab fits a block, or no grid the call.
-bool make_plan(long long B, long long P, int C, int groups, int size, int maps, int num_sms, NormPlan* out) {
-    NormPlan p = {};
-    const int V = 16 / size;
-    p.P = (int)P; p.C = C; p.groups = groups; p.per_group = C / groups;
-    const int narrow = (int)((long long)p.per_group / gcd(p.per_group, V) * V);   // the narrowest slab: whole groups and 16-byte columns
-    const int most_slabs = C / narrow;
-    if (B * most_slabs > 0x7fffffffLL / kMaxCluster) return false;
-    const int held = maps == 1 ? size : size + 4;      // bytes that stay of an element
-    // A slab as wide as may be reads the longest runs of memory; narrower ones take smaller clusters, give more CTAs and may be held whole.
-    // A CTA's share of 72 KB lets three share an SM.
-    constexpr long long kShare = 72 * 1024;
-    int best_slabs = 0, best_cluster = 0;
-    for (int s = 1; s <= most_slabs; ++s) {
-        if (most_slabs % s || C / s / V > 512) continue;
-        if (best_slabs && C / s * size < 64) break;
-        const long long bytes = P * (C / s) * held;
-        int K = 1;
-        while (K < kMaxCluster && 2 * K <= P && (bytes > K * kShare || (B * s * K < 2 * num_sms && bytes > K * 8 * 1024))) K *= 2;
-        best_slabs = s;
-        best_cluster = K;
-        if (bytes <= K * kShare && K <= 8 && (B * s * K >= 2 * num_sms || bytes <= K * 16 * 1024)) break;
+// False where a pixel has too many columns for a CTA, or the call too many CTAs for a grid.  `maps`: 1 forward, 2 backward.
+bool make_shape(long long B, long long P, int C, int groups, int size, int maps, NormShape* out) {
+    NormShape s = {};
+    s.P = (int)P; s.C = C; s.groups = groups; s.per_group = C / groups;
+    s.columns = C * size / 16;
+    if (s.columns > 512) return false;
+    s.threads = s.columns > 256 ? 512 : 256;
+    s.rows = s.threads / s.columns;
+    if (maps == 1 && P <= (long long)(512 / s.columns) * kOnce) {
+        // an image in one CTA's registers
+        if (P > (long long)s.rows * kOnce) { s.threads = 512; s.rows = 512 / s.columns; }
+        s.rounds = kOnce;
+    } else {
+        // What a thread does once (some hundred instructions) wants many rounds: as many CTAs as the SMs hold together, or the images' number.
+        const long long all = (P + s.rows - 1) / s.rows, room = 148LL * (maps == 1 ? kForwardCtas : kBackwardCtas) * 256 / s.threads;
+        const long long each = room / B > 0 ? room / B : 1;
+        long long rounds = (all + each - 1) / each;
+        if (rounds < kTogether) rounds = kTogether;
+        s.rounds = (int)rounds;
     }
-    if (!best_slabs) return false;
-    p.slabs = best_slabs; p.width = C / best_slabs; p.cluster = best_cluster;
-    while ((1 << p.log_cluster) < p.cluster) ++p.log_cluster;
-    p.columns = p.width / V;
-    p.threads = p.columns > 256 ? 512 : 256;
-    p.rows = p.threads / p.columns;
-    const int active = p.rows * p.columns, slab_groups = p.width / p.per_group;
-    const long long rounds = ((P + p.cluster - 1) / p.cluster + p.rows - 1) / p.rows;
-    const size_t rest = (size_t)p.threads * V * 4 + (size_t)(4 * slab_groups + (maps > 1 ? 4 * p.width : 0)) * 4;
-    const long long round_bytes = (long long)active * V * held;
-    const long long fit = (long long)(kMaxSmem - 1024 - rest) / round_bytes;
-    p.cached = (int)(rounds < fit ? rounds : fit);
-    p.smem = (size_t)p.cached * round_bytes + rest;
-    p.blocks = B * p.slabs * p.cluster;
-    *out = p;
+    const long long chunks = (P + (long long)s.rows * s.rounds - 1) / ((long long)s.rows * s.rounds);
+    if (B > 0x7fffffffLL / chunks) return false;
+    s.chunks = (int)chunks;
+    *out = s;
     return true;
 }
 
-template <auto Kernel>
-cudaError_t launch_clusters(const NormArgs& a, const NormPlan& p, cudaStream_t stream) {
-    static bool ready[64] = {};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev >= 64 || !ready[dev]) {
-        e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+// More than 48 KB of shared memory (thousands of channels) has to be asked for.
+template <typename... Params, typename... Args>
+cudaError_t launch_with(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
-        if (dev < 64) ready[dev] = true;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.blocks);
-    cfg.blockDim = dim3((unsigned)p.threads);
-    cfg.dynamicSmemBytes = p.smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, Kernel, a, p);
+    return launch_chained(kernel, grid, threads, smem, stream, args...);
 }
 
-template <typename T>
-cudaError_t forward_of(const NormArgs& a, const NormPlan& p, int act, cudaStream_t stream) {
-    switch (act) {
-        case SLIDE_ATTN_ACT_SILU: return launch_clusters<norm_forward_kernel<T, SLIDE_ATTN_ACT_SILU>>(a, p, stream);
-        case SLIDE_ATTN_ACT_GELU: return launch_clusters<norm_forward_kernel<T, SLIDE_ATTN_ACT_GELU>>(a, p, stream);
-        default: return launch_clusters<norm_forward_kernel<T, SLIDE_ATTN_ACT_NONE>>(a, p, stream);
+size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
+// A workspace: partial, factors, channels.
+struct NormRoom {
+    size_t factors, channels, bytes;
+    NormRoom(const NormShape& s, long long B, int maps) {
+        const bool once = maps == 1 && s.chunks == 1;
+        factors = once ? 0 : align16((size_t)B * s.groups * s.chunks * sizeof(float2));
+        channels = once ? 0 : factors + align16((size_t)B * 2 * maps * s.C * sizeof(float));
+        bytes = channels + (maps == 1 ? 0 : (size_t)B * s.chunks * 2 * s.C * sizeof(float));
     }
+};
+
+template <int Threads, typename T, int Act>
+cudaError_t forward_as(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
+    const dim3 grid((unsigned)(B * s.chunks));
+    const size_t smem = (size_t)(s.threads * 2 * Vec<T>::pairs + 2 * s.groups) * 4;
+    if (s.chunks == 1) return launch_with(norm_forward_once_kernel<Threads, T, Act>, grid, Threads, smem, stream, a, s);
+    cudaError_t e = launch_with(norm_sums_kernel<Threads, T>, grid, Threads, smem, stream, a, s);
+    if (e == cudaSuccess) e = launch_chained(norm_join_kernel, dim3((unsigned)B), 512, (size_t)s.groups * sizeof(float2), stream, a, s);
+    return e == cudaSuccess ? launch_chained(norm_forward_kernel<Threads, T, Act>, grid, Threads, 0, stream, a, s) : e;
+}
+template <typename T, int Act>
+cudaError_t forward_with(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
+    return s.threads == 512 ? forward_as<512, T, Act>(a, s, B, stream) : forward_as<256, T, Act>(a, s, B, stream);
 }
 template <typename T>
-cudaError_t backward_of(const NormArgs& a, const NormPlan& p, int act, cudaStream_t stream) {
+cudaError_t forward_of(const NormArgs& a, const NormShape& s, long long B, int act, cudaStream_t stream) {
     switch (act) {
-        case SLIDE_ATTN_ACT_SILU: return launch_clusters<norm_backward_kernel<T, SLIDE_ATTN_ACT_SILU>>(a, p, stream);
-        case SLIDE_ATTN_ACT_GELU: return launch_clusters<norm_backward_kernel<T, SLIDE_ATTN_ACT_GELU>>(a, p, stream);
-        default: return launch_clusters<norm_backward_kernel<T, SLIDE_ATTN_ACT_NONE>>(a, p, stream);
+        case SLIDE_ATTN_ACT_SILU: return forward_with<T, SLIDE_ATTN_ACT_SILU>(a, s, B, stream);
+        case SLIDE_ATTN_ACT_GELU: return forward_with<T, SLIDE_ATTN_ACT_GELU>(a, s, B, stream);
+        default: return forward_with<T, SLIDE_ATTN_ACT_NONE>(a, s, B, stream);
+    }
+}
+
+template <int Threads, typename T, int Act>
+cudaError_t backward_as(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
+    const dim3 grid((unsigned)(B * s.chunks));
+    const int red = s.threads * 2 * Vec<T>::pairs;
+    const size_t smem = (size_t)((red > 2 * s.C ? red : 2 * s.C) + 2 * s.C + 2 * s.groups) * 4;
+    cudaError_t e = launch_with(norm_slopes_kernel<Threads, T, Act>, grid, Threads, smem, stream, a, s);
+    if (e == cudaSuccess) e = launch_chained(norm_join_slopes_kernel, dim3((unsigned)B), 512, (size_t)s.groups * sizeof(float2), stream, a, s);
+    return e == cudaSuccess ? launch_chained(norm_backward_kernel<Threads, T, Act>, grid, Threads, 0, stream, a, s) : e;
+}
+template <typename T, int Act>
+cudaError_t backward_with(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
+    return s.threads == 512 ? backward_as<512, T, Act>(a, s, B, stream) : backward_as<256, T, Act>(a, s, B, stream);
+}
+template <typename T>
+cudaError_t backward_of(const NormArgs& a, const NormShape& s, long long B, int act, cudaStream_t stream) {
+    switch (act) {
+        case SLIDE_ATTN_ACT_SILU: return backward_with<T, SLIDE_ATTN_ACT_SILU>(a, s, B, stream);
+        case SLIDE_ATTN_ACT_GELU: return backward_with<T, SLIDE_ATTN_ACT_GELU>(a, s, B, stream);
+        default: return backward_with<T, SLIDE_ATTN_ACT_NONE>(a, s, B, stream);
     }
 }
 
 }  // namespace
 
-// One answer for forward and backward: a slab of the width that both settle for has to fit a block, and the grid its first dimension.
-bool group_norm_supports(long long B, long long P, int C, int groups, slide_attn_dtype dtype) {
-    NormPlan p;
-    const int size = dtype == SLIDE_ATTN_BF16 ? 2 : 4;
-    return make_plan(B, P, C, groups, size, 1, kMostSms, &p) && make_plan(B, P, C, groups, size, 2, kMostSms, &p);
+bool group_norm_workspace(long long B, long long P, int C, int groups, slide_attn_dtype dtype, int maps, size_t* bytes) {
+    NormShape s;
+    if (!make_shape(B, P, C, groups, dtype == SLIDE_ATTN_BF16 ? 2 : 4, maps, &s)) return false;
+    *bytes = NormRoom(s, B, maps).bytes;
+    return true;
 }
 
 cudaError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, long long B, long long P, int C, int groups, float eps,
-                                      slide_attn_activation act, slide_attn_dtype dtype, void* y, float* mean, float* rstd, int num_sms,
+                                      slide_attn_activation act, slide_attn_dtype dtype, void* y, float* mean, float* rstd, void* workspace,
                                       cudaStream_t stream) {
-    NormPlan p;
-    if (!make_plan(B, P, C, groups, dtype == SLIDE_ATTN_BF16 ? 2 : 4, 1, num_sms, &p)) return cudaErrorInvalidValue;
-    NormArgs a = {x, gamma, beta, nullptr, y, mean, rstd, nullptr, eps};
-    return dtype == SLIDE_ATTN_BF16 ? forward_of<__nv_bfloat16>(a, p, act, stream) : forward_of<float>(a, p, act, stream);
+    NormShape s;
+    if (!make_shape(B, P, C, groups, dtype == SLIDE_ATTN_BF16 ? 2 : 4, 1, &s)) return cudaErrorInvalidValue;
+    const NormRoom room(s, B, 1);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    const NormArgs a = {x, gamma, beta, nullptr, y, mean, rstd, reinterpret_cast<float2*>(ws), reinterpret_cast<float*>(ws + room.factors), nullptr, eps};
+    return dtype == SLIDE_ATTN_BF16 ? forward_of<__nv_bfloat16>(a, s, B, act, stream) : forward_of<float>(a, s, B, act, stream);
 }
 
 cudaError_t launch_group_norm_backward(const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, const void* dy,
                                        long long B, long long P, int C, int groups, slide_attn_activation act, slide_attn_dtype dtype, void* dx,
-                                       float* dgamma, float* dbeta, float* sums, int num_sms, cudaStream_t stream) {
-    NormPlan p;
-    if (!make_plan(B, P, C, groups, dtype == SLIDE_ATTN_BF16 ? 2 : 4, 2, num_sms, &p)) return cudaErrorInvalidValue;
-    NormArgs a = {x, gamma, beta, dy, dx, const_cast<float*>(mean), const_cast<float*>(rstd), dgamma ? sums : nullptr, 0.0f};
-    cudaError_t e = dtype == SLIDE_ATTN_BF16 ? backward_of<__nv_bfloat16>(a, p, act, stream) : backward_of<float>(a, p, act, stream);
+                                       float* dgamma, float* dbeta, void* workspace, cudaStream_t stream) {
+    NormShape s;
+    if (!make_shape(B, P, C, groups, dtype == SLIDE_ATTN_BF16 ? 2 : 4, 2, &s)) return cudaErrorInvalidValue;
+    const NormRoom room(s, B, 2);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    float* channels = dgamma ? reinterpret_cast<float*>(ws + room.channels) : nullptr;
+    const NormArgs a = {x, gamma, beta, dy, dx, const_cast<float*>(mean), const_cast<float*>(rstd), reinterpret_cast<float2*>(ws),
+                        reinterpret_cast<float*>(ws + room.factors), channels, 0.0f};
+    cudaError_t e = dtype == SLIDE_ATTN_BF16 ? backward_of<__nv_bfloat16>(a, s, B, act, stream) : backward_of<float>(a, s, B, act, stream);
     if (e != cudaSuccess || !dgamma) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((C + 31) / 32), 2);
-    cfg.blockDim = dim3(32, 8);
+    cfg.gridDim = dim3((unsigned)((2 * C + 31) / 32));
+    cfg.blockDim = dim3(32, 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, norm_weight_kernel, (const float*)sums, B, C, dgamma, dbeta);
+    return cudaLaunchKernelEx(&cfg, norm_weight_kernel, (const float*)channels, B * s.chunks, C, dgamma, dbeta);
 }
 
 }  // namespace slide_attn

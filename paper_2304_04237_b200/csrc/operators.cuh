@@ -4,14 +4,14 @@
 
 namespace slide_attn {
 
-// Group norm over [B][P][C].  sums: 2 B C floats for the weights' gradients (unused without them).
-bool group_norm_supports(long long B, long long P, int C, int groups, slide_attn_dtype dtype);
+// Group norm over [B][P][C].  group_norm_workspace: of the forward (maps = 1) or the backward (2); false where the shape is not supported.
+bool group_norm_workspace(long long B, long long P, int C, int groups, slide_attn_dtype dtype, int maps, size_t* bytes);
 cudaError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, long long B, long long P, int C, int groups, float eps,
-                                      slide_attn_activation act, slide_attn_dtype dtype, void* y, float* mean, float* rstd, int num_sms,
+                                      slide_attn_activation act, slide_attn_dtype dtype, void* y, float* mean, float* rstd, void* workspace,
                                       cudaStream_t stream);
 cudaError_t launch_group_norm_backward(const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, const void* dy,
                                        long long B, long long P, int C, int groups, slide_attn_activation act, slide_attn_dtype dtype, void* dx,
-                                       float* dgamma, float* dbeta, float* sums, int num_sms, cudaStream_t stream);
+                                       float* dgamma, float* dbeta, void* workspace, cudaStream_t stream);
 
 bool dropout_supports(long long images, long long per_image, bool whole_images);
 cudaError_t launch_dropout(const void* x, const void* residual, void* y, long long images, long long per_image, double p, bool whole_images,

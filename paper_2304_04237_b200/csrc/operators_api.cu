@@ -44,12 +44,12 @@ slide_attn_status launched(cudaError_t e) {
 
 bool known_dtype(slide_attn_dtype t) { return t == SLIDE_ATTN_F32 || t == SLIDE_ATTN_BF16; }
 
-slide_attn_status norm_shape(int B, int H, int W, int C, int groups, slide_attn_dtype dtype) {
+slide_attn_status norm_shape(int B, int H, int W, int C, int groups, slide_attn_dtype dtype, bool backward, size_t* workspace) {
     if (B < 1 || H < 1 || W < 1 || C < 1 || groups < 1 || !known_dtype(dtype)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (C % groups != 0 || C % 8 != 0) return SLIDE_ATTN_ERR_UNSUPPORTED;
     const long long P = (long long)H * W;
-    if (P > (1LL << 30) || B > (1LL << 40) / P / C || !group_norm_supports(B, P, C, groups, dtype)) return SLIDE_ATTN_ERR_UNSUPPORTED;
-    return SLIDE_ATTN_OK;
+    if (P > (1LL << 30) || B > (1LL << 40) / P / C) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    return group_norm_workspace(B, P, C, groups, dtype, backward ? 2 : 1, workspace) ? SLIDE_ATTN_OK : SLIDE_ATTN_ERR_UNSUPPORTED;
 }
 
 bool known_activation(slide_attn_activation a) { return a == SLIDE_ATTN_ACT_NONE || a == SLIDE_ATTN_ACT_SILU || a == SLIDE_ATTN_ACT_GELU; }
@@ -79,28 +79,32 @@ slide_attn_status with_top(sparse::Geometry* g, int top) {
 
 extern "C" {
 
-slide_attn_status slide_attn_group_norm_workspace(int B, int H, int W, int C, int groups, slide_attn_dtype dtype, size_t* bytes)
+slide_attn_status slide_attn_group_norm_workspace(int B, int H, int W, int C, int groups, slide_attn_dtype dtype, int backward, size_t* bytes)
 {
     if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
-    const slide_attn_status st = norm_shape(B, H, W, C, groups, dtype);
-    if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(float) * (size_t)B * C;
+    size_t need = 0;
+    const slide_attn_status st = norm_shape(B, H, W, C, groups, dtype, backward != 0, &need);
+    if (st == SLIDE_ATTN_OK) *bytes = need;
     return st;
 }
 
 slide_attn_status slide_attn_group_norm_forward(const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, int B, int H,
                                                 int W, int C, int groups, float eps, slide_attn_activation act, slide_attn_dtype dtype,
-                                                void* cuda_stream)
+                                                void* workspace, size_t workspace_bytes, void* cuda_stream)
 {
-    if (any_null(x, static_cast<const void*>(y), static_cast<const void*>(mean), static_cast<const void*>(rstd))) return SLIDE_ATTN_ERR_INVALID_ARG;
-    slide_attn_status st = norm_shape(B, H, W, C, groups, dtype);
+    const void *vy = y, *vm = mean, *vr = rstd, *vw = workspace;
+    if (any_null(x, vy, vm, vr)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    size_t need = 0;
+    slide_attn_status st = norm_shape(B, H, W, C, groups, dtype, false, &need);
     if (st != SLIDE_ATTN_OK) return st;
-    if (!known_activation(act) || !(eps >= 0.0f) || isinf(eps)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (any_misaligned(x, gamma, beta, y, mean, rstd)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    if (y == x || among(mean, x, y, gamma, beta, rstd) || among(rstd, x, y, gamma, beta) || among(y, gamma, beta)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (!known_activation(act) || !(eps >= 0.0f) || isinf(eps) || workspace_bytes < need || (need && !vw)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(x, gamma, beta, vy, vm, vr, vw)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    if (among(vy, x, gamma, beta, vm, vr, vw) || among(vm, x, gamma, beta, vr, vw) || among(vr, x, gamma, beta, vw) || (vw && among(vw, x, gamma, beta)))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
-    return launched(launch_group_norm_forward(x, gamma, beta, B, (long long)H * W, C, groups, eps, act, dtype, y, mean, rstd, sms,
+    return launched(launch_group_norm_forward(x, gamma, beta, B, (long long)H * W, C, groups, eps, act, dtype, y, mean, rstd, workspace,
                                               static_cast<cudaStream_t>(cuda_stream)));
 }
 
@@ -109,22 +113,22 @@ slide_attn_status slide_attn_group_norm_backward(const void* x, const float* gam
                                                  slide_attn_activation act, slide_attn_dtype dtype, void* workspace, size_t workspace_bytes,
                                                  void* cuda_stream)
 {
-    if (any_null(x, static_cast<const void*>(mean), static_cast<const void*>(rstd), dy, static_cast<const void*>(dx))) return SLIDE_ATTN_ERR_INVALID_ARG;
+    const void *vx = dx, *vg = dgamma, *vb = dbeta, *vw = workspace;
+    if (any_null(x, static_cast<const void*>(mean), static_cast<const void*>(rstd), dy, vx, vw)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if ((dgamma == nullptr) != (dbeta == nullptr)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    slide_attn_status st = norm_shape(B, H, W, C, groups, dtype);
+    size_t need = 0;
+    slide_attn_status st = norm_shape(B, H, W, C, groups, dtype, true, &need);
     if (st != SLIDE_ATTN_OK) return st;
-    if (!known_activation(act)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (dgamma && (!workspace || workspace_bytes < 2 * sizeof(float) * (size_t)B * C)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (any_misaligned(x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta) || (dgamma && misaligned(workspace))) return SLIDE_ATTN_ERR_ALIGNMENT;
-    if (among(dx, x, dy, gamma, beta, mean, rstd)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (dgamma && (among(dgamma, dbeta, x, dy, dx, gamma, beta, mean, rstd, workspace) || among(dbeta, x, dy, dx, gamma, beta, mean, rstd, workspace) ||
-                   among(workspace, x, dy, dx, gamma, beta, mean, rstd)))
-        return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (!known_activation(act) || workspace_bytes < need) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(x, gamma, beta, mean, rstd, dy, vx, vg, vb, vw)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    for (const void* o : {vx, vg, vb, vw})
+        if (o && among(o, x, dy, gamma, beta, mean, rstd)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (among(vx, vg, vb, vw) || (vg && among(vg, vb, vw)) || vb == vw) return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
     return launched(launch_group_norm_backward(x, gamma, beta, mean, rstd, dy, B, (long long)H * W, C, groups, act, dtype, dx, dgamma, dbeta,
-                                               static_cast<float*>(workspace), sms, static_cast<cudaStream_t>(cuda_stream)));
+                                               workspace, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 namespace {

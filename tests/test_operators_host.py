@@ -18,8 +18,9 @@ def lib():
     return binding.load()
 
 
-def norm(lib, x=A, gamma=B2, beta=C2, y=D2, mean=E2, rstd=F2, B=2, H=4, W=4, C=32, groups=4, eps=1e-5, act=0, dtype=0):
-    return lib.slide_attn_group_norm_forward(x, gamma, beta, y, mean, rstd, B, H, W, C, groups, eps, act, dtype, None)
+def norm(lib, x=A, gamma=B2, beta=C2, y=D2, mean=E2, rstd=F2, B=2, H=40, W=40, C=32, groups=4, eps=1e-5, act=0, dtype=0,
+         ws=G2, size=BIG):
+    return lib.slide_attn_group_norm_forward(x, gamma, beta, y, mean, rstd, B, H, W, C, groups, eps, act, dtype, ws, size, None)
 
 
 def norm_back(lib, x=A, gamma=B2, beta=C2, mean=D2, rstd=E2, dy=F2, dx=G2, dgamma=H2, dbeta=I2, B=2, H=4, W=4, C=32, groups=4, act=0, dtype=0, ws=J2,
@@ -53,12 +54,13 @@ SPARSE = [(c, ARG) for c in MAP + [dict(heads=0), dict(bh=0), dict(bw=-4), dict(
 
 CASES = {
     norm: [(c, ARG) for c in MAP + [dict(C=0), dict(groups=0), dict(x=None), dict(y=None), dict(mean=None), dict(rstd=None), dict(eps=-1.0), dict(eps=NAN),
-                                    dict(eps=INF), dict(act=3), dict(act=-1), dict(y=A), dict(y=B2), dict(mean=A), dict(mean=F2), dict(rstd=D2)]] +
+                                    dict(eps=INF), dict(act=3), dict(act=-1), dict(y=A), dict(y=B2), dict(mean=A), dict(mean=F2), dict(rstd=D2), dict(ws=None), dict(size=8),
+                                    dict(ws=A), dict(ws=D2)]] +
           [(dict(C=36), UNS), (dict(groups=3), UNS), (dict(C=20, groups=5), UNS), (dict(C=8192, groups=1), UNS), (dict(C=4096, groups=1), UNS),
            (dict(C=8192, groups=1, dtype=1), UNS), (dict(H=1 << 16, W=1 << 16), UNS), (dict(B=1 << 30, H=1 << 10, W=1 << 10), UNS),
-           (dict(x=A + 8), ALIGN), (dict(gamma=B2 + 4), ALIGN), (dict(y=D2 + 2), ALIGN), (dict(mean=E2 + 4), ALIGN)],
+           (dict(x=A + 8), ALIGN), (dict(gamma=B2 + 4), ALIGN), (dict(y=D2 + 2), ALIGN), (dict(mean=E2 + 4), ALIGN), (dict(ws=G2 + 8), ALIGN)],
     norm_back: [(c, ARG) for c in MAP + [dict(x=None), dict(mean=None), dict(rstd=None), dict(dy=None), dict(dx=None), dict(dgamma=None), dict(dbeta=None),
-                                         dict(ws=None), dict(size=2 * 2 * 32 * 4 - 1), dict(act=7), dict(dx=A), dict(dx=F2), dict(dgamma=I2),
+                                         dict(ws=None), dict(size=2 * 4 * 8 + 2 * 4 * 32 * 4 + 2 * 2 * 32 * 4 - 1), dict(act=7), dict(dx=A), dict(dx=F2), dict(dgamma=I2),
                                          dict(dgamma=G2), dict(ws=A), dict(ws=I2)]] +
                [(dict(groups=5), UNS), (dict(C=12, groups=1), UNS), (dict(ws=J2 + 4), ALIGN), (dict(dx=G2 + 8), ALIGN), (dict(dbeta=I2 + 4), ALIGN)],
     drop: [(c, ARG) for c in [dict(x=None), dict(y=None), dict(rng=None), dict(images=0), dict(per_image=0), dict(dtype=5), dict(unit=2), dict(p=-0.1),
@@ -87,18 +89,20 @@ def test_accepted_arguments_reach_the_device_check(lib):
         pytest.skip("a device is present")
     for call in CASES:
         assert call(lib) in (sa.ERR_CUDA, sa.ERR_ARCH)
+    assert norm(lib, H=4, W=4, ws=None, size=0) in (sa.ERR_CUDA, sa.ERR_ARCH)
     assert norm(lib, gamma=None, beta=None) in (sa.ERR_CUDA, sa.ERR_ARCH)
-    assert norm_back(lib, dgamma=None, dbeta=None, ws=None, size=0) in (sa.ERR_CUDA, sa.ERR_ARCH)
+    assert norm_back(lib, dgamma=None, dbeta=None) in (sa.ERR_CUDA, sa.ERR_ARCH)
     for same in (dict(y=A), dict(y=B2), dict(residual=None, y=A)):
         assert drop(lib, **same) in (sa.ERR_CUDA, sa.ERR_ARCH)
 
 
 def test_workspace_sizes(lib):
     n = ctypes.c_size_t()
-    assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 6, 1, ctypes.byref(n)) == sa.OK and n.value == 2 * 4 * 3 * 48
+    assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 6, 1, 0, ctypes.byref(n)) == sa.OK and n.value == 0
+    assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 6, 1, 1, ctypes.byref(n)) == sa.OK and n.value == 8 * 3 * 6 + 4 * 4 * 3 * 48 + 2 * 4 * 3 * 48
     assert lib.slide_attn_select_workspace(3, 9, 7, 2, 16, 4, 4, ctypes.byref(n)) == sa.OK and n.value == 2 * 8 * 3 * 2 * 6 * 16
     assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, ctypes.byref(n)) == sa.OK and n.value == 2 * 4 * 3 * 63 * 2
-    assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 7, 1, ctypes.byref(n)) == sa.ERR_UNSUPPORTED
+    assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 7, 1, 0, ctypes.byref(n)) == sa.ERR_UNSUPPORTED
     assert lib.slide_attn_select_workspace(3, 9, 7, 2, 8, 4, 4, ctypes.byref(n)) == sa.ERR_UNSUPPORTED
     assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, None) == sa.ERR_INVALID_ARG
 
