@@ -18,7 +18,7 @@ namespace slide_attn {
 
 namespace {
 
-constexpr int kTogether = 4;           // 16-byte pieces that a thread has in flight (backward: half of them of each map)
+constexpr int kTogether = 4;           // 16-byte pieces that a thread works on together (backward: half of them of each map)
 constexpr int kForwardCtas = 4, kBackwardCtas = 3;     // of 256 threads on an SM, as registers allow
 constexpr int kPair = kTogether / 2;
 constexpr int kOnce = 8;               // rounds of an image that one CTA keeps
@@ -216,6 +216,49 @@ template <typename T> __device__ __forceinline__ Place find_place(const NormShap
     return p;
 }
 
+// A thread's pieces of one or two maps on their way through shared memory, a batch of `Batch` rounds at a time, kRing - 1 batches ahead of the
+// arithmetic.  A thread reads only what it copied itself, so no barrier is needed; a batch's room is filled again one batch after it was read.
+template <int Threads, int Maps, int Batch> struct Stream {
+    static constexpr int kRing = 3, kPieces = Maps * Batch;
+    static constexpr size_t kSmem = (size_t)Threads * kRing * kPieces * 16;
+    unsigned char* ring;
+    const unsigned char *x, *g;
+    size_t step;
+    int left, to, from;
+    __device__ __forceinline__ Stream(unsigned char* smem, const unsigned char* src_x, const unsigned char* src_g, const Place& at)
+        : ring(smem + threadIdx.x * 16), x(src_x), g(src_g), step(at.step), left(at.mine), to(0), from(0) {
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) send();
+    }
+    __device__ __forceinline__ unsigned char* piece(int batch, int i) const { return ring + (batch * kPieces + i) * (Threads * 16); }
+    __device__ __forceinline__ void send() {
+#pragma unroll
+        for (int i = 0; i < Batch; ++i)
+            if (i < left) {
+                copy16(smem_u32(piece(to, i * Maps)), x);
+                x += step;
+                if constexpr (Maps > 1) {
+                    copy16(smem_u32(piece(to, i * Maps + 1)), g);
+                    g += step;
+                }
+            }
+        left -= Batch;
+        to = to == kRing - 1 ? 0 : to + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // The next batch has arrived: its pieces, those of a round side by side.
+    __device__ __forceinline__ void next(uint4 (&raw)[kPieces]) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) raw[i] = *reinterpret_cast<const uint4*>(piece(from, i));
+        from = from == kRing - 1 ? 0 : from + 1;
+        send();
+    }
+    static __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    }
+};
+
 // What the passes multiply by, V channels of it.  Forward: less the mean, and rstd gamma.  Backward, with c = x - mean: z = c (rstd gamma) + beta,
 // dx = dz (rstd gamma) + (c quad + shift), quad = -rstd^2 mean(du u), shift = -rstd mean(du).
 template <int V> __device__ __forceinline__ void get_factors(const float* factors, int C, int which, int column, pair (&v)[V / 2]) {
@@ -293,21 +336,20 @@ __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_su
 {
     constexpr int V = 2 * Vec<T>::pairs;
     extern __shared__ __align__(16) unsigned char smem[];
-    float* red = reinterpret_cast<float*>(smem);
+    using Maps = Stream<Threads, 1, kTogether>;
+    float* red = reinterpret_cast<float*>(smem + Maps::kSmem);
     float* means = red + s.threads * V;
     float* squares = means + s.groups;
     const Place at = find_place<T>(s);
-    const unsigned char* src = static_cast<const unsigned char*>(a.x) + at.start;
     grid_dependency_wait();
+    grid_launch_dependents();
+    Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, nullptr, at);
     Moments<T> m;
 #pragma unroll 1
     for (int done = 0; done < at.mine; done += kTogether) {
-        const int count = min(at.mine - done, kTogether);
         uint4 raw[kTogether];
-#pragma unroll
-        for (int i = 0; i < kTogether; ++i)
-            if (i < count) { raw[i] = *reinterpret_cast<const uint4*>(src); src += at.step; }
-        m.add(raw, count);
+        maps.next(raw);
+        m.add(raw, min(at.mine - done, kTogether));
     }
     int group[V];
     find_groups<V>(s.per_group, at.column, group);
@@ -323,6 +365,7 @@ __global__ void __launch_bounds__(512) norm_join_kernel(const NormArgs a, const 
     extern __shared__ __align__(16) unsigned char smem[];
     float2* stats = reinterpret_cast<float2*>(smem);
     grid_dependency_wait();
+    grid_launch_dependents();
     const size_t b = blockIdx.x;
     const int lane = threadIdx.x % 32;
     const float per = (float)s.per_group, n = (float)s.P * per;
@@ -372,11 +415,13 @@ template <int Threads, typename T, int Act>
 __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_forward_kernel(const NormArgs a, const NormShape s)
 {
     constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    extern __shared__ __align__(16) unsigned char smem[];
+    using Maps = Stream<Threads, 1, kTogether>;
     const Place at = find_place<T>(s);
-    const unsigned char* src = static_cast<const unsigned char*>(a.x) + at.start;
     unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
     grid_dependency_wait();
     if (!at.active) return;
+    Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, nullptr, at);
     pair scale[Q], beta[Q], mean[Q];
     const float* factors = a.factors + (size_t)at.image * 2 * s.C;
     get_factors<V>(factors, s.C, 0, at.column, mean);
@@ -385,13 +430,10 @@ __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_fo
 #pragma unroll 1
     for (int done = 0; done < at.mine; done += kTogether) {
         uint4 raw[kTogether];
-#pragma unroll
-        for (int i = 0; i < kTogether; ++i)
-            if (done + i < at.mine) raw[i] = *reinterpret_cast<const uint4*>(src + i * at.step);
+        maps.next(raw);
 #pragma unroll
         for (int i = 0; i < kTogether; ++i)
             if (done + i < at.mine) *reinterpret_cast<uint4*>(dst + i * at.step) = normalised<T, Act>(raw[i], mean, scale, beta);
-        src += kTogether * at.step;
         dst += kTogether * at.step;
     }
 }
@@ -446,13 +488,14 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
 {
     constexpr int Q = Vec<T>::pairs, V = 2 * Q;
     extern __shared__ __align__(16) unsigned char smem[];
-    float* red = reinterpret_cast<float*>(smem);                    // [row][channel]; later two values a channel
+    using Maps = Stream<Threads, 2, kPair>;
+    float* red = reinterpret_cast<float*>(smem + Maps::kSmem);      // [row][channel]; later two values a channel
     float* channel = red + max(s.threads * V, 2 * s.C);             // sums of dz, then of dz u
     float* local = channel + 2 * s.C;                               // the groups'
     const Place at = find_place<T>(s);
-    const unsigned char* src_x = static_cast<const unsigned char*>(a.x) + at.start;
-    const unsigned char* src_g = static_cast<const unsigned char*>(a.dy) + at.start;
     grid_dependency_wait();
+    grid_launch_dependents();
+    Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, static_cast<const unsigned char*>(a.dy) + at.start, at);
     pair mean[Q], scale[Q], beta[Q], s1[Q] = {}, s2[Q] = {};
     const float* means = a.mean + (size_t)at.image * s.groups;
     const float* rstds = a.rstd + (size_t)at.image * s.groups;
@@ -469,19 +512,14 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
     }
 #pragma unroll 1
     for (int done = 0; done < at.mine; done += kPair) {
-        uint4 x[kPair], g[kPair];
-#pragma unroll
-        for (int i = 0; i < kPair; ++i)
-            if (done + i < at.mine) {
-                x[i] = *reinterpret_cast<const uint4*>(src_x + i * at.step);
-                g[i] = *reinterpret_cast<const uint4*>(src_g + i * at.step);
-            }
+        uint4 raw[2 * kPair];
+        maps.next(raw);
 #pragma unroll
         for (int i = 0; i < kPair; ++i)
             if (done + i < at.mine) {
                 pair c[Q], dz[Q];
-                Vec<T>::get(x[i], c);
-                Vec<T>::get(g[i], dz);
+                Vec<T>::get(raw[2 * i], c);
+                Vec<T>::get(raw[2 * i + 1], dz);
 #pragma unroll
                 for (int e = 0; e < Q; ++e) {
                     c[e] = add2(c[e], mean[e]);
@@ -490,8 +528,6 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
                     s2[e] = fma2(dz[e], c[e], s2[e]);
                 }
             }
-        src_x += kPair * at.step;
-        src_g += kPair * at.step;
     }
     const int lanes = lanes_for(s.C);
     if (at.active) leave<V>(red, s1);
@@ -519,6 +555,7 @@ __global__ void __launch_bounds__(512) norm_join_slopes_kernel(const NormArgs a,
     extern __shared__ __align__(16) unsigned char smem[];
     float2* stats = reinterpret_cast<float2*>(smem);                // quad and shift
     grid_dependency_wait();
+    grid_launch_dependents();
     const size_t b = blockIdx.x;
     const int lane = threadIdx.x % 32;
     const float inv = 1.0f / ((float)s.P * (float)s.per_group);
@@ -549,12 +586,14 @@ template <int Threads, typename T, int Act>
 __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_backward_kernel(const NormArgs a, const NormShape s)
 {
     constexpr int Q = Vec<T>::pairs, V = 2 * Q;
+    extern __shared__ __align__(16) unsigned char smem[];
+    using Maps = Stream<Threads, 2, kPair>;
     const Place at = find_place<T>(s);
-    const unsigned char* src_x = static_cast<const unsigned char*>(a.x) + at.start;
-    const unsigned char* src_g = static_cast<const unsigned char*>(a.dy) + at.start;
     unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
     grid_dependency_wait();
+    if (a.channels) grid_launch_dependents();          // the weights' sums come next
     if (!at.active) return;
+    Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, static_cast<const unsigned char*>(a.dy) + at.start, at);
     pair mean[Q], scale[Q], beta[Q], quad[Q], shift[Q];
     const float* factors = a.factors + (size_t)at.image * 4 * s.C;
     get_factors<V>(factors, s.C, 0, at.column, mean);
@@ -564,19 +603,14 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_b
     get_weights<V>(a.beta, at.column * V, 0.0f, beta);
 #pragma unroll 1
     for (int done = 0; done < at.mine; done += kPair) {
-        uint4 x[kPair], g[kPair];
-#pragma unroll
-        for (int i = 0; i < kPair; ++i)
-            if (done + i < at.mine) {
-                x[i] = *reinterpret_cast<const uint4*>(src_x + i * at.step);
-                g[i] = *reinterpret_cast<const uint4*>(src_g + i * at.step);
-            }
+        uint4 raw[2 * kPair];
+        maps.next(raw);
 #pragma unroll
         for (int i = 0; i < kPair; ++i)
             if (done + i < at.mine) {
                 pair c[Q], dz[Q];
-                Vec<T>::get(x[i], c);
-                Vec<T>::get(g[i], dz);
+                Vec<T>::get(raw[2 * i], c);
+                Vec<T>::get(raw[2 * i + 1], dz);
 #pragma unroll
                 for (int e = 0; e < Q; ++e) {
                     c[e] = add2(c[e], mean[e]);
@@ -585,8 +619,6 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_b
                 }
                 *reinterpret_cast<uint4*>(dst + i * at.step) = Vec<T>::put(dz);
             }
-        src_x += kPair * at.step;
-        src_g += kPair * at.step;
         dst += kPair * at.step;
     }
 }
@@ -662,11 +694,12 @@ struct NormRoom {
 template <int Threads, typename T, int Act>
 cudaError_t forward_as(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
     const dim3 grid((unsigned)(B * s.chunks));
+    constexpr size_t ring = Stream<Threads, 1, kTogether>::kSmem;
     const size_t smem = (size_t)(s.threads * 2 * Vec<T>::pairs + 2 * s.groups) * 4;
     if (s.chunks == 1) return launch_with(norm_forward_once_kernel<Threads, T, Act>, grid, Threads, smem, stream, a, s);
-    cudaError_t e = launch_with(norm_sums_kernel<Threads, T>, grid, Threads, smem, stream, a, s);
+    cudaError_t e = launch_with(norm_sums_kernel<Threads, T>, grid, Threads, ring + smem, stream, a, s);
     if (e == cudaSuccess) e = launch_chained(norm_join_kernel, dim3((unsigned)B), 512, (size_t)s.groups * sizeof(float2), stream, a, s);
-    return e == cudaSuccess ? launch_chained(norm_forward_kernel<Threads, T, Act>, grid, Threads, 0, stream, a, s) : e;
+    return e == cudaSuccess ? launch_with(norm_forward_kernel<Threads, T, Act>, grid, Threads, ring, stream, a, s) : e;
 }
 template <typename T, int Act>
 cudaError_t forward_with(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
@@ -684,11 +717,12 @@ cudaError_t forward_of(const NormArgs& a, const NormShape& s, long long B, int a
 template <int Threads, typename T, int Act>
 cudaError_t backward_as(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
     const dim3 grid((unsigned)(B * s.chunks));
+    constexpr size_t ring = Stream<Threads, 2, kPair>::kSmem;
     const int red = s.threads * 2 * Vec<T>::pairs;
     const size_t smem = (size_t)((red > 2 * s.C ? red : 2 * s.C) + 2 * s.C + 2 * s.groups) * 4;
-    cudaError_t e = launch_with(norm_slopes_kernel<Threads, T, Act>, grid, Threads, smem, stream, a, s);
+    cudaError_t e = launch_with(norm_slopes_kernel<Threads, T, Act>, grid, Threads, ring + smem, stream, a, s);
     if (e == cudaSuccess) e = launch_chained(norm_join_slopes_kernel, dim3((unsigned)B), 512, (size_t)s.groups * sizeof(float2), stream, a, s);
-    return e == cudaSuccess ? launch_chained(norm_backward_kernel<Threads, T, Act>, grid, Threads, 0, stream, a, s) : e;
+    return e == cudaSuccess ? launch_with(norm_backward_kernel<Threads, T, Act>, grid, Threads, ring, stream, a, s) : e;
 }
 template <typename T, int Act>
 cudaError_t backward_with(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
