@@ -4,8 +4,10 @@
 // SC11) at counter (e / 4, offset) under the key (seed) is at least floor(p 2^32), so the mask is never stored: the backward
 // computes it again.  In units of images the word of image b decides for all of its elements.
 //
-// Bound by memory (3 maps forward, 2 backward) for fp32; a thread takes four words, ten rounds of two 32 x 32 -> 64 bit products, for
-// four elements.  The products are fp32, and the sum is rounded to the storage type once.
+// fp32 is bound by memory (3 maps forward, 2 backward).  bf16 is bound by the generator's integer instructions, ten products of 32 x 32 -> 64
+// bits and ten exclusive ors for two elements, on pipes of half rate: 64 x 56 x 56 x 96 takes 39.5 us for
+// forward and backward, the memory alone 29.5.
+// The products with the scale are fp32, and the sum is rounded to the storage type once.
 #include "operators.cuh"
 
 namespace slide_attn {
@@ -21,7 +23,7 @@ struct DropArgs {
     long long per_image;
     float scale;
     unsigned threshold;
-    int all;                        // p = 1: nothing is kept
+    int none;                       // images: p = 1, nothing is kept
 };
 
 struct Key {
@@ -81,11 +83,17 @@ template <> struct Pack<__nv_bfloat16> {
 
 constexpr int kThreads = 256, kEach = 4;         // 16-byte pieces a thread takes
 
-// The value of a dropped element is selected away, not multiplied by zero: an infinity or a NaN there does not reach the sum.
-__device__ __forceinline__ float combine(float x, float residual, bool kept, float scale) { return kept ? fmaf(x, scale, residual) : residual; }
+// The value of a dropped element is not added, and not multiplied by zero either: an infinity or a NaN there does not reach the sum.  (A
+// predicated instruction; a choice between two results costs one more.)
+__device__ __forceinline__ void add_if_kept(float& sum, unsigned word, unsigned threshold, float x, float scale) {
+    asm("{\n\t.reg .pred p;\n\t"
+        "setp.ge.u32 p, %1, %2;\n\t"
+        "@p fma.rn.f32 %0, %3, %4, %0;\n\t}"
+        : "+f"(sum) : "r"(word), "r"(threshold), "f"(x), "f"(scale));
+}
 
 template <typename T, bool Residual>
-__global__ void __launch_bounds__(kThreads) drop_elements_kernel(const DropArgs a)
+__global__ void __launch_bounds__(kThreads, 4) drop_elements_kernel(const DropArgs a)
 {
     constexpr int V = Pack<T>::n;
     grid_dependency_wait();
@@ -115,15 +123,16 @@ __global__ void __launch_bounds__(kThreads) drop_elements_kernel(const DropArgs 
             const unsigned word[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                xv[q * 4 + e] = combine(xv[q * 4 + e], rv[q * 4 + e], word[e] >= a.threshold && !a.all, a.scale);
+                add_if_kept(rv[q * 4 + e], word[e], a.threshold, xv[q * 4 + e], a.scale);
         }
-        static_cast<uint4*>(a.y)[v] = Pack<T>::put(xv);
+        static_cast<uint4*>(a.y)[v] = Pack<T>::put(rv);
     }
     // what no 16-byte piece holds
     if (blockIdx.x == 0 && threadIdx.x < a.n - pieces * V) {
         const long long e = pieces * V + threadIdx.x;
-        const float res = Residual ? to_float(static_cast<const T*>(a.residual)[e]) : 0.0f;
-        static_cast<T*>(a.y)[e] = from_float<T>(combine(to_float(static_cast<const T*>(a.x)[e]), res, word_of(e, key) >= a.threshold && !a.all, a.scale));
+        float sum = Residual ? to_float(static_cast<const T*>(a.residual)[e]) : 0.0f;
+        add_if_kept(sum, word_of(e, key), a.threshold, to_float(static_cast<const T*>(a.x)[e]), a.scale);
+        static_cast<T*>(a.y)[e] = from_float<T>(sum);
     }
 }
 
@@ -138,7 +147,7 @@ __global__ void __launch_bounds__(kThreads) drop_images_kernel(const DropArgs a,
     const long long first = (long long)(blockIdx.x - image * blocks_per_image) * (kThreads * kEach) + threadIdx.x;
     Key key;
     make_key(a.rng, key);
-    const bool kept = word_of(image, key) >= a.threshold && !a.all;
+    const bool kept = word_of(image, key) >= a.threshold && !a.none;
     uint4 x[kEach], r[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -173,10 +182,9 @@ __global__ void __launch_bounds__(kThreads) drop_images_ragged_kernel(const Drop
     Key key;
     make_key(a.rng, key);
     for (long long e = (long long)blockIdx.x * kThreads + threadIdx.x; e < a.n; e += (long long)gridDim.x * kThreads) {
-        const bool kept = word_of(e / a.per_image, key) >= a.threshold && !a.all;
-        const float x = kept ? to_float(static_cast<const T*>(a.x)[e]) : 0.0f;
-        const float res = Residual ? to_float(static_cast<const T*>(a.residual)[e]) : 0.0f;
-        static_cast<T*>(a.y)[e] = from_float<T>(combine(x, res, kept, a.scale));
+        float sum = Residual ? to_float(static_cast<const T*>(a.residual)[e]) : 0.0f;
+        if (!a.none && word_of(e / a.per_image, key) >= a.threshold) sum = fmaf(to_float(static_cast<const T*>(a.x)[e]), a.scale, sum);
+        static_cast<T*>(a.y)[e] = from_float<T>(sum);
     }
 }
 
@@ -184,7 +192,7 @@ template <typename T, bool Residual>
 cudaError_t launch_of(const DropArgs& a, bool images, int num_sms, cudaStream_t stream) {
     constexpr int V = Pack<T>::n;
     constexpr long long kPieces = (long long)kThreads * kEach;
-    if (!images) {
+    if (!images && !a.none) {
         const long long blocks = (a.n / V + kPieces - 1) / kPieces;
         return launch_chained(drop_elements_kernel<T, Residual>, dim3((unsigned)(blocks ? blocks : 1)), kThreads, 0, stream, a);
     }
@@ -210,9 +218,10 @@ cudaError_t launch_dropout(const void* x, const void* residual, void* y, long lo
     DropArgs a = {};
     a.x = x; a.residual = residual; a.y = y; a.rng = rng;
     a.n = images * per_image; a.per_image = per_image;
-    a.all = p >= 1.0;
-    a.threshold = a.all ? 0u : (unsigned)(p * 4294967296.0);
-    a.scale = a.all ? 0.0f : (float)(1.0 / (1.0 - p));
+    a.none = p >= 1.0;                 // no word is enough, which 32 bits cannot say: all is one image that is dropped
+    if (a.none) a.per_image = a.n;
+    a.threshold = a.none ? 0u : (unsigned)(p * 4294967296.0);
+    a.scale = a.none ? 0.0f : (float)(1.0 / (1.0 - p));
     if (dtype == SLIDE_ATTN_BF16)
         return residual ? launch_of<__nv_bfloat16, true>(a, whole_images, num_sms, stream) : launch_of<__nv_bfloat16, false>(a, whole_images, num_sms, stream);
     return residual ? launch_of<float, true>(a, whole_images, num_sms, stream) : launch_of<float, false>(a, whole_images, num_sms, stream);
