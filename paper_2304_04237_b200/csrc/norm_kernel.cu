@@ -342,7 +342,6 @@ __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_su
     float* squares = means + s.groups;
     const Place at = find_place<T>(s);
     grid_dependency_wait();
-    grid_launch_dependents();
     Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, nullptr, at);
     Moments<T> m;
 #pragma unroll 1
@@ -494,7 +493,6 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
     float* local = channel + 2 * s.C;                               // the groups'
     const Place at = find_place<T>(s);
     grid_dependency_wait();
-    grid_launch_dependents();
     Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, static_cast<const unsigned char*>(a.dy) + at.start, at);
     pair mean[Q], scale[Q], beta[Q], s1[Q] = {}, s2[Q] = {};
     const float* means = a.mean + (size_t)at.image * s.groups;

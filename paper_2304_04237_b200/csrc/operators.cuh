@@ -19,7 +19,7 @@ cudaError_t launch_dropout(const void* x, const void* residual, void* y, long lo
 
 // pooled: 2 B heads blocks head_dim doubles; the backward's workspace: two floats a query.
 cudaError_t launch_select(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
-                          int* idx, cudaStream_t stream);
+                          int* idx, int num_sms, cudaStream_t stream);
 cudaError_t launch_sparse_forward(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k,
                                   const void* v, const int* idx, void* out, float* lse, int num_sms, cudaStream_t stream);
 cudaError_t launch_sparse_backward(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const sparse::BackwardMaps& m,

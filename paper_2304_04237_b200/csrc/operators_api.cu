@@ -68,6 +68,9 @@ slide_attn_status sparse_shape(int B, int H, int W, int heads, int head_dim, int
     return SLIDE_ATTN_OK;
 }
 
+// The threads that pool are counted in 31 bits.
+bool poolable(const sparse::Geometry& g, long long B, int head_dim) { return B * g.heads * g.blocks < (1LL << 31) / (head_dim / 4); }
+
 slide_attn_status with_top(sparse::Geometry* g, int top) {
     if (top < 1) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (top > sparse::kMaxTop) return SLIDE_ATTN_ERR_UNSUPPORTED;
@@ -168,6 +171,7 @@ slide_attn_status slide_attn_select_workspace(int B, int H, int W, int heads, in
     if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
     sparse::Geometry g;
     const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK && !poolable(g, B, head_dim)) return SLIDE_ATTN_ERR_UNSUPPORTED;
     if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(double) * (size_t)B * heads * g.blocks * head_dim;
     return st;
 }
@@ -180,13 +184,14 @@ slide_attn_status slide_attn_select_blocks(const void* q, const void* k, int* id
     slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
     if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st != SLIDE_ATTN_OK) return st;
+    if (!poolable(g, B, head_dim)) return SLIDE_ATTN_ERR_UNSUPPORTED;
     if (top > g.blocks || workspace_bytes < 2 * sizeof(double) * (size_t)B * heads * g.blocks * head_dim) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (any_misaligned(q, k, idx, workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
     if (among(idx, q, k, workspace) || among(workspace, q, k)) return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
-    return launched(launch_select(g, B, head_dim, dtype, q, k, static_cast<double*>(workspace), idx, static_cast<cudaStream_t>(cuda_stream)));
+    return launched(launch_select(g, B, head_dim, dtype, q, k, static_cast<double*>(workspace), idx, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const void* v, const int* idx, void* out, float* lse, int B, int H, int W,

@@ -21,48 +21,57 @@ template <> __device__ __forceinline__ void widen<__nv_bfloat16>(const uint4& r,
     v[4] = bf16_lo(r.z); v[5] = bf16_hi(r.z); v[6] = bf16_lo(r.w); v[7] = bf16_hi(r.w);
 }
 
-// A CTA pools one block of q (blockIdx.y = 0) or k: a thread keeps to a 16-byte column of the pixels and takes every so many of them.
+// A thread keeps to a 16-byte column of one block and takes every `parts`-th of its pixels; neighbouring threads have neighbouring columns, then
+// neighbouring blocks, so that a warp reads whole lines.  Parts are joined through shared memory, in their order.  blockIdx.y: q or k.
 // pooled: [q or k][B][heads][blocks][d]
 template <typename T>
-__global__ void __launch_bounds__(kPoolThreads) pool_kernel(const Geometry g, int d, long long images, const T* q, const T* k, double* pooled)
+__global__ void __launch_bounds__(kPoolThreads) pool_kernel(const Geometry g, Divisor by_columns, int d, long long images, int parts, const T* q, const T* k,
+                                                            double* pooled)
 {
     constexpr int V = 16 / sizeof(T);
-    __shared__ double part[kPoolThreads][V];
+    __shared__ double part_sums[kPoolThreads][V + 1];
     grid_dependency_wait();
-    const int C = g.heads * d, columns = C / V;
-    const int r = blockIdx.x % g.blocks;
-    const size_t b = blockIdx.x / g.blocks;
-    const Block own = block_of(g, r);
-    const int size = own.size();
-    const unsigned char* src = reinterpret_cast<const unsigned char*>((blockIdx.y ? k : q) + b * g.H * g.W * C);
-    for (int first = 0; first < columns; first += kPoolThreads) {
-        const int here = min(columns - first, kPoolThreads), rows = kPoolThreads / here;
-        const int column = threadIdx.x % here, row = threadIdx.x / here;
-        double sum[V] = {};
-        if (row < rows) {
-#pragma unroll 4
-            for (int i = row; i < size; i += rows) {
-                double v[V];
-                widen<T>(*reinterpret_cast<const uint4*>(src + ((size_t)pixel_of(g, own, i) * columns + first + column) * 16), v);
+    const int C = g.heads * d, columns = C / V, units = kPoolThreads / parts;
+    const int part = (int)threadIdx.x / units, own = (int)threadIdx.x - part * units;
+    const long long at = (long long)blockIdx.x * units + own;          // (image, block, column)
+    const bool there = at < images * g.blocks * columns;
+    unsigned column = there ? (unsigned)at : 0u;
+    unsigned r = by_columns.divide(column);
+    const unsigned b = g.by_blocks.divide(r);
+    const Block block = block_of(g, (int)r);
+    const int size = block.size();
+    double sum[V] = {};
+    if (there) {
+        const unsigned char* src = reinterpret_cast<const unsigned char*>((blockIdx.y ? k : q) + (size_t)b * (unsigned)(g.H * g.W) * (unsigned)C) + column * 16;
+#pragma unroll 8
+        for (int i = part; i < size; i += parts) {
+            double v[V];
+            widen<T>(*reinterpret_cast<const uint4*>(src + (size_t)(unsigned)pixel_of(g, block, i) * (unsigned)(C * (int)sizeof(T))), v);
 #pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] += v[e];
-            }
+            for (int e = 0; e < V; ++e) sum[e] += v[e];
         }
+    }
+    if (parts > 1) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) part[threadIdx.x][e] = sum[e];
+        for (int e = 0; e < V; ++e) part_sums[threadIdx.x][e] = sum[e];
         __syncthreads();
-        for (int c = threadIdx.x; c < here * V; c += kPoolThreads) {
-            double s = 0.0;
-            for (int i = 0; i < rows; ++i) s += part[i * here + c / V][c % V];
-            const int channel = first * V + c, h = channel / d;
-            pooled[((((size_t)blockIdx.y * images + b) * g.heads + h) * g.blocks + r) * d + channel - h * d] = blockIdx.y ? s / (double)size : s;
-        }
-        __syncthreads();
+        for (int p = 1; p < parts; ++p)
+            if (part == 0)
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += part_sums[p * units + own][e];
+    }
+    if (part || !there) return;
+    const unsigned channel = column * V, h = channel / (unsigned)d;
+    double* out = pooled + ((((size_t)blockIdx.y * images + b) * g.heads + h) * g.blocks + r) * d + (channel - h * d);
+#pragma unroll
+    for (int e = 0; e < V; e += 2) {
+        const double2 v = blockIdx.y ? make_double2(sum[e] / (double)size, sum[e + 1] / (double)size) : make_double2(sum[e], sum[e + 1]);
+        *reinterpret_cast<double2*>(out + e) = v;
     }
 }
 
 constexpr int kRankRows = 8;              // rows of scores of a CTA, one to a warp when they are ranked
-constexpr int kRankThreads = 32 * kRankRows;
+constexpr int kRankThreads = 32 * kRankRows, kRankColumns = 64;
 
 // The order of doubles as that of unsigned integers.  0 is below every score.
 __device__ __forceinline__ unsigned long long order_of(double x) {
@@ -71,32 +80,42 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
     return bits < 0 ? ~(unsigned long long)bits : (unsigned long long)bits | 0x8000000000000000ull;
 }
 
+// Eight rows of one image's and head's scores, the keys' means in tiles of 64 through shared memory (rows padded against bank conflicts), then
+// the largest, again and again.
 template <int D>
 __global__ void __launch_bounds__(kRankThreads) rank_kernel(const Geometry g, long long images, const double* pooled, int* idx)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     double* rows = reinterpret_cast<double*>(smem);                                       // [kRankRows][D]
-    unsigned long long* order = reinterpret_cast<unsigned long long*>(rows + kRankRows * D);      // [kRankRows][blocks]
+    double* tile = rows + kRankRows * D;                                                  // [kRankColumns][D + 1]
+    unsigned long long* order = reinterpret_cast<unsigned long long*>(tile + kRankColumns * (D + 1));     // [kRankRows][blocks]
     grid_dependency_wait();
     const int groups = (g.blocks + kRankRows - 1) / kRankRows;
-    const size_t plane = blockIdx.x / groups;                       // image and head
-    const int r0 = (int)(blockIdx.x % groups) * kRankRows, n = min(kRankRows, g.blocks - r0);
+    const size_t plane = blockIdx.x / (unsigned)groups;             // image and head
+    const int r0 = (int)(blockIdx.x - (unsigned)plane * (unsigned)groups) * kRankRows, n = min(kRankRows, g.blocks - r0);
     const double* qs = pooled + (plane * g.blocks + r0) * D;
     const double* ks = pooled + ((size_t)images * g.heads + plane) * g.blocks * D;
-    for (int i = threadIdx.x; i < n * D; i += kRankThreads) rows[i] = qs[i];
-    __syncthreads();
-    for (int s = threadIdx.x; s < g.blocks; s += kRankThreads) {
-        double sum[kRankRows] = {};
-#pragma unroll 4
-        for (int c = 0; c < D; ++c) {
-            const double kc = ks[(size_t)s * D + c];
-#pragma unroll
-            for (int i = 0; i < kRankRows; ++i) sum[i] = fma(rows[i * D + c], kc, sum[i]);
-        }
-        for (int i = 0; i < n; ++i) order[i * g.blocks + s] = order_of(sum[i]);
-    }
-    __syncthreads();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    for (int i = threadIdx.x; i < n * D; i += kRankThreads) rows[i] = qs[i];
+    for (int s0 = 0; s0 < g.blocks; s0 += kRankColumns) {
+        const int count = min(kRankColumns, g.blocks - s0);
+#pragma unroll
+        for (int i = threadIdx.x; i < kRankColumns * D; i += kRankThreads)
+            if (i < count * D) tile[i / D * (D + 1) + i % D] = ks[(size_t)s0 * D + i];
+        __syncthreads();
+        double x = 0.0, y = 0.0;                                    // columns lane and lane + 32 of the warp's row
+#pragma unroll 8
+        for (int c = 0; c < D; ++c) {
+            const double qc = rows[warp * D + c];
+            x = fma(qc, tile[lane * (D + 1) + c], x);
+            y = fma(qc, tile[(lane + 32) * (D + 1) + c], y);
+        }
+        if (warp < n) {
+            if (lane < count) order[warp * g.blocks + s0 + lane] = order_of(x);
+            if (lane + 32 < count) order[warp * g.blocks + s0 + lane + 32] = order_of(y);
+        }
+        __syncthreads();
+    }
     if (warp >= n) return;
     unsigned long long* mine = order + warp * g.blocks;
     int* out = idx + (plane * g.blocks + r0 + warp) * g.top;
@@ -116,7 +135,7 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const Geometry g, lo
 
 template <int D>
 cudaError_t launch_rank(const Geometry& g, long long B, const double* pooled, int* idx, cudaStream_t stream) {
-    constexpr int kMost = kRankRows * (kMaxBlocks + D) * 8;
+    constexpr int kFixed = (kRankRows * D + kRankColumns * (D + 1)) * 8, kMost = kFixed + kRankRows * kMaxBlocks * 8;
     static bool ready[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -127,21 +146,27 @@ cudaError_t launch_rank(const Geometry& g, long long B, const double* pooled, in
         if (dev < 64) ready[dev] = true;
     }
     const long long groups = (g.blocks + kRankRows - 1) / kRankRows;
-    return launch_chained(rank_kernel<D>, dim3((unsigned)(B * g.heads * groups)), kRankThreads, (size_t)kRankRows * (g.blocks + D) * 8, stream, g, B,
+    return launch_chained(rank_kernel<D>, dim3((unsigned)(B * g.heads * groups)), kRankThreads, (size_t)(kFixed + kRankRows * g.blocks * 8), stream, g, B,
                           pooled, idx);
 }
 
 }  // namespace sparse
 
 cudaError_t launch_select(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
-                          int* idx, cudaStream_t stream) {
+                          int* idx, int sms, cudaStream_t stream) {
     using namespace sparse;
     g.complete();
-    const dim3 grid((unsigned)(B * g.blocks), 2);
+    // Some 512 threads an SM, and 16-byte loads a thread to spare, keep the memory busy: fewer columns than that share their pixels.
+    const int columns = g.heads * head_dim * (dtype == SLIDE_ATTN_BF16 ? 2 : 4) / 16;
+    const long long units = B * g.blocks * columns;
+    int parts = 1;
+    while (parts < 16 && 2 * units * parts < 512LL * sms && parts * 8 < g.bh * g.bw) parts *= 2;
+    const dim3 grid((unsigned)((units * parts + kPoolThreads - 1) / kPoolThreads), 2);
+    const Divisor by_columns = Divisor::of(columns);
     cudaError_t e = dtype == SLIDE_ATTN_BF16
-                        ? launch_chained(pool_kernel<__nv_bfloat16>, grid, kPoolThreads, 0, stream, g, head_dim, B, static_cast<const __nv_bfloat16*>(q),
-                                         static_cast<const __nv_bfloat16*>(k), pooled)
-                        : launch_chained(pool_kernel<float>, grid, kPoolThreads, 0, stream, g, head_dim, B, static_cast<const float*>(q),
+                        ? launch_chained(pool_kernel<__nv_bfloat16>, grid, kPoolThreads, 0, stream, g, by_columns, head_dim, B, parts,
+                                         static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(k), pooled)
+                        : launch_chained(pool_kernel<float>, grid, kPoolThreads, 0, stream, g, by_columns, head_dim, B, parts, static_cast<const float*>(q),
                                          static_cast<const float*>(k), pooled);
     if (e != cudaSuccess) return e;
     if (head_dim == 16) return launch_rank<16>(g, B, pooled, idx, stream);

@@ -67,7 +67,7 @@ CASES = {
                               dict(p=1.01), dict(p=NAN), dict(y=D2)]] +
           [(dict(images=1 << 40, per_image=2), UNS), (dict(images=1 << 31, per_image=8, unit=1), UNS),
            (dict(x=A + 4), ALIGN), (dict(residual=B2 + 8), ALIGN), (dict(y=C2 + 2), ALIGN), (dict(rng=D2 + 4), ALIGN)],
-    select: SPARSE + [(c, ARG) for c in [dict(q=None), dict(k=None), dict(idx=None), dict(ws=None), dict(top=5), dict(size=2 * 8 * 2 * 2 * 4 * 32 - 1),
+    select: SPARSE + [(dict(B=1 << 20, heads=200, d=64), UNS)] + [(c, ARG) for c in [dict(q=None), dict(k=None), dict(idx=None), dict(ws=None), dict(top=5), dict(size=2 * 8 * 2 * 2 * 4 * 32 - 1),
                                          dict(idx=A), dict(ws=B2), dict(ws=C2)]] + [(dict(q=A + 8), ALIGN), (dict(idx=C2 + 4), ALIGN), (dict(ws=D2 + 8), ALIGN)],
     sparse: SPARSE + [(c, ARG) for c in [dict(q=None), dict(k=None), dict(v=None), dict(idx=None), dict(out=None), dict(lse=None), dict(out=A), dict(out=F2),
                                          dict(lse=C2)]] + [(dict(v=C2 + 8), ALIGN), (dict(lse=F2 + 4), ALIGN)],
