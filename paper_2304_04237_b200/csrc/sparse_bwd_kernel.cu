@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 2 : 3)
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 3 : D == 64 ? 3 : 4)
 sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, const T* dout, const float2* stats, T* dq)
 {
     using P = BackwardPipe<T, D>;
@@ -93,29 +93,33 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
         } else {
             const uint32_t tile = pipe.tile(at);
             const int used = min(N, keys - (step - P::kOwnSteps) * N);
-            if (busy) with_width<NT>(used, [&](auto width) {
+            if (busy) with_width<NT>(used, [&](auto width, auto partial) {
                 constexpr int W = decltype(width)::value;
-                float s[W][4], dp[W][4];
-                scores<D, L::kPlanes, W>(rows_q, tile, P::kPlane, lane, s);
-                scores<D, L::kPlanes, W>(rows_g, tile + P::kBehind, P::kPlane, lane, dp);
+#pragma unroll (L::kSplit ? 1 : W / 2)
+                for (int n = 0; n < W; n += 2) {             // 16 columns at a time
+                    float s[2][4], dp[2][4];
+                    const uint32_t at16 = tile + n * 8 * 2 * D;
+                    scores16<D, L::kPlanes>(rows_q, at16, P::kPlane, lane, s[0], s[1]);
+                    scores16<D, L::kPlanes>(rows_g, at16 + P::kBehind, P::kPlane, lane, dp[0], dp[1]);
 #pragma unroll
-                for (int n = 0; n < W; ++n)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float x, y;
-                        split_pair(fma2(make_pair(s[n][2 * i], s[n][2 * i + 1]), scales, sums[i]), x, y);
-                        x = fast_exp2(x);
-                        y = fast_exp2(y);
-                        split_pair(mul2(make_pair(x, y), add2(make_pair(dp[n][2 * i], dp[n][2 * i + 1]), deltas[i])), s[n][2 * i], s[n][2 * i + 1]);
+                        for (int i = 0; i < 2; ++i) {
+                            float x, y;
+                            split_pair(fma2(make_pair(s[j][2 * i], s[j][2 * i + 1]), scales, sums[i]), x, y);
+                            x = fast_exp2(x);
+                            y = fast_exp2(y);
+                            split_pair(mul2(make_pair(x, y), add2(make_pair(dp[j][2 * i], dp[j][2 * i + 1]), deltas[i])), s[j][2 * i], s[j][2 * i + 1]);
+                        }
+                    if (decltype(partial)::value && (W == 2 || n >= W / 2)) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if ((n + j) * 8 + 2 * (lane & 3) + (e & 1) >= used) s[j][e] = 0.0f;
                     }
-                if (used < W * 8) {
-#pragma unroll
-                    for (int n = 0; n < W; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = 0.0f;
+                    gather16<D, L::kPlanes>(s[0], s[1], at16, P::kPlane, lane, dqs);
                 }
-                gather<D, L::kPlanes, W>(s, tile, P::kPlane, lane, dqs);
             });
         }
         pipe.release();
@@ -153,7 +157,7 @@ template <typename T, int D> struct KeysPlan {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 && D == 64 ? 1 : 2)
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 2 : D == 64 ? 2 : 3)
 sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const int* idx, const float2* stats, const T* dout, T* dk, T* dv)
 {
     using K = KeysPlan<T, D>;
@@ -285,33 +289,37 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
                 }
                 const pair* stat = reinterpret_cast<const pair*>(columns + slot * 2 * N) + (lane & 3);       // of two queries each
                 const int used = min(N, total - done);
-                if (busy) with_width<NT>(used, [&](auto width) {
+                if (busy) with_width<NT>(used, [&](auto width, auto partial) {
                     constexpr int W = decltype(width)::value;
-                    float s[W][4], dp[W][4];
-                    scores<D, L::kPlanes, W>(rows_k, tile, K::kPlane, lane, s);
-                    scores<D, L::kPlanes, W>(rows_v, tile + K::kBehind, K::kPlane, lane, dp);
+#pragma unroll (L::kSplit ? 1 : W / 2)
+                    for (int n = 0; n < W; n += 2) {             // 16 columns at a time
+                        float s[2][4], dp[2][4];
+                        const uint32_t at16 = tile + n * 8 * 2 * D;
+                        scores16<D, L::kPlanes>(rows_k, at16, K::kPlane, lane, s[0], s[1]);
+                        scores16<D, L::kPlanes>(rows_v, at16 + K::kBehind, K::kPlane, lane, dp[0], dp[1]);
 #pragma unroll
-                    for (int n = 0; n < W; ++n) {
-                        const pair sums = stat[n * 4], deltas = stat[N / 2 + n * 4];
+                        for (int j = 0; j < 2; ++j) {
+                            const pair sums = stat[(n + j) * 4], deltas = stat[N / 2 + (n + j) * 4];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float& x = s[n][2 * i];
-                            float& y = s[n][2 * i + 1];
-                            split_pair(fma2(make_pair(x, y), scales, sums), x, y);
-                            x = fast_exp2(x);
-                            y = fast_exp2(y);
-                            split_pair(mul2(make_pair(x, y), add2(make_pair(dp[n][2 * i], dp[n][2 * i + 1]), deltas)), dp[n][2 * i], dp[n][2 * i + 1]);
+                            for (int i = 0; i < 2; ++i) {
+                                float& x = s[j][2 * i];
+                                float& y = s[j][2 * i + 1];
+                                split_pair(fma2(make_pair(x, y), scales, sums), x, y);
+                                x = fast_exp2(x);
+                                y = fast_exp2(y);
+                                split_pair(mul2(make_pair(x, y), add2(make_pair(dp[j][2 * i], dp[j][2 * i + 1]), deltas)), dp[j][2 * i], dp[j][2 * i + 1]);
+                            }
                         }
-                    }
-                    if (used < W * 8) {                          // (a key that is not finite makes a NaN of rows that hold nothing)
+                        if (decltype(partial)::value && (W == 2 || n >= W / 2)) {        // (a key that is not finite makes a NaN of rows that hold nothing)
 #pragma unroll
-                        for (int n = 0; n < W; ++n)
+                            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = dp[n][e] = 0.0f;
+                                for (int e = 0; e < 4; ++e)
+                                    if ((n + j) * 8 + 2 * (lane & 3) + (e & 1) >= used) s[j][e] = dp[j][e] = 0.0f;
+                        }
+                        gather16<D, L::kPlanes>(s[0], s[1], at16 + K::kBehind, K::kPlane, lane, dvs);
+                        gather16<D, L::kPlanes>(dp[0], dp[1], at16, K::kPlane, lane, dks);
                     }
-                    gather<D, L::kPlanes, W>(s, tile + K::kBehind, K::kPlane, lane, dvs);
-                    gather<D, L::kPlanes, W>(dp, tile, K::kPlane, lane, dks);
                 });
                 bar_arrive<kBlock>(Ring<S>::empty(slot));
                 slot = Ring<S>::after(slot);

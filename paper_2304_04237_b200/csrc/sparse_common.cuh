@@ -89,6 +89,11 @@ struct BackwardMaps {
 
 template <int D> __device__ __forceinline__ constexpr float root() { return D == 16 ? 0.25f : D == 32 ? 0.17677669529663688f : 0.125f; }
 
+__device__ __forceinline__ float log2_approx(float x) {         // off by 2^-22 at most
+    float d;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+    return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -214,11 +219,47 @@ __device__ __forceinline__ float settle(float large, float small) {
     return (__float_as_uint(large) & 0x7F800000u) == 0x7F800000u ? large : large + small;
 }
 
-// s[n-tile] = rows . tile^T (16 x D times D x 8 NT); `stride`: from a plane of the tile to the next.
-template <int D, int Planes, int NT>
-__device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t tile, uint32_t stride, int lane, float (&s)[NT][4]) {
+// Two neighbouring n-tiles, 16 columns, of rows . tile^T; `tile` points at the first of their rows, `stride`: from a plane of the tile to the next.
+template <int D, int Planes>
+__device__ __forceinline__ void scores16(const Rows<D, Planes>& rows, uint32_t tile, uint32_t stride, int lane, float (&s0)[4], float (&s1)[4]) {
     const int row = (lane & 7) + ((lane >> 4) << 3), piece = (lane >> 3) & 1;
     if constexpr (Planes == 1) {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            uint32_t b[4];
+            ldmatrix4(tile + plane_at<D>(row, 2 * ks + piece), b);
+            if (ks == 0) {
+                mma<true>(s0, rows.a[ks], b[0], b[1]);
+                mma<true>(s1, rows.a[ks], b[2], b[3]);
+            } else {
+                mma<false>(s0, rows.a[ks], b[0], b[1]);
+                mma<false>(s1, rows.a[ks], b[2], b[3]);
+            }
+        }
+    } else {
+        float small0[4], small1[4];
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            uint32_t a[3][4], b[3][4];
+            rows.get(ks, lane, a);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) ldmatrix4(tile + p * stride + plane_at<D>(row, 2 * ks + piece), b[p]);
+            if (ks == 0) products<true>(s0, s1, small0, small1, a, b);
+            else products<false>(s0, s1, small0, small1, a, b);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s0[e] = settle(s0[e], small0[e]);
+            s1[e] = settle(s1[e], small1[e]);
+        }
+    }
+}
+
+// s[n-tile] = rows . tile^T (16 x D times D x 8 NT), step by step over D for all columns.
+template <int D, int Planes, int NT>
+__device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t tile, uint32_t stride, int lane, float (&s)[NT][4]) {
+    if constexpr (Planes == 1) {
+        const int row = (lane & 7) + ((lane >> 4) << 3), piece = (lane >> 3) & 1;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
@@ -234,81 +275,63 @@ __device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t til
                 }
             }
     } else {
-        float small[NT][4];
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            uint32_t a[3][4];
-            rows.get(ks, lane, a);
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                uint32_t b[3][4];
-#pragma unroll
-                for (int p = 0; p < 3; ++p) ldmatrix4(tile + p * stride + n * 8 * 2 * D + plane_at<D>(row, 2 * ks + piece), b[p]);
-                if (ks == 0) products<true>(s[n], s[n + 1], small[n], small[n + 1], a, b);
-                else products<false>(s[n], s[n + 1], small[n], small[n + 1], a, b);
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = settle(s[n][e], small[n][e]);
+        for (int n = 0; n < NT; n += 2) scores16<D, 3>(rows, tile + n * 8 * 2 * D, stride, lane, s[n], s[n + 1]);
     }
 }
 
-// o[n-tile] += weights . tile (16 x 8 NT times 8 NT x D), the weights as `scores` leaves them.  fp32: the tensor core truncates as it adds, so a
-// tile's sums start at zero and are added in fp32.
-template <int D, int Planes, int NT>
-__device__ __forceinline__ void gather(const float (&w)[NT][4], uint32_t tile, uint32_t stride, int lane, float (&o)[D / 8][4]) {
-    const uint32_t at = tile;
+// o[n-tile] += weights . tile for 16 rows of the tile (16 x 16 times 16 x D), the weights as scores16 leaves them; `tile` points at the first of the
+// rows.  fp32: the tensor core truncates as it adds, so 16 products are added up from zero and the sums in fp32.
+template <int D, int Planes>
+__device__ __forceinline__ void gather16(const float (&w0)[4], const float (&w1)[4], uint32_t tile, uint32_t stride, int lane, float (&o)[D / 8][4]) {
     if constexpr (Planes == 1) {
+        const uint32_t a[4] = {pack_bf16(w0[0], w0[1]), pack_bf16(w0[2], w0[3]), pack_bf16(w1[0], w1[1]), pack_bf16(w1[2], w1[3])};
 #pragma unroll
-        for (int ks = 0; ks < NT / 2; ++ks) {
-            const uint32_t a[4] = {pack_bf16(w[2 * ks][0], w[2 * ks][1]), pack_bf16(w[2 * ks][2], w[2 * ks][3]),
-                                   pack_bf16(w[2 * ks + 1][0], w[2 * ks + 1][1]), pack_bf16(w[2 * ks + 1][2], w[2 * ks + 1][3])};
-#pragma unroll
-            for (int n = 0; n < D / 8; n += 2) {
-                uint32_t b[4];
-                ldmatrix4_trans(at + ks * 16 * 2 * D + plane_at<D>(lane & 15, n + (lane >> 4)), b);
-                mma_bf16(o[n], a, b[0], b[1]);
-                mma_bf16(o[n + 1], a, b[2], b[3]);
-            }
+        for (int n = 0; n < D / 8; n += 2) {
+            uint32_t b[4];
+            ldmatrix4_trans(tile + plane_at<D>(lane & 15, n + (lane >> 4)), b);
+            mma_bf16(o[n], a, b[0], b[1]);
+            mma_bf16(o[n + 1], a, b[2], b[3]);
         }
     } else {
-        float large[D / 8][4], small[D / 8][4];
+        uint32_t a[3][4];
 #pragma unroll
-        for (int ks = 0; ks < NT / 2; ++ks) {
-            uint32_t a[3][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float2 v = make_float2(w[2 * ks + (i >> 1)][2 * (i & 1)], w[2 * ks + (i >> 1)][2 * (i & 1) + 1]);
-                a[0][i] = split::pack_upper(v.x, v.y);
-                v = split::rest2(v);
-                a[1][i] = split::pack_upper(v.x, v.y);
-                v = split::rest2(v);
-                a[2][i] = split::pack_upper(v.x, v.y);
-            }
-#pragma unroll
-            for (int n = 0; n < D / 8; n += 2) {
-                uint32_t b[3][4];
-#pragma unroll
-                for (int p = 0; p < 3; ++p) ldmatrix4_trans(at + p * stride + ks * 16 * 2 * D + plane_at<D>(lane & 15, n + (lane >> 4)), b[p]);
-                if (ks == 0) products<true>(large[n], large[n + 1], small[n], small[n + 1], a, b);
-                else products<false>(large[n], large[n + 1], small[n], small[n + 1], a, b);
-            }
+        for (int i = 0; i < 4; ++i) {
+            float2 v = i < 2 ? make_float2(w0[2 * (i & 1)], w0[2 * (i & 1) + 1]) : make_float2(w1[2 * (i & 1)], w1[2 * (i & 1) + 1]);
+            a[0][i] = split::pack_upper(v.x, v.y);
+            v = split::rest2(v);
+            a[1][i] = split::pack_upper(v.x, v.y);
+            v = split::rest2(v);
+            a[2][i] = split::pack_upper(v.x, v.y);
         }
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n)
+        for (int n = 0; n < D / 8; n += 2) {
+            float large[2][4], small[2][4];
+            uint32_t b[3][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[n][e] += settle(large[n][e], small[n][e]);
+            for (int p = 0; p < 3; ++p) ldmatrix4_trans(tile + p * stride + plane_at<D>(lane & 15, n + (lane >> 4)), b[p]);
+            products<true>(large[0], large[1], small[0], small[1], a, b);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o[n][e] += settle(large[0][e], small[0][e]);
+                o[n + 1][e] += settle(large[1][e], small[1][e]);
+            }
+        }
     }
 }
 
-// Calls f with the smallest of the tile widths (in n-tiles of 8) that holds `used` rows: straight code for each instead of a branch at each step.
-template <int NT, typename F> __device__ __forceinline__ void with_width(int used, F f) {
+// Calls f(width in n-tiles of 8, whether some of the columns hold nothing): for a full tile, or with the smallest of its halves, quarters ... that
+// holds `used` rows.  Straight code for each, instead of a branch at each step; columns that hold nothing are in the second half (of two
+// n-tiles: anywhere).
+template <int NT, typename F> __device__ __forceinline__ void with_part(int used, F f) {
     if constexpr (NT > 2) {
-        if (used <= NT * 4) return with_width<NT / 2>(used, f);
+        if (used <= NT * 4) return with_part<NT / 2>(used, f);
     }
-    f(std::integral_constant<int, NT>{});
+    f(std::integral_constant<int, NT>{}, std::true_type{});
+}
+template <int NT, typename F> __device__ __forceinline__ void with_width(int used, F f) {
+    if (used == NT * 8) f(std::integral_constant<int, NT>{}, std::false_type{});
+    else with_part<NT>(used, f);
 }
 
 // An entry of a list, worked out once: the pixels of a block `width` wide whose first is `pixel`, and the list's rows up to its end.

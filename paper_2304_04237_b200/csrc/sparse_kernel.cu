@@ -33,9 +33,9 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
 
     Unit unit;
     Rows<D, L::kPlanes> rows;
-    float o[D / 8][4], sum[2], base[2], limit[2];      // base: scaled; limit: the score above which it is raised
-    const pair scales = make_pair(scale, scale);
-    pair bases[2];                                     // less the base, twice
+    float o[D / 8][4], sum[2], limit[2];               // limit: the score above which the base is raised
+    const pair scales = both(scale);
+    pair bases[2];                                     // less the base that exponents are taken from, scaled, twice
     int item = 0, step = 0, keys = 0;
     while (item < pipe.items) {
         const uint32_t at = pipe.next();
@@ -48,19 +48,19 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) { sum[i] = base[i] = 0.0f; limit[i] = -INFINITY; bases[i] = make_pair(0.0f, 0.0f); }
+            for (int i = 0; i < 2; ++i) { sum[i] = 0.0f; limit[i] = -INFINITY; bases[i] = both(0.0f); }
         }
         const bool busy = warp * 16 < unit.rows;
         if (step > 0) {
             const uint32_t tile = pipe.tile(at);
             const int used = min(N, keys - (step - 1) * N);
-            if (busy) with_width<NT>(used, [&](auto width) {
+            if (busy) with_width<NT>(used, [&](auto width, auto partial) {
                 constexpr int W = decltype(width)::value;
                 float s[W][4];
                 scores<D, L::kPlanes, W>(rows, tile, P::kPlane, lane, s);
-                if (used < W * 8) {
+                if constexpr (decltype(partial)::value) {
 #pragma unroll
-                    for (int n = 0; n < W; ++n)
+                    for (int n = W > 2 ? W / 2 : 0; n < W; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             if (n * 8 + 2 * (lane & 3) + (e & 1) >= used) s[n][e] = -INFINITY;
@@ -79,9 +79,10 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
                         if (m > limit[i]) {
-                            const float raised = m * scale, fade = limit[i] == -INFINITY ? 0.0f : fast_exp2(base[i] - raised);
-                            base[i] = raised;
-                            bases[i] = make_pair(-raised, -raised);
+                            float less, same;
+                            split_pair(bases[i], less, same);
+                            const float raised = m * scale, fade = limit[i] == -INFINITY ? 0.0f : fast_exp2(-less - raised);
+                            bases[i] = both(-raised);
                             limit[i] = m + 8.0f / scale;
                             sum[i] *= fade;
 #pragma unroll
@@ -89,23 +90,27 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                         }
                     }
                 }
+                // 16 columns at a time, so that the exponentials of the next go beside the products of these
+                pair l[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    pair l = 0;
+                for (int n = 0; n < W; ++n) {
 #pragma unroll
-                    for (int n = 0; n < W; ++n) {
+                    for (int i = 0; i < 2; ++i) {
                         float& x = s[n][2 * i];
                         float& y = s[n][2 * i + 1];
                         split_pair(fma2(make_pair(x, y), scales, bases[i]), x, y);
                         x = fast_exp2(x);
                         y = fast_exp2(y);
-                        l = n == 0 ? make_pair(x, y) : add2(l, make_pair(x, y));
+                        l[i] = n == 0 ? make_pair(x, y) : add2(l[i], make_pair(x, y));
                     }
+                    if (n & 1) gather16<D, L::kPlanes>(s[n - 1], s[n], tile + P::kBehind + (n - 1) * 8 * 2 * D, P::kPlane, lane, o);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
                     float l0, l1;
-                    split_pair(l, l0, l1);
+                    split_pair(l[i], l0, l1);
                     sum[i] += l0 + l1;
                 }
-                gather<D, L::kPlanes, W>(s, tile + P::kBehind, P::kPlane, lane, o);
             });
         }
         pipe.release();
@@ -118,13 +123,14 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
                 l += __shfl_xor_sync(0xffffffffu, l, 2);
                 const int row = warp * 16 + i * 8 + (lane >> 2);
                 if (row < unit.rows) {
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;      // no keys, or none that is not -inf: zeros
+                    const float inv = l == 0.0f ? 0.0f : rcp_approx(l);      // no keys, or none that is not -inf: zeros
                     const size_t at_row = (unit.image * (unsigned)(g.H * g.W) + unit.pixel(g, row)) * (unsigned)g.heads + (unsigned)unit.h;
                     T* dst = out + at_row * D + 2 * (lane & 3);
 #pragma unroll
                     for (int n = 0; n < D / 8; ++n) store2(dst + n * 8, o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
-                    if ((lane & 3) == 0)
-                        lse[at_row] = l == 0.0f ? -INFINITY : base[i] * kLn2 + logf(l);
+                    float less, same;
+                    split_pair(bases[i], less, same);
+                    if ((lane & 3) == 0) lse[at_row] = (log2_approx(l) - less) * kLn2;      // log 0 is -infinity
                 }
             }
         }
