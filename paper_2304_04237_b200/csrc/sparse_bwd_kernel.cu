@@ -53,7 +53,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
     using L = Layout<T, D>;
     constexpr int N = P::N, NT = N / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = uniform((int)threadIdx.x / 32), lane = threadIdx.x % 32;
     constexpr float scale = root<D>();
 
     grid_dependency_wait();
@@ -73,7 +73,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
         const uint32_t at = pipe.next();
         if (step == 0) {
             unit.find(g, pipe.first + item);
-            keys = pipe.rows_of(item);
+            keys = uniform(pipe.rows_of(item));
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = warp * 16 + i * 8 + (lane >> 2);
@@ -168,7 +168,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     const uint32_t base = smem_u32(smem);
     Entry* list = reinterpret_cast<Entry*>(smem + K::kListAt);
     const float* columns = reinterpret_cast<const float*>(smem + K::kStatsAt);          // of each stage: less the logarithms, then less the deltas
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = uniform((int)threadIdx.x / 32), lane = threadIdx.x % 32;
     const bool copying = warp == kThreads / 32;
     constexpr float scale = root<D>();
 
@@ -250,7 +250,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
             }
             if constexpr (L::kSplit) __syncthreads();        // the stages are free
         }
-        const int total = (int)(listed & 0x1FFFFFu);
+        const int total = uniform((int)(listed & 0x1FFFFFu));
         if (copying) {
             Ring<S> ring;
             Cursor cursor;

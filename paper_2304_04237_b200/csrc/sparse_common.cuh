@@ -108,6 +108,9 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// A value that is the same in all lanes, so that the compiler knows it: branches on it need no reconvergence.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // Named barriers of `Count` threads, by whole warps: a wait, or an arrival only.
 template <int Count> __device__ __forceinline__ void bar_sync(int id) {
     __syncwarp();
@@ -546,7 +549,7 @@ template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
                     ring.commit();
                 }
             }
-            const int total = rows_of(item);
+            const int total = uniform(rows_of(item));
             if (item + 1 < items) {
                 unit.find(g, first + item + 1);
                 read();                                          // on its way while this unit's tiles are sent for

@@ -21,7 +21,7 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
     using L = Layout<T, D>;
     constexpr int N = P::N, NT = N / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = uniform((int)threadIdx.x / 32), lane = threadIdx.x % 32;
     constexpr float scale = root<D>() * kLog2e;
 
     grid_dependency_wait();
@@ -41,7 +41,7 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
         const uint32_t at = pipe.next();
         if (step == 0) {
             unit.find(g, pipe.first + item);
-            keys = pipe.rows_of(item);
+            keys = uniform(pipe.rows_of(item));
             pipe.take(at, 0, warp * 16, lane, rows, nullptr);
 #pragma unroll
             for (int n = 0; n < D / 8; ++n)
