@@ -12,7 +12,7 @@ namespace slide_attn {
 
 namespace sparse {
 
-template <typename T, int D> using BackwardPipe = QueryPipe<T, D, sizeof(T) == 4 || D == 64 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 3 : 4, 2>;
+template <typename T, int D> using BackwardPipe = QueryPipe<T, D, sizeof(T) == 4 ? 32 : 64, sizeof(T) == 4 && D == 64 ? 3 : 4, 2>;
 
 // The logarithm to base 2 of a row's sum.  A row that has none (no keys, or none but -inf) has no weights: exp2 of less infinity.
 __device__ __forceinline__ float log2_of_sum(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
@@ -31,18 +31,27 @@ template <> __device__ __forceinline__ float dot_piece<__nv_bfloat16>(const __nv
     return s;
 }
 
-// Less each query's logarithm of the sum (base 2), and less its delta: a thread a query and head.
+// Less each query's logarithm of the sum (base 2), and less its delta: a query and head by as many neighbouring lanes as it has 16-byte pieces.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats)
 {
+    constexpr int kPiece = 16 / sizeof(T), kLanes = D / kPiece, kEach = 4, kAtOnce = 256 / kLanes;
     grid_dependency_wait();
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    float s = 0.0f;
-    constexpr int kPiece = 16 / sizeof(T);
+    const int lane = threadIdx.x % kLanes;
+    const long long first = (long long)blockIdx.x * (kAtOnce * kEach) + threadIdx.x / kLanes;
+    float s[kEach];
 #pragma unroll
-    for (int e = 0; e < D; e += kPiece) s += dot_piece<T>(dout + i * D + e, out + i * D + e);
-    stats[i] = make_float2(-log2_of_sum(lse[i]), -s);
+    for (int i = 0; i < kEach; ++i) {
+        const long long row = first + i * kAtOnce;
+        s[i] = row < n ? dot_piece<T>(dout + row * D + lane * kPiece, out + row * D + lane * kPiece) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o /= 2) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+        const long long row = first + i * kAtOnce;
+        if (row < n && lane == 0) stats[row] = make_float2(-log2_of_sum(lse[row]), -s[i]);
+    }
 }
 
 template <typename T, int D>
@@ -182,8 +191,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
         unsigned pixels[kRows / 32];
 #pragma unroll
         for (int i = 0; i < kRows / 32; ++i) pixels[i] = unit.pixel(g, lane + 32 * i);
-        Sender<T, D, kRows>::send(base + K::kOwnAt, reinterpret_cast<const unsigned char*>(k + plane), pixel_bytes, pixels, unit.rows, lane);
-        Sender<T, D, kRows>::send(base + K::kOwnAt + K::kOwn, reinterpret_cast<const unsigned char*>(v + plane), pixel_bytes, pixels, unit.rows, lane);
+        Sender<T, D, kRows>::send(base + K::kOwnAt, base + K::kOwnAt + K::kOwn, k + plane, v + plane, pixel_bytes, pixels, unit.rows, lane);
         copies_commit();
     }
     const bool busy = warp * 16 < unit.rows;
@@ -263,8 +271,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
                 for (int i = 0; i < N / 32; ++i) pixels[i] = done + 32 * i + lane < total ? cursor.pixel(g, done + 32 * i + lane) : 0u;
                 ring.claim();
                 const uint32_t stage = base + (uint32_t)ring.slot * K::kStage, at = base + K::kStatsAt + (uint32_t)(ring.slot * 2 * N * 4);
-                Sender<T, D, N>::send(stage, reinterpret_cast<const unsigned char*>(q + plane), pixel_bytes, pixels, total - done, lane);
-                Sender<T, D, N>::send(stage + K::kTile, reinterpret_cast<const unsigned char*>(dout + plane), pixel_bytes, pixels, total - done, lane);
+                Sender<T, D, N>::send(stage, stage + K::kTile, q + plane, dout + plane, pixel_bytes, pixels, total - done, lane);
 #pragma unroll
                 for (int i = 0; i < N / 32; ++i)
                     if (done + 32 * i + lane < total) {
@@ -359,7 +366,8 @@ cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& 
     const long long n = B * g.H * g.W * g.heads;
     auto in = [](const void* p) { return static_cast<const T*>(p); };
     auto to = [](void* p) { return static_cast<T*>(p); };
-    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + 255) / 256)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats);
+    constexpr long long rows = 256 / (D * sizeof(T) / 16) * 4;      // of a block
+    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + rows - 1) / rows)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats);
     if (e != cudaSuccess) return e;
     e = launch_chained(sparse_queries_kernel<T, D>, dim3((units + chain - 1) / chain), kBlock, smem_q, stream, g, units, chain, in(m.q), in(m.k),
                        in(m.v), m.idx, in(m.dout), static_cast<const float2*>(stats), to(m.dq));

@@ -441,22 +441,34 @@ template <int S> struct Ring {
     }
 };
 
-// Copies of the copying warp: N rows, a row by as many neighbouring lanes as it has pieces.  Lane l has looked up rows l, l + 32, ...
+// Copies of the copying warp: N rows of one map or of two, a row by as many neighbouring lanes as it has pieces.  Lane l has looked up rows l,
+// l + 32, ...
 template <typename T, int D, int N> struct Sender {
     using L = Layout<T, D>;
     static constexpr int kRowsAtOnce = 32 / L::kPieces, kPasses = N / kRowsAtOnce, kLookups = N / 32;
     static_assert(N % 32 == 0 && kRowsAtOnce >= 1, "rows by lanes");
     // pixels[i]: of row lane + 32 i, anything where there is none; rows from `count` on are zeros
-    static __device__ __forceinline__ void send(uint32_t tile, const unsigned char* plane, unsigned pixel_bytes, const unsigned (&pixels)[kLookups], int count,
-                                                int lane) {
+    static __device__ __forceinline__ void send(uint32_t tile_a, uint32_t tile_b, const void* plane_a, const void* plane_b, unsigned pixel_bytes,
+                                                const unsigned (&pixels)[kLookups], int count, int lane) {
+        if (count >= N) rows<true>(tile_a, tile_b, plane_a, plane_b, pixel_bytes, pixels, count, lane);
+        else rows<false>(tile_a, tile_b, plane_a, plane_b, pixel_bytes, pixels, count, lane);
+    }
+    template <bool Full>
+    static __device__ __forceinline__ void rows(uint32_t tile_a, uint32_t tile_b, const void* plane_a, const void* plane_b, unsigned pixel_bytes,
+                                                const unsigned (&pixels)[kLookups], int count, int lane) {
         const int row0 = lane / L::kPieces, piece = lane % L::kPieces;
-        const unsigned char* src = plane + piece * 16;
+        const unsigned char* const a = static_cast<const unsigned char*>(plane_a) + piece * 16;
+        const unsigned char* const b = static_cast<const unsigned char*>(plane_b) + piece * 16;
 #pragma unroll
         for (int i = 0; i < kPasses; ++i) {
             const int row = i * kRowsAtOnce + row0;
-            const unsigned pixel = __shfl_sync(0xffffffffu, pixels[i * kRowsAtOnce / 32], row & 31);
-            const bool there = row < count;
-            copy16(tile + L::at(row, piece), src + (there ? (size_t)pixel * pixel_bytes : 0), there);
+            unsigned pixel = __shfl_sync(0xffffffffu, pixels[i * kRowsAtOnce / 32], row & 31);
+            const uint32_t at = L::at(row, piece);
+            const bool there = Full || row < count;
+            if constexpr (!Full) pixel = there ? pixel : 0u;
+            const size_t off = (size_t)pixel * pixel_bytes;
+            copy16(tile_a + at, a + off, there);
+            if (plane_b) copy16(tile_b + at, b + off, there);
         }
     }
 };
@@ -543,9 +555,10 @@ template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
                         __syncwarp();
                     }
                     const uint32_t stage = base + (uint32_t)ring.slot * kStage;
-                    Sender<T, D, kRows>::send(stage, reinterpret_cast<const unsigned char*>((o ? own1 : own0) + plane), pixel_bytes, pixels, unit.rows, lane);
                     if constexpr (Own > 1 && kOwnSteps == 1)
-                        Sender<T, D, kRows>::send(stage + kOwn, reinterpret_cast<const unsigned char*>(own1 + plane), pixel_bytes, pixels, unit.rows, lane);
+                        Sender<T, D, kRows>::send(stage, stage + kOwn, own0 + plane, own1 + plane, pixel_bytes, pixels, unit.rows, lane);
+                    else
+                        Sender<T, D, kRows>::send(stage, 0, (o ? own1 : own0) + plane, nullptr, pixel_bytes, pixels, unit.rows, lane);
                     ring.commit();
                 }
             }
@@ -563,8 +576,7 @@ template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
                 for (int i = 0; i < N / 32; ++i) pixels[i] = done + 32 * i + lane < total ? cursor.pixel(g, done + 32 * i + lane) : 0u;
                 ring.claim();
                 const uint32_t stage = base + (uint32_t)ring.slot * kStage;
-                Sender<T, D, N>::send(stage, reinterpret_cast<const unsigned char*>(k + plane), pixel_bytes, pixels, total - done, lane);
-                Sender<T, D, N>::send(stage + kTile, reinterpret_cast<const unsigned char*>(v + plane), pixel_bytes, pixels, total - done, lane);
+                Sender<T, D, N>::send(stage, stage + kTile, k + plane, v + plane, pixel_bytes, pixels, total - done, lane);
                 ring.commit();
             }
             __syncwarp();                                        // the table is free again
