@@ -246,18 +246,19 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 def _device_ptrs(where, *tensors):
     """Addresses of contiguous CUDA tensors (None stays None), all on the current device."""
-    device, ptrs = None, []
+    device = _raw_device() if _raw_device and torch.cuda.is_initialized() else None
+    ptrs = []
     for t in tensors:
         if t is None:
             ptrs.append(None)
-            continue
-        if not t.is_cuda or not t.is_contiguous():
+        elif t.get_device() == device and t.is_contiguous():
+            ptrs.append(t.data_ptr())
+        elif not t.is_cuda or not t.is_contiguous():
             raise ValueError(f"{where} takes contiguous CUDA tensors")
-        if device is None:
-            device = _raw_device() if _raw_device else torch.cuda.current_device()
-        if t.get_device() != device:
-            raise ValueError(f"{where}: a tensor is on device {t.get_device()}, the current device is {device}")
-        ptrs.append(t.data_ptr())
+        elif t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"{where}: a tensor is on device {t.get_device()}, the current device is {torch.cuda.current_device()}")
+        else:
+            ptrs.append(t.data_ptr())
     return ptrs
 
 

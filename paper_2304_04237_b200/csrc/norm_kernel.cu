@@ -5,12 +5,16 @@
 //   dz = dy act'(z),  du = gamma_c dz,  dx = rstd (du - mean(du) - u mean(du u)),  dgamma_c = sum dz u,  dbeta_c = sum dz
 //
 // Bound by memory: x in and y out; x, dy in and dx out.  Two passes that stream over the map: sums of chunks of pixels, then the result, whose
-// inputs the second pass finds in L2 (126 MB) as long as they fit; a small launch between them joins the chunks and lays out what the second
-// pass multiplies each channel by.  A thread keeps to one 16-byte column of the pixels, of which a CTA takes whole rows.  Images that
+// inputs the second pass finds in L2 (126 MB) as long as they fit.  The chunks are joined by every CTA of the second pass or, where there are many
+// groups, by a small launch between the passes.  A thread keeps to one 16-byte column of the pixels, of which a CTA takes whole rows.  Images that
 // one CTA can hold in its registers take one launch.
+// 64 x 56 x 56 x 96, bf16, 32 groups: with GELU forward and backward in turn 96 us, of 29.5 for the 193 MB that they cannot do without (with SiLU, over and
+// over on the same maps, 30 us and 46).  Each pass reads its maps again, and the activation's special functions and roundings share the issue slots.
 // (One pass for all, with an image's pixels kept in the shared memory of a cluster of CTAs that exchange their sums, read every map once,
-// but its barriers and low occupancy made 64 x 56 x 56 x 96, bf16, GELU, forward and backward, take 114 us against PASS_US here.)
+// but its barriers and low occupancy made 64 x 56 x 56 x 96, bf16, GELU, forward and backward, take 114 us.)
 // All sums are fp32, in an order that only the shape decides.
+#include <atomic>
+
 #include "operators.cuh"
 #include "packed.cuh"
 
@@ -38,7 +42,8 @@ struct NormArgs {
     float* mean;          // [B][groups], written by the forward and read by the backward
     float* rstd;
     float2* partial;      // [B][groups][chunks]: forward mean and sum of squares about it, backward sums of du and of du u
-    float* factors;       // [B][2 (forward) or 4 (backward)][C]: see Factors
+    float2* joined;       // backward: [B][groups], what a launch between the passes joined; null: the second pass does it
+    bool join;            // forward: the second pass joins the chunks
     float* channels;      // backward: [B][chunks][2][C], sums of dz and of dz u; or null
     float eps;
 };
@@ -259,10 +264,37 @@ template <int Threads, int Maps, int Batch> struct Stream {
     }
 };
 
-// What the passes multiply by, V channels of it.  Forward: less the mean, and rstd gamma.  Backward, with c = x - mean: z = c (rstd gamma) + beta,
-// dx = dz (rstd gamma) + (c quad + shift), quad = -rstd^2 mean(du u), shift = -rstd mean(du).
-template <int V> __device__ __forceinline__ void get_factors(const float* factors, int C, int which, int column, pair (&v)[V / 2]) {
-    get_weights<V>(factors + (size_t)which * C, column * V, 0.0f, v);
+// An image's group's moments from its chunks', by a warp; deviations from the first chunk's mean, so that nothing large cancels.  (mean, rstd)
+__device__ __forceinline__ float2 join_moments(const NormShape& s, const float2* chunks, float eps, int lane) {
+    const float per = (float)s.per_group, n = (float)s.P * per;
+    const float m0 = chunks[0].x;
+    float shift = 0.0f;
+    for (int c = lane; c < s.chunks; c += 32) shift += (float)chunk_pixels(s, c) * per * (chunks[c].x - m0);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) shift += __shfl_xor_sync(0xffffffffu, shift, o);
+    const float m = m0 + shift / n;
+    float m2 = 0.0f;
+    for (int c = lane; c < s.chunks; c += 32) {
+        const float2 v = chunks[c];
+        const float d = v.x - m;
+        m2 += fmaf((float)chunk_pixels(s, c) * per * d, d, v.y);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+    return make_float2(m, 1.0f / sqrtf(m2 / n + eps));
+}
+// The same of the backward's sums: (quad, shift), of which dx = dz (rstd gamma) + (c quad + shift) with c = x - mean: quad = -rstd^2 mean(du u),
+// shift = -rstd mean(du).
+__device__ __forceinline__ float2 join_slopes(const NormShape& s, const float2* chunks, float rstd, int lane) {
+    float2 t = make_float2(0.0f, 0.0f);
+    for (int c = lane; c < s.chunks; c += 32) { t.x += chunks[c].x; t.y += chunks[c].y; }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+        t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+        t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+    }
+    const float inv = 1.0f / ((float)s.P * (float)s.per_group);
+    return make_float2(-rstd * rstd * (t.y * inv), -rstd * (t.x * inv));
 }
 
 // First pass, forward: of a chunk, each group's mean and sum of squares about that mean, which loses nothing however far it is from zero: batch by
@@ -357,46 +389,21 @@ __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_su
         a.partial[((size_t)at.image * s.groups + g) * s.chunks + at.chunk] = make_float2(means[g], squares[g]);
 }
 
-// Between the passes, a CTA an image, a warp a group: joins the chunks' moments (deviations from the first chunk's mean, so that nothing
-// large cancels), then lays out the factors.
-__global__ void __launch_bounds__(512) norm_join_kernel(const NormArgs a, const NormShape s)
+// Between the passes: a warp an image and group.
+template <bool Backward>
+__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a, const NormShape s, long long n)
 {
-    extern __shared__ __align__(16) unsigned char smem[];
-    float2* stats = reinterpret_cast<float2*>(smem);
     grid_dependency_wait();
     grid_launch_dependents();
-    const size_t b = blockIdx.x;
+    const long long i = (long long)blockIdx.x * 8 + threadIdx.x / 32;
+    if (i >= n) return;
     const int lane = threadIdx.x % 32;
-    const float per = (float)s.per_group, n = (float)s.P * per;
-    for (int g = threadIdx.x / 32; g < s.groups; g += blockDim.x / 32) {
-        const float2* chunks = a.partial + (b * s.groups + g) * s.chunks;
-        const float m0 = chunks[0].x;
-        float shift = 0.0f;
-        for (int c = lane; c < s.chunks; c += 32) shift += (float)chunk_pixels(s, c) * per * (chunks[c].x - m0);
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) shift += __shfl_xor_sync(0xffffffffu, shift, o);
-        const float m = m0 + shift / n;
-        float m2 = 0.0f;
-        for (int c = lane; c < s.chunks; c += 32) {
-            const float2 v = chunks[c];
-            const float d = v.x - m;
-            m2 += fmaf((float)chunk_pixels(s, c) * per * d, d, v.y);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-        if (lane == 0) {
-            const float rstd = 1.0f / sqrtf(m2 / n + a.eps);
-            stats[g] = make_float2(m, rstd);
-            a.mean[b * s.groups + g] = m;
-            a.rstd[b * s.groups + g] = rstd;
-        }
-    }
-    __syncthreads();
-    float* out = a.factors + b * 2 * s.C;
-    for (int c = threadIdx.x; c < s.C; c += blockDim.x) {
-        const float2 v = stats[c / s.per_group];
-        out[c] = -v.x;
-        out[s.C + c] = v.y * (a.gamma ? a.gamma[c] : 1.0f);
+    if constexpr (Backward) {
+        const float2 r = join_slopes(s, a.partial + i * s.chunks, a.rstd[i], lane);
+        if (lane == 0) a.joined[i] = r;
+    } else {
+        const float2 r = join_moments(s, a.partial + i * s.chunks, a.eps, lane);
+        if (lane == 0) { a.mean[i] = r.x; a.rstd[i] = r.y; }
     }
 }
 
@@ -418,14 +425,36 @@ __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_fo
     using Maps = Stream<Threads, 1, kTogether>;
     const Place at = find_place<T>(s);
     unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
+    float2* stats = reinterpret_cast<float2*>(smem + Maps::kSmem);        // mean and rstd
     grid_dependency_wait();
-    if (!at.active) return;
     Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, nullptr, at);
-    pair scale[Q], beta[Q], mean[Q];
-    const float* factors = a.factors + (size_t)at.image * 2 * s.C;
-    get_factors<V>(factors, s.C, 0, at.column, mean);
-    get_factors<V>(factors, s.C, 1, at.column, scale);
+    const size_t first = (size_t)at.image * s.groups;
+    if (a.join) {
+        const int lane = threadIdx.x % 32;
+        for (int g = threadIdx.x / 32; g < s.groups; g += Threads / 32) {
+            const float2 r = join_moments(s, a.partial + (first + g) * s.chunks, a.eps, lane);
+            if (lane) continue;
+            stats[g] = r;
+            if (at.chunk == 0) { a.mean[first + g] = r.x; a.rstd[first + g] = r.y; }
+        }
+    } else {
+        for (int g = threadIdx.x; g < s.groups; g += Threads) stats[g] = make_float2(a.mean[first + g], a.rstd[first + g]);
+    }
+    __syncthreads();
+    if (!at.active) return;
+    pair scale[Q], beta[Q], mean[Q];                                // mean: less it
+    get_weights<V>(a.gamma, at.column * V, 1.0f, scale);
     get_weights<V>(a.beta, at.column * V, 0.0f, beta);
+    {
+        int group[V];
+        find_groups<V>(s.per_group, at.column, group);
+#pragma unroll
+        for (int e = 0; e < Q; ++e) {
+            const float2 u = stats[group[2 * e]], v = stats[group[2 * e + 1]];
+            mean[e] = make_pair(-u.x, -v.x);
+            scale[e] = mul2(scale[e], make_pair(u.y, v.y));
+        }
+    }
 #pragma unroll 1
     for (int done = 0; done < at.mine; done += kTogether) {
         uint4 raw[kTogether];
@@ -547,39 +576,6 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
         a.partial[((size_t)at.image * s.groups + g) * s.chunks + at.chunk] = make_float2(local[g], local[s.groups + g]);
 }
 
-// Between the passes of the backward, a CTA an image, a warp a group.
-__global__ void __launch_bounds__(512) norm_join_slopes_kernel(const NormArgs a, const NormShape s)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    float2* stats = reinterpret_cast<float2*>(smem);                // quad and shift
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const size_t b = blockIdx.x;
-    const int lane = threadIdx.x % 32;
-    const float inv = 1.0f / ((float)s.P * (float)s.per_group);
-    const float* rstds = a.rstd + b * s.groups;
-    for (int g = threadIdx.x / 32; g < s.groups; g += blockDim.x / 32) {
-        const float2* chunks = a.partial + (b * s.groups + g) * s.chunks;
-        float2 t = make_float2(0.0f, 0.0f);
-        for (int c = lane; c < s.chunks; c += 32) { t.x += chunks[c].x; t.y += chunks[c].y; }
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) {
-            t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
-            t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
-        }
-        if (lane == 0) stats[g] = make_float2(-rstds[g] * rstds[g] * (t.y * inv), -rstds[g] * (t.x * inv));
-    }
-    __syncthreads();
-    float* out = a.factors + b * 4 * s.C;
-    for (int c = threadIdx.x; c < s.C; c += blockDim.x) {
-        const int g = c / s.per_group;
-        out[c] = -a.mean[b * s.groups + g];
-        out[s.C + c] = rstds[g] * (a.gamma ? a.gamma[c] : 1.0f);
-        out[2 * s.C + c] = stats[g].x;
-        out[3 * s.C + c] = stats[g].y;
-    }
-}
-
 template <int Threads, typename T, int Act>
 __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_backward_kernel(const NormArgs a, const NormShape s)
 {
@@ -590,15 +586,35 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_b
     unsigned char* dst = static_cast<unsigned char*>(a.y) + at.start;
     grid_dependency_wait();
     if (a.channels) grid_launch_dependents();          // the weights' sums come next
-    if (!at.active) return;
     Maps maps(smem, static_cast<const unsigned char*>(a.x) + at.start, static_cast<const unsigned char*>(a.dy) + at.start, at);
+    float2* stats = reinterpret_cast<float2*>(smem + Maps::kSmem);        // quad and shift
+    const size_t first = (size_t)at.image * s.groups;
+    if (!a.joined) {
+        const int lane = threadIdx.x % 32;
+        for (int g = threadIdx.x / 32; g < s.groups; g += Threads / 32) {
+            const float2 r = join_slopes(s, a.partial + (first + g) * s.chunks, a.rstd[first + g], lane);
+            if (lane == 0) stats[g] = r;
+        }
+    } else {
+        for (int g = threadIdx.x; g < s.groups; g += Threads) stats[g] = a.joined[first + g];
+    }
+    __syncthreads();
+    if (!at.active) return;
     pair mean[Q], scale[Q], beta[Q], quad[Q], shift[Q];
-    const float* factors = a.factors + (size_t)at.image * 4 * s.C;
-    get_factors<V>(factors, s.C, 0, at.column, mean);
-    get_factors<V>(factors, s.C, 1, at.column, scale);
-    get_factors<V>(factors, s.C, 2, at.column, quad);
-    get_factors<V>(factors, s.C, 3, at.column, shift);
+    get_weights<V>(a.gamma, at.column * V, 1.0f, scale);
     get_weights<V>(a.beta, at.column * V, 0.0f, beta);
+    {
+        int group[V];
+        find_groups<V>(s.per_group, at.column, group);
+#pragma unroll
+        for (int e = 0; e < Q; ++e) {
+            const int i = group[2 * e], j = group[2 * e + 1];
+            mean[e] = make_pair(-a.mean[first + i], -a.mean[first + j]);
+            scale[e] = mul2(scale[e], make_pair(a.rstd[first + i], a.rstd[first + j]));
+            quad[e] = make_pair(stats[i].x, stats[j].x);
+            shift[e] = make_pair(stats[i].y, stats[j].y);
+        }
+    }
 #pragma unroll 1
     for (int done = 0; done < at.mine; done += kPair) {
         uint4 raw[2 * kPair];
@@ -661,30 +677,44 @@ bool make_shape(long long B, long long P, int C, int groups, int size, int maps,
         s.rounds = (int)rounds;
     }
     const long long chunks = (P + (long long)s.rows * s.rounds - 1) / ((long long)s.rows * s.rounds);
-    if (B > 0x7fffffffLL / chunks) return false;
+    if (B > 0x7fffffffLL / chunks || B > 0x7fffffffLL / groups) return false;
     s.chunks = (int)chunks;
     *out = s;
     return true;
 }
 
-// More than 48 KB of shared memory (thousands of channels) has to be asked for.
-template <typename... Params, typename... Args>
-cudaError_t launch_with(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
+// More than 48 KB of shared memory has to be asked for, once on each device and for the most that any call takes (kMostSmem: the backward's first
+// pass of 4096 channels in as many groups), so that threads of the host that launch at the same time ask for the same.
+constexpr size_t kMostSmem = 192 * 1024;
+template <auto Kernel, typename... Args>
+cudaError_t launch_with(dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
+    static std::atomic<bool> asked[64];
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
+        if (dev >= 64 || !asked[dev].load(std::memory_order_acquire)) {
+            e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
+            if (e != cudaSuccess) return e;
+            if (dev < 64) asked[dev].store(true, std::memory_order_release);
+        }
     }
-    return launch_chained(kernel, grid, threads, smem, stream, args...);
+    return launch_chained(Kernel, grid, threads, smem, stream, args...);
 }
 
 size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
-// A workspace: partial, factors, channels.
+// Every CTA of the second pass joins the chunks of its image by itself where each of its warps has one group at most, which saves a launch: 128 x 128
+// x 96, fp32, SiLU, 8 groups 11.9 us against 12.3, backward 12.9 against 14.6 (no launch gaps counted; launched one by one 14.4 against 16.1, 17.9
+// against 19.9).  With 32 groups it would take 17.9 us against 11.1, 17.1 against 15.2.
+bool joins_inline(const NormShape& s) { return s.groups <= s.threads / 32; }
+
+// A workspace: partial, joined, channels.
 struct NormRoom {
-    size_t factors, channels, bytes;
+    size_t joined, channels, bytes;
     NormRoom(const NormShape& s, long long B, int maps) {
         const bool once = maps == 1 && s.chunks == 1;
-        factors = once ? 0 : align16((size_t)B * s.groups * s.chunks * sizeof(float2));
-        channels = once ? 0 : factors + align16((size_t)B * 2 * maps * s.C * sizeof(float));
+        joined = once ? 0 : align16((size_t)B * s.groups * s.chunks * sizeof(float2));
+        channels = joined + (maps == 1 || joins_inline(s) ? 0 : align16((size_t)B * s.groups * sizeof(float2)));
         bytes = channels + (maps == 1 ? 0 : (size_t)B * s.chunks * 2 * s.C * sizeof(float));
     }
 };
@@ -694,10 +724,12 @@ cudaError_t forward_as(const NormArgs& a, const NormShape& s, long long B, cudaS
     const dim3 grid((unsigned)(B * s.chunks));
     constexpr size_t ring = Stream<Threads, 1, kTogether>::kSmem;
     const size_t smem = (size_t)(s.threads * 2 * Vec<T>::pairs + 2 * s.groups) * 4;
-    if (s.chunks == 1) return launch_with(norm_forward_once_kernel<Threads, T, Act>, grid, Threads, smem, stream, a, s);
-    cudaError_t e = launch_with(norm_sums_kernel<Threads, T>, grid, Threads, ring + smem, stream, a, s);
-    if (e == cudaSuccess) e = launch_chained(norm_join_kernel, dim3((unsigned)B), 512, (size_t)s.groups * sizeof(float2), stream, a, s);
-    return e == cudaSuccess ? launch_with(norm_forward_kernel<Threads, T, Act>, grid, Threads, ring, stream, a, s) : e;
+    if (s.chunks == 1) return launch_with<norm_forward_once_kernel<Threads, T, Act>>(grid, Threads, smem, stream, a, s);
+    cudaError_t e = launch_with<norm_sums_kernel<Threads, T>>(grid, Threads, ring + smem, stream, a, s);
+    if (e == cudaSuccess && !a.join)
+        e = launch_chained(norm_join_kernel<false>, dim3((unsigned)((B * s.groups + 7) / 8)), 256, 0, stream, a, s, B * s.groups);
+    if (e != cudaSuccess) return e;
+    return launch_with<norm_forward_kernel<Threads, T, Act>>(grid, Threads, ring + s.groups * sizeof(float2), stream, a, s);
 }
 template <typename T, int Act>
 cudaError_t forward_with(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
@@ -718,9 +750,11 @@ cudaError_t backward_as(const NormArgs& a, const NormShape& s, long long B, cuda
     constexpr size_t ring = Stream<Threads, 2, kPair>::kSmem;
     const int red = s.threads * 2 * Vec<T>::pairs;
     const size_t smem = (size_t)((red > 2 * s.C ? red : 2 * s.C) + 2 * s.C + 2 * s.groups) * 4;
-    cudaError_t e = launch_with(norm_slopes_kernel<Threads, T, Act>, grid, Threads, ring + smem, stream, a, s);
-    if (e == cudaSuccess) e = launch_chained(norm_join_slopes_kernel, dim3((unsigned)B), 512, (size_t)s.groups * sizeof(float2), stream, a, s);
-    return e == cudaSuccess ? launch_with(norm_backward_kernel<Threads, T, Act>, grid, Threads, ring, stream, a, s) : e;
+    cudaError_t e = launch_with<norm_slopes_kernel<Threads, T, Act>>(grid, Threads, ring + smem, stream, a, s);
+    if (e == cudaSuccess && a.joined)
+        e = launch_chained(norm_join_kernel<true>, dim3((unsigned)((B * s.groups + 7) / 8)), 256, 0, stream, a, s, B * s.groups);
+    if (e != cudaSuccess) return e;
+    return launch_with<norm_backward_kernel<Threads, T, Act>>(grid, Threads, ring + s.groups * sizeof(float2), stream, a, s);
 }
 template <typename T, int Act>
 cudaError_t backward_with(const NormArgs& a, const NormShape& s, long long B, cudaStream_t stream) {
@@ -749,9 +783,7 @@ cudaError_t launch_group_norm_forward(const void* x, const float* gamma, const f
                                       cudaStream_t stream) {
     NormShape s;
     if (!make_shape(B, P, C, groups, dtype == SLIDE_ATTN_BF16 ? 2 : 4, 1, &s)) return cudaErrorInvalidValue;
-    const NormRoom room(s, B, 1);
-    unsigned char* ws = static_cast<unsigned char*>(workspace);
-    const NormArgs a = {x, gamma, beta, nullptr, y, mean, rstd, reinterpret_cast<float2*>(ws), reinterpret_cast<float*>(ws + room.factors), nullptr, eps};
+    const NormArgs a = {x, gamma, beta, nullptr, y, mean, rstd, static_cast<float2*>(workspace), nullptr, joins_inline(s), nullptr, eps};
     return dtype == SLIDE_ATTN_BF16 ? forward_of<__nv_bfloat16>(a, s, B, act, stream) : forward_of<float>(a, s, B, act, stream);
 }
 
@@ -764,7 +796,7 @@ cudaError_t launch_group_norm_backward(const void* x, const float* gamma, const 
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     float* channels = dgamma ? reinterpret_cast<float*>(ws + room.channels) : nullptr;
     const NormArgs a = {x, gamma, beta, dy, dx, const_cast<float*>(mean), const_cast<float*>(rstd), reinterpret_cast<float2*>(ws),
-                        reinterpret_cast<float*>(ws + room.factors), channels, 0.0f};
+                        joins_inline(s) ? nullptr : reinterpret_cast<float2*>(ws + room.joined), false, channels, 0.0f};
     cudaError_t e = dtype == SLIDE_ATTN_BF16 ? backward_of<__nv_bfloat16>(a, s, B, act, stream) : backward_of<float>(a, s, B, act, stream);
     if (e != cudaSuccess || !dgamma) return e;
     cudaLaunchConfig_t cfg = {};

@@ -69,7 +69,7 @@ def test_forward_and_backward(shape, act, dtype):
     check(call(x, gamma, beta, groups, act, dy), ops.group_norm(back(x), back(gamma), back(beta), groups, 1e-5, act, back(dy)), dtype)
 
 
-@pytest.mark.parametrize("groups", [1, 8, 2048])
+@pytest.mark.parametrize("groups", [1, 8, 2048, 4096])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("half", [False, True])
 def test_as_many_channels_as_there_may_be(dtype, groups, half):
