@@ -329,7 +329,7 @@ slide_attn_status slide_attn_profile_end(slide_attn_ctx* ctx, double* forward_ms
  * replayed side by side, need one each.  Every call is asynchronous on `cuda_stream`, allocates nothing,
  * may be captured into a graph, and gives the same bits every time.  Arguments are checked on the host
  * before anything is launched; a workspace that is missing or too small is SLIDE_ATTN_ERR_INVALID_ARG.
- * Outputs may not be inputs unless that is said.
+ * Outputs may not share memory with inputs or with one another unless that is said.
  * ================================================================================================== */
 
 typedef enum {
@@ -381,7 +381,7 @@ typedef enum {
 /*
  * Dropout with a residual, from a counter-based generator; the mask is never stored:
  *     y = residual + (kept ? x / (1 - p) : 0)
- *   x, y       [in / out] `images` times `per_image` elements; y may be x or residual
+ *   x, y       [in / out] `images` times `per_image` elements; y may be x or residual itself
  *   residual   [in]  the same, or NULL (zeros)
  *   p          0 <= p <= 1; with p = 1 nothing is kept
  *   rng        [in, DEVICE] two unsigned 64-bit integers: seed and offset.  They are read when the call
@@ -407,7 +407,8 @@ slide_attn_status slide_attn_dropout_backward(const void* dy, void* dx, long lon
  * blocks = ceil(H / block_h) * ceil(W / block_w).  Every block of queries has, head by head, a list of `top`
  * blocks, and its queries attend to all pixels of the listed blocks.  A sequence of n tokens is a map with
  * H = 1, W = n.
- * Supported: head_dim 16, 32 or 64; block edges up to 32; up to 1024 blocks; top up to 64.
+ * Supported: head_dim 16, 32 or 64; block edges up to 32; up to 1024 blocks; top up to 64; pixels of less
+ * than 2^29 elements.
  *
  * slide_attn_select_blocks fills the lists by a score of pooled queries and keys,
  *     score(r, s) = sum over d of (sum of q over block r)[d] * (mean of k over block s)[d]
@@ -432,8 +433,8 @@ slide_attn_status slide_attn_select_workspace(int B, int H, int W, int heads, in
  *                 listed twice counts twice.
  *   lse           [out] float [B][H][W][heads]
  * Queries that see nothing, or nothing but scores of -infinity, get out = 0 and lse = -infinity.  fp32
- * storage: fp32 arithmetic (products of operands in two TF32 parts).  bf16: products of bf16 operands, softmax weights rounded
- * to bf16 for the product with v, sums in fp32, out rounded once.
+ * storage: fp32 arithmetic (products of operands cut into three bf16 parts, to 2^-24).  bf16: products of
+ * bf16 operands, softmax weights rounded to bf16 for the product with v, sums in fp32, out rounded once.
  */
 slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const void* v, const int* idx,
                                             void* out, float* lse,

@@ -13,8 +13,17 @@ bool misaligned(const void* p, unsigned to = 16) { return (reinterpret_cast<uint
 template <typename... P> bool any_null(P... p) { return (... || (p == nullptr)); }
 template <typename... P> bool any_misaligned(P... p) { return (... || misaligned(p)); }
 
-// Whether an output is also one of the others.
-template <typename... P> bool among(const void* out, P... p) { return (... || (out == static_cast<const void*>(p))); }
+// Memory that a call reads or writes.
+struct Span {
+    uintptr_t at;
+    size_t bytes;
+    Span(const void* p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), bytes(p ? n : 0) {}
+};
+// Whether an output shares memory with one of the others.
+bool meet(const Span& a, const Span& b) { return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+template <typename... S> bool meets(const Span& out, const S&... s) { return (... || meet(out, s)); }
+
+size_t size_of(slide_attn_dtype t) { return t == SLIDE_ATTN_BF16 ? 2 : 4; }
 
 // The current device is one that the kernels run on; its SMs.
 slide_attn_status current_device(int* num_sms) {
@@ -57,6 +66,7 @@ bool known_activation(slide_attn_activation a) { return a == SLIDE_ATTN_ACT_NONE
 slide_attn_status sparse_shape(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, sparse::Geometry* g) {
     if (B < 1 || H < 1 || W < 1 || heads < 1 || head_dim < 1 || block_h < 1 || block_w < 1) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (head_dim != 16 && head_dim != 32 && head_dim != 64) return SLIDE_ATTN_ERR_UNSUPPORTED;
+    if (heads >= (1 << 29) / head_dim) return SLIDE_ATTN_ERR_UNSUPPORTED;       // the kernels count a pixel's bytes in 31 bits
     if (block_h > sparse::kMaxEdge || block_w > sparse::kMaxEdge) return SLIDE_ATTN_ERR_UNSUPPORTED;
     const long long across = ((long long)W + block_w - 1) / block_w, down = ((long long)H + block_h - 1) / block_h;
     if (across > sparse::kMaxBlocks || down > sparse::kMaxBlocks || across * down > sparse::kMaxBlocks) return SLIDE_ATTN_ERR_UNSUPPORTED;
@@ -70,6 +80,11 @@ slide_attn_status sparse_shape(int B, int H, int W, int heads, int head_dim, int
 
 // The threads that pool are counted in 31 bits.
 bool poolable(const sparse::Geometry& g, long long B, int head_dim) { return B * g.heads * g.blocks < (1LL << 31) / (head_dim / 4); }
+
+size_t map_bytes(const sparse::Geometry& g, int B, int head_dim, slide_attn_dtype t) { return (size_t)B * g.H * g.W * g.heads * head_dim * size_of(t); }
+size_t lse_bytes(const sparse::Geometry& g, int B) { return (size_t)B * g.H * g.W * g.heads * sizeof(float); }
+size_t list_bytes(const sparse::Geometry& g, int B) { return (size_t)B * g.heads * g.blocks * g.top * sizeof(int); }
+size_t pooled_bytes(const sparse::Geometry& g, int B, int head_dim) { return 2 * (size_t)B * g.heads * g.blocks * head_dim * sizeof(double); }
 
 slide_attn_status with_top(sparse::Geometry* g, int top) {
     if (top < 1) return SLIDE_ATTN_ERR_INVALID_ARG;
@@ -95,14 +110,15 @@ slide_attn_status slide_attn_group_norm_forward(const void* x, const float* gamm
                                                 int W, int C, int groups, float eps, slide_attn_activation act, slide_attn_dtype dtype,
                                                 void* workspace, size_t workspace_bytes, void* cuda_stream)
 {
-    const void *vy = y, *vm = mean, *vr = rstd, *vw = workspace;
-    if (any_null(x, vy, vm, vr)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_null(x, static_cast<const void*>(y), static_cast<const void*>(mean), static_cast<const void*>(rstd))) return SLIDE_ATTN_ERR_INVALID_ARG;
     size_t need = 0;
     slide_attn_status st = norm_shape(B, H, W, C, groups, dtype, false, &need);
     if (st != SLIDE_ATTN_OK) return st;
-    if (!known_activation(act) || !(eps >= 0.0f) || isinf(eps) || workspace_bytes < need || (need && !vw)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (any_misaligned(x, gamma, beta, vy, vm, vr, vw)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    if (among(vy, x, gamma, beta, vm, vr, vw) || among(vm, x, gamma, beta, vr, vw) || among(vr, x, gamma, beta, vw) || (vw && among(vw, x, gamma, beta)))
+    if (!known_activation(act) || !(eps >= 0.0f) || isinf(eps) || workspace_bytes < need || (need && !workspace)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(x, gamma, beta, y, mean, rstd, workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    const size_t map = (size_t)B * H * W * C * size_of(dtype), weights = (size_t)C * sizeof(float), moments = (size_t)B * groups * sizeof(float);
+    const Span sx(x, map), sg(gamma, weights), sb(beta, weights), sy(y, map), sm(mean, moments), sr(rstd, moments), sw(workspace, need);
+    if (meets(sy, sx, sg, sb, sm, sr, sw) || meets(sm, sx, sg, sb, sr, sw) || meets(sr, sx, sg, sb, sw) || meets(sw, sx, sg, sb))
         return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
@@ -116,17 +132,20 @@ slide_attn_status slide_attn_group_norm_backward(const void* x, const float* gam
                                                  slide_attn_activation act, slide_attn_dtype dtype, void* workspace, size_t workspace_bytes,
                                                  void* cuda_stream)
 {
-    const void *vx = dx, *vg = dgamma, *vb = dbeta, *vw = workspace;
-    if (any_null(x, static_cast<const void*>(mean), static_cast<const void*>(rstd), dy, vx, vw)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_null(x, static_cast<const void*>(mean), static_cast<const void*>(rstd), dy, static_cast<const void*>(dx), static_cast<const void*>(workspace)))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
     if ((dgamma == nullptr) != (dbeta == nullptr)) return SLIDE_ATTN_ERR_INVALID_ARG;
     size_t need = 0;
     slide_attn_status st = norm_shape(B, H, W, C, groups, dtype, true, &need);
     if (st != SLIDE_ATTN_OK) return st;
     if (!known_activation(act) || workspace_bytes < need) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (any_misaligned(x, gamma, beta, mean, rstd, dy, vx, vg, vb, vw)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    for (const void* o : {vx, vg, vb, vw})
-        if (o && among(o, x, dy, gamma, beta, mean, rstd)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (among(vx, vg, vb, vw) || (vg && among(vg, vb, vw)) || vb == vw) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (any_misaligned(x, gamma, beta, mean, rstd, dy, dx, dgamma, dbeta, workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
+    const size_t map = (size_t)B * H * W * C * size_of(dtype), weights = (size_t)C * sizeof(float), moments = (size_t)B * groups * sizeof(float);
+    const Span sx(x, map), sg(gamma, weights), sb(beta, weights), sm(mean, moments), sr(rstd, moments), sy(dy, map), so(dx, map), sdg(dgamma, weights),
+        sdb(dbeta, weights), sw(workspace, need);
+    for (const Span& o : {so, sdg, sdb, sw})
+        if (meets(o, sx, sg, sb, sm, sr, sy)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (meets(so, sdg, sdb, sw) || meets(sdg, sdb, sw) || meets(sdb, sw)) return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
@@ -144,7 +163,10 @@ slide_attn_status dropout(const void* x, const void* residual, void* y, long lon
     if (!(p >= 0.0f && p <= 1.0f)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (per_image > (1LL << 40) / images || !dropout_supports(images, per_image, unit == SLIDE_ATTN_DROP_IMAGES)) return SLIDE_ATTN_ERR_UNSUPPORTED;
     if (any_misaligned(x, residual, y) || misaligned(rng, 8)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    if (y == rng) return SLIDE_ATTN_ERR_INVALID_ARG;
+    const size_t map = (size_t)images * per_image * size_of(dtype);
+    const Span sy(y, map);
+    if ((y != x && meets(sy, Span(x, map))) || (y != residual && meets(sy, Span(residual, map))) || meets(sy, Span(rng, 16)))
+        return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     const slide_attn_status st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
@@ -172,7 +194,7 @@ slide_attn_status slide_attn_select_workspace(int B, int H, int W, int heads, in
     sparse::Geometry g;
     const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
     if (st == SLIDE_ATTN_OK && !poolable(g, B, head_dim)) return SLIDE_ATTN_ERR_UNSUPPORTED;
-    if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(double) * (size_t)B * heads * g.blocks * head_dim;
+    if (st == SLIDE_ATTN_OK) *bytes = pooled_bytes(g, B, head_dim);
     return st;
 }
 
@@ -185,9 +207,11 @@ slide_attn_status slide_attn_select_blocks(const void* q, const void* k, int* id
     if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st != SLIDE_ATTN_OK) return st;
     if (!poolable(g, B, head_dim)) return SLIDE_ATTN_ERR_UNSUPPORTED;
-    if (top > g.blocks || workspace_bytes < 2 * sizeof(double) * (size_t)B * heads * g.blocks * head_dim) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (top > g.blocks || workspace_bytes < pooled_bytes(g, B, head_dim)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (any_misaligned(q, k, idx, workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    if (among(idx, q, k, workspace) || among(workspace, q, k)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    const size_t map = map_bytes(g, B, head_dim, dtype);
+    const Span sq(q, map), sk(k, map), si(idx, list_bytes(g, B)), sw(workspace, pooled_bytes(g, B, head_dim));
+    if (meets(si, sq, sk, sw) || meets(sw, sq, sk)) return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
@@ -204,7 +228,9 @@ slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const 
     if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st != SLIDE_ATTN_OK) return st;
     if (any_misaligned(q, k, v, idx, out, lse)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    if (among(out, q, k, v, idx, lse) || among(lse, q, k, v, idx)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    const size_t map = map_bytes(g, B, head_dim, dtype);
+    const Span sq(q, map), sk(k, map), sv(v, map), si(idx, list_bytes(g, B)), so(out, map), sl(lse, lse_bytes(g, B));
+    if (meets(so, sq, sk, sv, si, sl) || meets(sl, sq, sk, sv, si)) return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;
@@ -216,7 +242,7 @@ slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, in
     if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
     sparse::Geometry g;
     const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
-    if (st == SLIDE_ATTN_OK) *bytes = 2 * sizeof(float) * (size_t)B * H * W * heads;
+    if (st == SLIDE_ATTN_OK) *bytes = 2 * lse_bytes(g, B);
     return st;
 }
 
@@ -232,11 +258,14 @@ slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const
     slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
     if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st != SLIDE_ATTN_OK) return st;
-    if (workspace_bytes < 2 * sizeof(float) * (size_t)B * H * W * heads) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (workspace_bytes < 2 * lse_bytes(g, B)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (any_misaligned(q, k, v, idx, out, lse, dout, dq, dk, dv) || misaligned(workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
-    for (const void* o : {static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(workspace)})
-        if (among(o, q, k, v, idx, out, lse, dout)) return SLIDE_ATTN_ERR_INVALID_ARG;
-    if (among(dq, dk, dv, workspace) || among(dk, dv, workspace) || dv == workspace) return SLIDE_ATTN_ERR_INVALID_ARG;
+    const size_t map = map_bytes(g, B, head_dim, dtype);
+    const Span sq(q, map), sk(k, map), sv(v, map), si(idx, list_bytes(g, B)), so(out, map), sl(lse, lse_bytes(g, B)), sd(dout, map), sdq(dq, map),
+        sdk(dk, map), sdv(dv, map), sw(workspace, 2 * lse_bytes(g, B));
+    for (const Span& o : {sdq, sdk, sdv, sw})
+        if (meets(o, sq, sk, sv, si, so, sl, sd)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (meets(sdq, sdk, sdv, sw) || meets(sdk, sdv, sw) || meets(sdv, sw)) return SLIDE_ATTN_ERR_INVALID_ARG;
     int sms = 0;
     st = current_device(&sms);
     if (st != SLIDE_ATTN_OK) return st;

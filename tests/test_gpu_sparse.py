@@ -9,7 +9,8 @@ from oracle import operators as ops
 pytestmark = pytest.mark.gpu
 
 TD = {"f32": torch.float32, "bf16": torch.bfloat16}
-# Errors relative to the sums of absolute values (`*_abs`).  fp32: products of two TF32 parts lose 2^-21 of sum |q||k| / sqrt(d), here up to some 15, which
+# Errors relative to the sums of absolute values (`*_abs`).  fp32: of the nine products of three bf16 parts three are left out, 2^-23 of |q||k| at most, and the
+# six that are added up are truncated to 2^-24 each: 2^-21 of sum |q||k| / sqrt(d), here up to some 15, which
 # moves exponents by up to 7e-6; the exponent's own rounding 1e-6; the rest is a dozen steps of 2^-24.  bf16: one rounding (half a step of 2^-8) of
 # each weight beside those, and of the result.
 TERMS = {"f32": 2e-5, "bf16": 2.0 ** -8 + 2e-5}

@@ -7,7 +7,7 @@ import torch
 import paper_2304_04237_b200 as sa
 from paper_2304_04237_b200 import binding
 
-A, B2, C2, D2, E2, F2, G2, H2, I2, J2, K2 = (0x10000 * i for i in range(1, 12))     # addresses that nothing reads
+A, B2, C2, D2, E2, F2, G2, H2, I2, J2, K2 = (i << 32 for i in range(1, 12))     # addresses that nothing reads
 BIG = 1 << 40
 
 
@@ -50,7 +50,8 @@ NAN, INF = float("nan"), float("inf")
 MAP = [dict(B=0), dict(H=0), dict(W=-1), dict(dtype=2)]
 SPARSE = [(c, ARG) for c in MAP + [dict(heads=0), dict(bh=0), dict(bw=-4), dict(top=0)]] + [
     (dict(d=8), UNS), (dict(d=48), UNS), (dict(d=128), UNS), (dict(bh=33), UNS), (dict(bw=64), UNS), (dict(top=65), UNS),
-    (dict(H=64, W=64, bh=1, bw=2), UNS), (dict(H=1 << 30, W=1 << 30), UNS), (dict(B=1 << 30, heads=64), UNS)]
+    (dict(H=64, W=64, bh=1, bw=2), UNS), (dict(H=1 << 30, W=1 << 30), UNS), (dict(B=1 << 30, heads=64), UNS),
+    (dict(B=1, heads=1 << 25), UNS)]
 
 CASES = {
     norm: [(c, ARG) for c in MAP + [dict(C=0), dict(groups=0), dict(x=None), dict(y=None), dict(mean=None), dict(rstd=None), dict(eps=-1.0), dict(eps=NAN),
@@ -75,6 +76,33 @@ CASES = {
                                               dict(ws=None), dict(size=2 * 4 * 2 * 64 * 2 - 1), dict(dq=A), dict(dk=G2), dict(dv=I2), dict(dq=J2), dict(ws=F2),
                                               dict(ws=H2)]] + [(dict(dk=I2 + 8), ALIGN), (dict(ws=K2 + 4), ALIGN)],
 }
+
+
+# Outputs that share a part of their memory with another tensor: the last 16 bytes of one, or a place inside it.  Bytes of a tensor of `norm`, ...
+NORM, BACK, DROP, SPARSE_MAP = 2 * 40 * 40 * 32 * 4, 2 * 4 * 4 * 32 * 4, 2 * 12 * 4, 2 * 8 * 8 * 2 * 32 * 4
+PARTS = [(norm, dict(y=A + NORM - 16)), (norm, dict(mean=D2 + 64)), (norm, dict(rstd=E2 + 16)), (norm, dict(ws=F2 + 16)), (norm, dict(y=C2 - NORM + 16)),
+         (norm_back, dict(dx=F2 + BACK - 16)), (norm_back, dict(dgamma=I2 + 64)), (norm_back, dict(dx=J2 - 16)), (norm_back, dict(ws=E2 + 16)),
+         (drop, dict(per_image=12, y=A + DROP - 16)), (drop, dict(per_image=12, y=A, residual=A + 16)), (drop, dict(per_image=12, y=B2 - 16)),
+         (drop, dict(per_image=12, rng=C2 + 8)), (drop, dict(per_image=12, y=D2 - DROP + 16)),
+         (select, dict(idx=A + SPARSE_MAP - 16)), (select, dict(ws=B2 + 16)), (select, dict(idx=D2 + 64)),
+         (sparse, dict(out=C2 - 16)), (sparse, dict(lse=E2 + SPARSE_MAP - 16)), (sparse, dict(out=D2 - 16)),
+         (sparse_back, dict(dk=H2 + 16)), (sparse_back, dict(dv=G2 + SPARSE_MAP - 16)), (sparse_back, dict(ws=F2 - 16)), (sparse_back, dict(ws=J2 + 16)),
+         (sparse_back, dict(dq=D2 - 16))]
+
+
+@pytest.mark.parametrize("call,change", PARTS, ids=lambda v: getattr(v, "__name__", None) or str(v))
+def test_outputs_that_share_memory(lib, call, change):
+    assert call(lib, **change) == ARG
+
+
+def test_neighbours_share_nothing(lib):
+    """Outputs that begin where an input ends, and the other way round, are fine."""
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    fine = (sa.ERR_CUDA, sa.ERR_ARCH)
+    assert norm(lib, y=A + NORM) in fine and norm(lib, y=C2 - NORM) in fine
+    assert drop(lib, per_image=12, y=A + DROP) in fine and drop(lib, per_image=12, rng=C2 + DROP) in fine
+    assert sparse(lib, out=C2 + SPARSE_MAP) in fine and sparse_back(lib, dk=H2 + SPARSE_MAP, dv=H2 - SPARSE_MAP) in fine
 
 
 @pytest.mark.parametrize("call,change,status", [(f, c, s) for f, cases in CASES.items() for c, s in cases],
