@@ -637,23 +637,25 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_b
     }
 }
 
-// dbeta and dgamma: the chunks' sums, added up in their order.  32 of the 2 C columns a block, 32 rows at a time.
-__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* channels, long long chunks, int C, float* dgamma, float* dbeta)
+// dbeta and dgamma: the chunks' sums, added up in their order.  32 of the 2 C columns a block, kWeightRows rows at a time.  It runs beside the second pass,
+// which it takes nothing from: all of that pass's CTAs have waited for the first when it starts.  It waits for the second at its end.
+constexpr int kWeightRows = 8;
+__global__ void __launch_bounds__(32 * kWeightRows) norm_weight_kernel(const float* channels, long long chunks, int C, float* dgamma, float* dbeta)
 {
-    __shared__ float part[32][33];
-    grid_dependency_wait();
+    __shared__ float part[kWeightRows][32];
     const int c = blockIdx.x * 32 + threadIdx.x;
     float s = 0.0f;
     if (c < 2 * C)
 #pragma unroll 8
-        for (long long r = threadIdx.y; r < chunks; r += 32) s += channels[(size_t)r * 2 * C + c];
+        for (long long r = threadIdx.y; r < chunks; r += kWeightRows) s += channels[(size_t)r * 2 * C + c];
     part[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
-    s = part[threadIdx.x][threadIdx.y];                             // a warp a column
+    if (threadIdx.y == 0 && c < 2 * C) {
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const int column = blockIdx.x * 32 + threadIdx.y;
-    if (threadIdx.x == 0 && column < 2 * C) (column < C ? dbeta : dgamma)[column < C ? column : column - C] = s;
+        for (int i = 1; i < kWeightRows; ++i) s += part[i][threadIdx.x];
+        (c < C ? dbeta : dgamma)[c < C ? c : c - C] = s;
+    }
+    grid_dependency_wait();
 }
 
 // False where a pixel has too many columns for a CTA, or the call too many CTAs for a grid.  `maps`: 1 forward, 2 backward.
@@ -801,7 +803,7 @@ cudaError_t launch_group_norm_backward(const void* x, const float* gamma, const 
     if (e != cudaSuccess || !dgamma) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((2 * C + 31) / 32));
-    cfg.blockDim = dim3(32, 32);
+    cfg.blockDim = dim3(32, kWeightRows);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

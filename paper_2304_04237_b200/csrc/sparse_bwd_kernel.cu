@@ -66,6 +66,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
     constexpr float scale = root<D>();
 
     grid_dependency_wait();
+    grid_launch_dependents();                                // the keys' kernel needs nothing of this one
     P pipe(smem, units, chain);
     if (warp == kThreads / 32) {
         pipe.copy_all(g, q, dout, k, v, idx);
@@ -181,10 +182,11 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
     const bool copying = warp == kThreads / 32;
     constexpr float scale = root<D>();
 
-    grid_dependency_wait();
+    // No wait here: this kernel starts when every CTA of the queries' kernel has waited for what was launched before the two, and takes nothing
+    // from it.  The wait for it is at the end.
     Unit unit;
     unit.find(g, blockIdx.x);
-    if (unit.rows <= 0) return;
+    if (unit.rows <= 0) return;                              // (part 0 of each block has rows)
     const size_t plane = unit.plane(g, D);
     const unsigned pixel_bytes = (unsigned)(g.heads * D * (int)sizeof(T));
     if (copying) {
@@ -334,6 +336,7 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
         }
         __syncthreads();                                     // the list is free again
     }
+    if (copying) grid_dependency_wait();                     // complete only when the queries' kernel is
     if (copying || !busy) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
