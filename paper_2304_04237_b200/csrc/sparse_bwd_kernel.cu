@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* 
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 3 : D == 64 ? 3 : 4)
-sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, const T* dout, const float2* stats, T* dq)
+sparse_queries_kernel(const Geometry g, unsigned units, const T* q, const T* k, const T* v, const int* idx, const T* dout, const float2* stats, T* dq)
 {
     using P = BackwardPipe<T, D>;
     using L = Layout<T, D>;
@@ -67,7 +67,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, int chain, const T* q, c
 
     grid_dependency_wait();
     grid_launch_dependents();                                // the keys' kernel needs nothing of this one
-    P pipe(smem, units, chain);
+    P pipe(smem, units);
     if (warp == kThreads / 32) {
         pipe.copy_all(g, q, dout, k, v, idx);
         return;
@@ -354,25 +354,18 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
 template <typename T, int D>
 cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, float2* stats, int sms, cudaStream_t stream) {
     constexpr size_t smem_q = BackwardPipe<T, D>::kSmem, smem_k = KeysPlan<T, D>::kSmem;
-    static bool ready[64] = {};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    int ctas = 0, ctas_k = 0;
+    cudaError_t e = resident<sparse_queries_kernel<T, D>, smem_q>(sms, &ctas);
+    if (e == cudaSuccess) e = resident<sparse_keys_kernel<T, D>, smem_k>(sms, &ctas_k);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !ready[dev]) {
-        e = cudaFuncSetAttribute(sparse_queries_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_q);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(sparse_keys_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_k);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) ready[dev] = true;
-    }
-    const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads);
-    const int chain = chain_of(g, units, sms, BackwardPipe<T, D>::N);
+    const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads), grid = units < (unsigned)ctas ? units : (unsigned)ctas;
     const long long n = B * g.H * g.W * g.heads;
     auto in = [](const void* p) { return static_cast<const T*>(p); };
     auto to = [](void* p) { return static_cast<T*>(p); };
     constexpr long long rows = 256 / (D * sizeof(T) / 16) * 4;      // of a block
     e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + rows - 1) / rows)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats);
     if (e != cudaSuccess) return e;
-    e = launch_chained(sparse_queries_kernel<T, D>, dim3((units + chain - 1) / chain), kBlock, smem_q, stream, g, units, chain, in(m.q), in(m.k),
+    e = launch_chained(sparse_queries_kernel<T, D>, dim3(grid), kBlock, smem_q, stream, g, units, in(m.q), in(m.k),
                        in(m.v), m.idx, in(m.dout), static_cast<const float2*>(stats), to(m.dq));
     if (e != cudaSuccess) return e;
     return launch_chained(sparse_keys_kernel<T, D>, dim3(units), kBlock, smem_k, stream, g, in(m.q), in(m.k), in(m.v), m.idx,

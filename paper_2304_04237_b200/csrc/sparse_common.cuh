@@ -9,6 +9,7 @@
 // bf16: mma.sync m16n8k16 on the tiles as they are.  fp32: every tile is cut into three bf16 planes in shared memory, once for the four
 // warps (split.cuh: exact), and a product is six bf16 products, down to 2^-24 of it.
 #pragma once
+#include <atomic>
 #include <type_traits>
 
 #include "common.cuh"
@@ -473,9 +474,11 @@ template <typename T, int D, int N> struct Sender {
     }
 };
 
-// What the kernels that keep queries share: a CTA takes `chain` neighbouring units one after the other, and the copies run ahead of the
+// What the kernels that keep queries share: a CTA takes its even share of the units, neighbours, one after the other, and the copies run ahead of the
 // arithmetic across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
-// trips to memory.  A unit begins with the step (or steps) that bring the rows that stay.
+// trips to memory.  There are as many CTAs as the SMs hold.  (Several times as many, of up to eight units, took 85.2 us instead of 82.6 for the
+// forward of 64 x 56 x 56, 3 heads, bf16, and 161 instead of 155.5 for 32 x 28 x 42, 3 heads of 64, bf16, forward and backward.)
+// A unit begins with the step (or steps) that bring the rows that stay.
 //   own0, own1: the rows that stay (queries; gradients of the output, or null);  k, v: the tiles.
 template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
     using L = Layout<T, D>;
@@ -497,10 +500,11 @@ template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
     int items;
     int slot;                                                                        // the computing warps' stage
 
-    __device__ __forceinline__ QueryPipe(unsigned char* memory, unsigned units, int chain) : smem(memory) {
+    __device__ __forceinline__ QueryPipe(unsigned char* memory, unsigned units) : smem(memory) {
         base = smem_u32(memory);
-        first = blockIdx.x * (unsigned)chain;
-        items = (int)min((unsigned)chain, units - first);
+        const unsigned each = units / gridDim.x, more = units - each * gridDim.x;     // `more` CTAs take one more
+        first = blockIdx.x * each + min(blockIdx.x, more);
+        items = (int)each + (blockIdx.x < more);
         slot = 0;
     }
     // Rows of a unit's list, known when its first step has arrived.
@@ -618,12 +622,22 @@ template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {
     }
 };
 
-// Units a CTA takes one after the other: enough for some ten tiles, while the CTAs still fill the SMs a few times over.
-inline int chain_of(const Geometry& g, unsigned units, int sms, int tile) {
-    const int steps = (g.top * g.bh * g.bw + tile - 1) / tile;
-    int chain = 1;
-    while (chain < 8 && chain * steps < 10 && units / (2 * chain) >= 8u * (unsigned)sms) chain *= 2;
-    return chain;
+// How many CTAs of a kernel the current device holds at once, with `Smem` bytes of shared memory each; set up on a device's first call.
+template <auto Kernel, size_t Smem> cudaError_t resident(int sms, int* ctas) {
+    static std::atomic<int> known[64];                     // of an SM
+    int dev = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) n = known[dev].load(std::memory_order_acquire);
+    if (n == 0) {
+        e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, kBlock, Smem);
+        if (e != cudaSuccess) return e;
+        if (n < 1) n = 1;
+        if (dev < 64) known[dev].store(n, std::memory_order_release);
+    }
+    *ctas = n * sms;
+    return cudaSuccess;
 }
 
 // Two neighbouring values of a row.

@@ -15,7 +15,7 @@ template <typename T, int D> using ForwardPipe = QueryPipe<T, D, sizeof(T) == 4 
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kBlock, sizeof(T) == 4 || D == 64 ? 3 : 4)
-sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, const T* k, const T* v, const int* idx, T* out, float* lse)
+sparse_forward_kernel(const Geometry g, unsigned units, const T* q, const T* k, const T* v, const int* idx, T* out, float* lse)
 {
     using P = ForwardPipe<T, D>;
     using L = Layout<T, D>;
@@ -25,7 +25,7 @@ sparse_forward_kernel(const Geometry g, unsigned units, int chain, const T* q, c
     constexpr float scale = root<D>() * kLog2e;
 
     grid_dependency_wait();
-    P pipe(smem, units, chain);
+    P pipe(smem, units);
     if (warp == kThreads / 32) {
         pipe.copy_all(g, q, nullptr, k, v, idx);
         return;
@@ -143,18 +143,11 @@ template <typename T, int D>
 cudaError_t launch_forward(const Geometry& g, long long B, const void* q, const void* k, const void* v, const int* idx, void* out, float* lse, int sms,
                            cudaStream_t stream) {
     constexpr size_t smem = ForwardPipe<T, D>::kSmem;
-    static bool ready[64] = {};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    int ctas = 0;
+    const cudaError_t e = resident<sparse_forward_kernel<T, D>, smem>(sms, &ctas);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !ready[dev]) {
-        e = cudaFuncSetAttribute(sparse_forward_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) ready[dev] = true;
-    }
-    const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads);
-    const int chain = chain_of(g, units, sms, ForwardPipe<T, D>::N);
-    return launch_chained(sparse_forward_kernel<T, D>, dim3((units + chain - 1) / chain), kBlock, smem, stream, g, units, chain,
+    const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads), grid = units < (unsigned)ctas ? units : (unsigned)ctas;
+    return launch_chained(sparse_forward_kernel<T, D>, dim3(grid), kBlock, smem, stream, g, units,
                           static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), idx, static_cast<T*>(out), lse);
 }
 
