@@ -83,6 +83,7 @@ bool poolable(const sparse::Geometry& g, long long B, int head_dim) { return B *
 
 size_t map_bytes(const sparse::Geometry& g, int B, int head_dim, slide_attn_dtype t) { return (size_t)B * g.H * g.W * g.heads * head_dim * size_of(t); }
 size_t lse_bytes(const sparse::Geometry& g, int B) { return (size_t)B * g.H * g.W * g.heads * sizeof(float); }
+size_t backward_bytes(const sparse::Geometry& g, int B) { return 2 * lse_bytes(g, B) + 16; }
 size_t list_bytes(const sparse::Geometry& g, int B) { return (size_t)B * g.heads * g.blocks * g.top * sizeof(int); }
 size_t pooled_bytes(const sparse::Geometry& g, int B, int head_dim) { return 2 * (size_t)B * g.heads * g.blocks * head_dim * sizeof(double); }
 
@@ -242,7 +243,7 @@ slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, in
     if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
     sparse::Geometry g;
     const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
-    if (st == SLIDE_ATTN_OK) *bytes = 2 * lse_bytes(g, B);
+    if (st == SLIDE_ATTN_OK) *bytes = backward_bytes(g, B);
     return st;
 }
 
@@ -258,11 +259,11 @@ slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const
     slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
     if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st != SLIDE_ATTN_OK) return st;
-    if (workspace_bytes < 2 * lse_bytes(g, B)) return SLIDE_ATTN_ERR_INVALID_ARG;
+    if (workspace_bytes < backward_bytes(g, B)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (any_misaligned(q, k, v, idx, out, lse, dout, dq, dk, dv) || misaligned(workspace)) return SLIDE_ATTN_ERR_ALIGNMENT;
     const size_t map = map_bytes(g, B, head_dim, dtype);
     const Span sq(q, map), sk(k, map), sv(v, map), si(idx, list_bytes(g, B)), so(out, map), sl(lse, lse_bytes(g, B)), sd(dout, map), sdq(dq, map),
-        sdk(dk, map), sdv(dv, map), sw(workspace, 2 * lse_bytes(g, B));
+        sdk(dk, map), sdv(dv, map), sw(workspace, backward_bytes(g, B));
     for (const Span& o : {sdq, sdk, sdv, sw})
         if (meets(o, sq, sk, sv, si, so, sl, sd)) return SLIDE_ATTN_ERR_INVALID_ARG;
     if (meets(sdq, sdk, sdv, sw) || meets(sdk, sdv, sw) || meets(sdv, sw)) return SLIDE_ATTN_ERR_INVALID_ARG;

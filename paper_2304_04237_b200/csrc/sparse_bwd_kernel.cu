@@ -6,6 +6,9 @@
 // Three launches: each query's logarithm and delta, side by side; queries (dq, over the blocks of their list); keys (dk and dv, over the blocks of
 // queries whose lists name the key's block, found by going through the image's lists in their order).  None adds to memory that
 // another CTA writes, so results do not depend on which CTA runs first.
+// Bound by latency: a warp's products, exponentials and products again wait for one another, and registers allow 12 to 16 such warps an SM.  128 x 128 x 2,
+// 3 heads, bf16, lists of 16 blocks of 8 x 8: queries 74 us, keys 104 (tensor pipe 50 and 44 %, issue slots 40 and 33 %); with the forward 231 in all, of 27 for the
+// products at the rate of large matrices.
 #include "operators.cuh"
 
 namespace slide_attn {
@@ -33,10 +36,11 @@ template <> __device__ __forceinline__ float dot_piece<__nv_bfloat16>(const __nv
 
 // Less each query's logarithm of the sum (base 2), and less its delta: a query and head by as many neighbouring lanes as it has 16-byte pieces.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats)
+__global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats, unsigned* taken)
 {
     constexpr int kPiece = 16 / sizeof(T), kLanes = D / kPiece, kEach = 4, kAtOnce = 256 / kLanes;
     grid_dependency_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *taken = 0;
     const int lane = threadIdx.x % kLanes;
     const long long first = (long long)blockIdx.x * (kAtOnce * kEach) + threadIdx.x / kLanes;
     float s[kEach];
@@ -151,129 +155,172 @@ sparse_queries_kernel(const Geometry g, unsigned units, const T* q, const T* k, 
     }
 }
 
-constexpr int kScanEach = 8, kScan = kScanEach * kThreads;      // entries of the image's lists that the keys' kernel looks at in one go
-constexpr int kListed = kScan + 512;                            // entries that it lists before it goes through them
+constexpr int kScanEach = 2, kScan = 128 * kScanEach;    // entries of the image's lists that are looked at in one go: four neighbours a lane, again and again
+constexpr int kListed = 4 * kScan;                              // entries that a table holds
 
+// Shared memory of the keys' kernel: the pipe's, two tables, of each stage the queries' numbers (less the logarithms, then less the deltas) and a
+// word on what the stage holds.
 template <typename T, int D> struct KeysPlan {
-    using L = Layout<T, D>;
-    static constexpr int N = BackwardPipe<T, D>::N, S = BackwardPipe<T, D>::S;
-    static constexpr uint32_t kTile = N * L::kRowBytes, kStage = 2 * kTile, kOwn = kRows * L::kRowBytes;
-    static constexpr uint32_t kPlane = 2 * N * 2 * D, kOwnPlane = kRows * 2 * D, kBehind = L::kSplit ? kPlane / 2 : kTile;
-    // fp32: the rows that stay arrive where the stages are, and what stays are their planes
-    static constexpr uint32_t kPartsAt = S * kStage, kOwnAt = L::kSplit ? 0 : kPartsAt, kOwnPartsAt = kPartsAt + (L::kSplit ? 3 * kPlane : 0);
-    static constexpr uint32_t kListAt = kOwnPartsAt + (L::kSplit ? 6 * kOwnPlane : 2 * kOwn), kStatsAt = kListAt + kListed * sizeof(Entry);
-    static constexpr size_t kSmem = kStatsAt + S * N * sizeof(float2);
-    static_assert(!L::kSplit || 2 * kOwn <= kPartsAt, "room for the rows that stay");
+    using P = BackwardPipe<T, D>;
+    static constexpr uint32_t kListAt = (uint32_t)(P::kSmem + 15) / 16 * 16, kStatsAt = kListAt + 2 * kListed * sizeof(Entry);
+    static constexpr uint32_t kWordsAt = kStatsAt + P::S * P::N * sizeof(float2);
+    static constexpr size_t kSmem = kWordsAt + P::S * sizeof(unsigned);
+};
+constexpr unsigned kLast = 1u << 16;                            // the unit's last tile; below: its rows
+
+// The blocks of queries that see a block, in the order of the lists, found by a warp.
+struct Seers {
+    Unit unit;
+    Entry* table;
+    int seen, n, total;                                         // entries looked at; of the table; their rows
+    int4 mine[kScanEach];
+    __device__ __forceinline__ void begin(const Geometry& g, unsigned u, Entry* room) {
+        unit.find(g, u);
+        table = room;
+        seen = n = total = 0;
+    }
+    __device__ __forceinline__ bool room(const Geometry& g) const { return seen < g.blocks * g.top && n + kScan <= kListed; }
+    // Entries sent for, and looked at.
+    __device__ __forceinline__ void read(const Geometry& g, const int* idx, int lane) {
+        const int entries = g.blocks * g.top;
+        const int* lists = idx + unit.list * (unsigned)entries;
+#pragma unroll
+        for (int e = 0; e < kScanEach; ++e) {
+            const int i = seen + e * 128 + lane * 4;
+            mine[e] = make_int4(-1, -1, -1, -1);
+            if (entries % 4 == 0) {
+                if (i < entries) mine[e] = *reinterpret_cast<const int4*>(lists + i);
+            } else {
+                if (i < entries) mine[e].x = lists[i];
+                if (i + 1 < entries) mine[e].y = lists[i + 1];
+                if (i + 2 < entries) mine[e].z = lists[i + 2];
+                if (i + 3 < entries) mine[e].w = lists[i + 3];
+            }
+        }
+    }
+    __device__ __forceinline__ void look(const Geometry& g, int lane) {
+#pragma unroll
+        for (int e = 0; e < kScanEach; ++e) {
+            const int4 m = mine[e];
+            const bool is[4] = {m.x == unit.r, m.y == unit.r, m.z == unit.r, m.w == unit.r};
+            if (!__any_sync(0xffffffffu, is[0] || is[1] || is[2] || is[3])) continue;
+            Block block[4] = {};
+            unsigned own = 0;                                    // blocks << 24 | rows
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (is[j]) {
+                    block[j] = block_of(g, (int)g.by_top.quotient((unsigned)(seen + e * 128 + lane * 4 + j)));
+                    own += (1u << 24) + (unsigned)block[j].size();
+                }
+            unsigned before = own;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const unsigned x = __shfl_up_sync(0xffffffffu, before, d);
+                if (lane >= d) before += x;
+            }
+            const unsigned all = __shfl_sync(0xffffffffu, before, 31);
+            before -= own;
+            int place = n + (int)(before >> 24), end = total + (int)(before & 0xFFFFFFu);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (is[j]) {
+                    end += block[j].size();
+                    table[place++] = Entry::of(g, block[j], end);
+                }
+            n += (int)(all >> 24);
+            total += (int)(all & 0xFFFFFFu);
+        }
+        seen += kScan;
+    }
 };
 
+// What the copying warp of the keys' kernel does.  Units are taken from a counter, one ahead: how many blocks see a block is known only when the lists have been
+// gone through, and a fixed share of the units would leave the CTAs with the sought-after blocks behind.  While a unit's tiles are sent for, the next one's
+// lists are gone through, a part beside each tile.
 template <typename T, int D>
-__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 2 : D == 64 ? 2 : 3)
-sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const int* idx, const float2* stats, const T* dout, T* dk, T* dv)
-{
+__device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, unsigned char* smem, const T* q, const T* k, const T* v, const int* idx,
+                                           const float2* stats, const T* dout, unsigned* taken) {
     using K = KeysPlan<T, D>;
-    using L = Layout<T, D>;
-    constexpr int N = K::N, NT = N / 8, S = K::S;
-    extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ unsigned warp_sums[kThreads / 32];
+    using P = BackwardPipe<T, D>;
+    constexpr int N = P::N;
+    const int lane = threadIdx.x % 32;
     const uint32_t base = smem_u32(smem);
-    Entry* list = reinterpret_cast<Entry*>(smem + K::kListAt);
-    const float* columns = reinterpret_cast<const float*>(smem + K::kStatsAt);          // of each stage: less the logarithms, then less the deltas
-    const int warp = uniform((int)threadIdx.x / 32), lane = threadIdx.x % 32;
-    const bool copying = warp == kThreads / 32;
-    constexpr float scale = root<D>();
-
-    // No wait here: this kernel starts when every CTA of the queries' kernel has waited for what was launched before the two, and takes nothing
-    // from it.  The wait for it is at the end.
-    Unit unit;
-    unit.find(g, blockIdx.x);
-    if (unit.rows <= 0) return;                              // (part 0 of each block has rows)
-    const size_t plane = unit.plane(g, D);
+    Entry* tables = reinterpret_cast<Entry*>(smem + K::kListAt);
+    unsigned* words = reinterpret_cast<unsigned*>(smem + K::kWordsAt);
     const unsigned pixel_bytes = (unsigned)(g.heads * D * (int)sizeof(T));
-    if (copying) {
-        unsigned pixels[kRows / 32];
-#pragma unroll
-        for (int i = 0; i < kRows / 32; ++i) pixels[i] = unit.pixel(g, lane + 32 * i);
-        Sender<T, D, kRows>::send(base + K::kOwnAt, base + K::kOwnAt + K::kOwn, k + plane, v + plane, pixel_bytes, pixels, unit.rows, lane);
-        copies_commit();
-    }
-    const bool busy = warp * 16 < unit.rows;
-    Rows<D, L::kPlanes> rows_k, rows_v;
-    float dks[D / 8][4] = {}, dvs[D / 8][4] = {};
-    const pair scales = make_pair(scale * kLog2e, scale * kLog2e);
-    const int* lists = idx + unit.list * (unsigned)(g.blocks * g.top);
-    const int entries = g.blocks * g.top;
-    for (int seen = 0; seen < entries;) {
-        // the next blocks of queries that see this block, in an order that the lists alone decide
-        const bool start = seen == 0;
-        unsigned listed = 0;                                 // blocks << 21 | rows: at most 1536 blocks of 1024
-        do {
-            int mine[kScanEach];
-            unsigned sum = 0;
-            if (!copying) {
-#pragma unroll
-                for (int e = 0; e < kScanEach; ++e) {
-                    const int i = seen + e * kThreads + (int)threadIdx.x;
-                    mine[e] = i < entries ? lists[i] : -1;
-                }
-#pragma unroll
-                for (int e = 0; e < kScanEach; ++e) {
-                    const bool is = mine[e] == unit.r;
-                    mine[e] = is ? (int)g.by_top.quotient((unsigned)(seen + e * kThreads) + threadIdx.x) : -1;
-                    if (is) sum += (1u << 21) + (unsigned)block_of(g, mine[e]).size();
-                }
-            }
-            unsigned before = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const unsigned x = __shfl_up_sync(0xffffffffu, before, o);
-                if (lane >= o) before += x;
-            }
-            if (lane == 31 && !copying) warp_sums[warp] = before;
-            __syncthreads();
-            before += listed - sum;
-#pragma unroll
-            for (int w = 0; w < kThreads / 32; ++w) {
-                if (w < warp) before += warp_sums[w];
-                listed += warp_sums[w];
-            }
-            if (!copying) {
-#pragma unroll
-                for (int e = 0; e < kScanEach; ++e)
-                    if (mine[e] >= 0) {
-                        const Block block = block_of(g, mine[e]);
-                        const unsigned place = before >> 21;
-                        before += (1u << 21) + (unsigned)block.size();
-                        list[place] = Entry::of(g, block, (int)(before & 0x1FFFFFu));
-                    }
-            }
-            seen += kScan;
-            if (start && copying) copies_wait<0>();
-            __syncthreads();
-        } while (seen < entries && (int)(listed >> 21) + kScan <= kListed);
-        if (start) {                                         // the rows that stay have arrived
-            if (!copying) {
-                if constexpr (L::kSplit)
-#pragma unroll
-                    for (int o = 0; o < 2; ++o) cut_rows<D, kRows>(base + K::kOwnAt + o * K::kOwn, base + K::kOwnPartsAt + o * 3 * K::kOwnPlane);
-                rows_k.load(L::kSplit ? base + K::kOwnPartsAt : base + K::kOwnAt, K::kOwnPlane, warp * 16, lane);
-                rows_v.load(L::kSplit ? base + K::kOwnPartsAt + 3 * K::kOwnPlane : base + K::kOwnAt + K::kOwn, K::kOwnPlane, warp * 16, lane);
-            }
-            if constexpr (L::kSplit) __syncthreads();        // the stages are free
+    Ring<P::S> ring;
+    auto ask = [&]() { return lane == 0 ? atomicAdd(taken, 1u) : 0u; };
+    auto take = [&](unsigned asked) {                            // the next unit that has rows
+        for (;;) {
+            const unsigned u = __shfl_sync(0xffffffffu, asked, 0);
+            if (u >= units) return units;
+            Unit unit;
+            unit.find(g, u);
+            if (unit.rows > 0) return u;
+            asked = ask();
         }
-        const int total = uniform((int)(listed & 0x1FFFFFu));
-        if (copying) {
-            Ring<S> ring;
-            Cursor cursor;
-            cursor.reset(list);
-            const float2* from_stats = stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
+    };
+    Seers next;
+    unsigned u = take(ask()), turn = 0;
+    if (u < units) next.begin(g, u, tables);
 #pragma unroll 1
-            for (int done = 0; done < total; done += N) {
+    while (u < units) {
+        const Unit unit = next.unit;
+        Entry* const table = next.table;
+        const unsigned asked = ask();                            // for the unit after this one, on its way
+        // the rows that stay
+        const size_t plane = unit.plane(g, D);
+        {
+            unsigned pixels[kRows / 32];
+#pragma unroll
+            for (int i = 0; i < kRows / 32; ++i) pixels[i] = unit.pixel(g, lane + 32 * i);
+#pragma unroll
+            for (int o = 0; o < P::kOwnSteps; ++o) {
+                ring.claim();
+                const uint32_t stage = base + (uint32_t)ring.slot * P::kStage;
+                if (lane == 0) words[ring.slot] = u;
+                if constexpr (P::kOwnSteps == 1)
+                    Sender<T, D, kRows>::send(stage, stage + P::kOwn, k + plane, v + plane, pixel_bytes, pixels, unit.rows, lane);
+                else
+                    Sender<T, D, kRows>::send(stage, 0, (o ? v : k) + plane, nullptr, pixel_bytes, pixels, unit.rows, lane);
+                ring.commit();
+            }
+        }
+        if (next.room(g)) ring.drain();
+        const float2* from_stats = stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
+        bool last = false, ahead = false;                        // ahead: `next` is the unit after this one
+        unsigned u_next = units;
+        while (!last) {
+            // what is left of this unit's lists, as far as the table goes
+            while (next.room(g)) {
+                next.read(g, idx, lane);
+                next.look(g, lane);
+            }
+            __syncwarp();
+            const int total = next.total;
+            const bool whole = next.seen >= g.blocks * g.top;    // no more tables of this unit
+            if (whole) {
+                u_next = take(asked);
+                ahead = u_next < units;
+                if (ahead) next.begin(g, u_next, tables + (turn ^= 1u) * kListed);
+            }
+            const int looks = max((g.blocks * g.top / kScan + 1) * N / max(total, 1), 1);       // at each tile: about all of the lists in all
+            Cursor cursor;
+            cursor.reset(table);
+            int done = 0;
+#pragma unroll 1
+            do {
+                if (done >= total && !whole) break;              // an empty table, and more of them
+                const bool look = ahead && next.room(g);
+                if (look) next.read(g, idx, lane);               // on its way while this tile is sent for
                 unsigned pixels[N / 32];
 #pragma unroll
                 for (int i = 0; i < N / 32; ++i) pixels[i] = done + 32 * i + lane < total ? cursor.pixel(g, done + 32 * i + lane) : 0u;
                 ring.claim();
-                const uint32_t stage = base + (uint32_t)ring.slot * K::kStage, at = base + K::kStatsAt + (uint32_t)(ring.slot * 2 * N * 4);
-                Sender<T, D, N>::send(stage, stage + K::kTile, q + plane, dout + plane, pixel_bytes, pixels, total - done, lane);
+                last = whole && done + N >= total;
+                if (lane == 0) words[ring.slot] = (unsigned)max(min(N, total - done), 0) | (last ? kLast : 0u);
+                const uint32_t stage = base + (uint32_t)ring.slot * P::kStage, at = base + K::kStatsAt + (uint32_t)(ring.slot * 2 * N * 4);
+                if (total > 0) Sender<T, D, N>::send(stage, stage + P::kTile, q + plane, dout + plane, pixel_bytes, pixels, total - done, lane);
 #pragma unroll
                 for (int i = 0; i < N / 32; ++i)
                     if (done + 32 * i + lane < total) {
@@ -282,30 +329,83 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
                         copy4(at + (N + 32 * i + lane) * 4, from + 1);
                     }
                 ring.commit();
-            }
-            ring.finish();
-        } else {
-            int slot = 0;
+                if (look) next.look(g, lane);
 #pragma unroll 1
-            for (int done = 0; done < total; done += N) {
-                bar_sync<kBlock>(Ring<S>::full(slot));
-                uint32_t tile = base + (uint32_t)slot * K::kStage;
-                if constexpr (L::kSplit) {
-                    compute_sync();
-                    cut_rows<D, 2 * N>(tile, base + K::kPartsAt);
-                    compute_sync();
-                    tile = base + K::kPartsAt;
+                for (int i = 1; i < looks && ahead && next.room(g); ++i) {
+                    next.read(g, idx, lane);
+                    next.look(g, lane);
                 }
-                const pair* stat = reinterpret_cast<const pair*>(columns + slot * 2 * N) + (lane & 3);       // of two queries each
-                const int used = min(N, total - done);
+                done += N;
+            } while (done < total);
+            __syncwarp();                                        // the table is free again
+            if (!whole) next.n = next.total = 0;
+        }
+        u = u_next;
+    }
+    ring.claim();
+    if (lane == 0) words[ring.slot] = units;                     // no more
+    ring.commit();
+    ring.finish();
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 2 : D == 64 ? 2 : 3)
+sparse_keys_kernel(const Geometry g, unsigned units, const T* q, const T* k, const T* v, const int* idx, const float2* stats, const T* dout, T* dk, T* dv,
+                   unsigned* taken)
+{
+    using K = KeysPlan<T, D>;
+    using P = BackwardPipe<T, D>;
+    using L = Layout<T, D>;
+    constexpr int N = P::N, NT = N / 8;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int warp = uniform((int)threadIdx.x / 32), lane = threadIdx.x % 32;
+    constexpr float scale = root<D>();
+
+    // No wait here: this kernel starts when every CTA of the queries' kernel has waited for what was launched before the two, and takes nothing
+    // from it.  The wait for it is at the end.
+    if (warp == kThreads / 32) {
+        send_seers<T, D>(g, units, smem, q, k, v, idx, stats, dout, taken);
+        grid_dependency_wait();                              // complete only when the queries' kernel is
+        return;
+    }
+    P pipe(smem, units);
+    const float* columns = reinterpret_cast<const float*>(smem + K::kStatsAt);          // of each stage: less the logarithms, then less the deltas
+    const unsigned* words = reinterpret_cast<const unsigned*>(smem + K::kWordsAt);
+    const pair scales = make_pair(scale * kLog2e, scale * kLog2e);
+    for (;;) {
+        uint32_t own = pipe.next();
+        const unsigned u = (unsigned)uniform((int)words[pipe.slot]);
+        if (u >= units) {
+            pipe.release();
+            return;
+        }
+        Unit unit;
+        unit.find(g, u);
+        const bool busy = warp * 16 < unit.rows;
+        Rows<D, L::kPlanes> rows_k, rows_v;
+        float dks[D / 8][4] = {}, dvs[D / 8][4] = {};
+#pragma unroll
+        for (int o = 0; o < P::kOwnSteps; ++o) {
+            if (o) own = pipe.next();
+            pipe.take(own, o, warp * 16, lane, rows_k, &rows_v);
+            pipe.release();
+        }
+        for (bool last = false; !last;) {
+            const uint32_t at = pipe.next();
+            const unsigned word = (unsigned)uniform((int)words[pipe.slot]);
+            const int used = (int)(word & (kLast - 1u));
+            last = word >= kLast;
+            if (used > 0) {
+                const uint32_t tile = pipe.tile(at);
+                const pair* stat = reinterpret_cast<const pair*>(columns + pipe.slot * 2 * N) + (lane & 3);       // of two queries each
                 if (busy) with_width<NT>(used, [&](auto width, auto partial) {
                     constexpr int W = decltype(width)::value;
 #pragma unroll (L::kSplit ? 1 : W / 2)
                     for (int n = 0; n < W; n += 2) {             // 16 columns at a time
                         float s[2][4], dp[2][4];
                         const uint32_t at16 = tile + n * 8 * 2 * D;
-                        scores16<D, L::kPlanes>(rows_k, at16, K::kPlane, lane, s[0], s[1]);
-                        scores16<D, L::kPlanes>(rows_v, at16 + K::kBehind, K::kPlane, lane, dp[0], dp[1]);
+                        scores16<D, L::kPlanes>(rows_k, at16, P::kPlane, lane, s[0], s[1]);
+                        scores16<D, L::kPlanes>(rows_v, at16 + P::kBehind, P::kPlane, lane, dp[0], dp[1]);
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             const pair sums = stat[(n + j) * 4], deltas = stat[N / 2 + (n + j) * 4];
@@ -326,33 +426,31 @@ sparse_keys_kernel(const Geometry g, const T* q, const T* k, const T* v, const i
                                 for (int e = 0; e < 4; ++e)
                                     if ((n + j) * 8 + 2 * (lane & 3) + (e & 1) >= used) s[j][e] = dp[j][e] = 0.0f;
                         }
-                        gather16<D, L::kPlanes>(s[0], s[1], at16 + K::kBehind, K::kPlane, lane, dvs);
-                        gather16<D, L::kPlanes>(dp[0], dp[1], at16, K::kPlane, lane, dks);
+                        gather16<D, L::kPlanes>(s[0], s[1], at16 + P::kBehind, P::kPlane, lane, dvs);
+                        gather16<D, L::kPlanes>(dp[0], dp[1], at16, P::kPlane, lane, dks);
                     }
                 });
-                bar_arrive<kBlock>(Ring<S>::empty(slot));
-                slot = Ring<S>::after(slot);
             }
+            pipe.release();
         }
-        __syncthreads();                                     // the list is free again
-    }
-    if (copying) grid_dependency_wait();                     // complete only when the queries' kernel is
-    if (copying || !busy) return;
+        if (!busy) continue;
+        const size_t plane = unit.plane(g, D);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int row = warp * 16 + i * 8 + (lane >> 2);
-        if (row >= unit.rows) continue;
-        const size_t at = plane + (size_t)unit.pixel(g, row) * (unsigned)(g.heads * D) + 2 * (lane & 3);
+        for (int i = 0; i < 2; ++i) {
+            const int row = warp * 16 + i * 8 + (lane >> 2);
+            if (row >= unit.rows) continue;
+            const size_t at = plane + (size_t)unit.pixel(g, row) * (unsigned)(g.heads * D) + 2 * (lane & 3);
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n) {
-            store2(dk + at + n * 8, dks[n][2 * i] * scale, dks[n][2 * i + 1] * scale);
-            store2(dv + at + n * 8, dvs[n][2 * i], dvs[n][2 * i + 1]);
+            for (int n = 0; n < D / 8; ++n) {
+                store2(dk + at + n * 8, dks[n][2 * i] * scale, dks[n][2 * i + 1] * scale);
+                store2(dv + at + n * 8, dvs[n][2 * i], dvs[n][2 * i + 1]);
+            }
         }
     }
 }
 
 template <typename T, int D>
-cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, float2* stats, int sms, cudaStream_t stream) {
+cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, float2* stats, unsigned* taken, int sms, cudaStream_t stream) {
     constexpr size_t smem_q = BackwardPipe<T, D>::kSmem, smem_k = KeysPlan<T, D>::kSmem;
     int ctas = 0, ctas_k = 0;
     cudaError_t e = resident<sparse_queries_kernel<T, D>, smem_q>(sms, &ctas);
@@ -363,13 +461,13 @@ cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& 
     auto in = [](const void* p) { return static_cast<const T*>(p); };
     auto to = [](void* p) { return static_cast<T*>(p); };
     constexpr long long rows = 256 / (D * sizeof(T) / 16) * 4;      // of a block
-    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + rows - 1) / rows)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats);
+    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + rows - 1) / rows)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats, taken);
     if (e != cudaSuccess) return e;
     e = launch_chained(sparse_queries_kernel<T, D>, dim3(grid), kBlock, smem_q, stream, g, units, in(m.q), in(m.k),
                        in(m.v), m.idx, in(m.dout), static_cast<const float2*>(stats), to(m.dq));
     if (e != cudaSuccess) return e;
-    return launch_chained(sparse_keys_kernel<T, D>, dim3(units), kBlock, smem_k, stream, g, in(m.q), in(m.k), in(m.v), m.idx,
-                          static_cast<const float2*>(stats), in(m.dout), to(m.dk), to(m.dv));
+    return launch_chained(sparse_keys_kernel<T, D>, dim3(units < (unsigned)ctas_k ? units : (unsigned)ctas_k), kBlock, smem_k, stream, g, units, in(m.q), in(m.k),
+                          in(m.v), m.idx, static_cast<const float2*>(stats), in(m.dout), to(m.dk), to(m.dv), taken);
 }
 
 }  // namespace sparse
@@ -378,15 +476,16 @@ cudaError_t launch_sparse_backward(sparse::Geometry g, long long B, int head_dim
                                    void* workspace, int sms, cudaStream_t stream) {
     using namespace sparse;
     g.complete();
-    float2* stats = static_cast<float2*>(workspace);
+    float2* stats = static_cast<float2*>(workspace);             // and behind them the counter of the units that are taken
+    unsigned* taken = reinterpret_cast<unsigned*>(stats + B * g.H * g.W * g.heads);
     if (dtype == SLIDE_ATTN_BF16) {
-        if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, stats, sms, stream);
-        if (head_dim == 32) return launch_backward<__nv_bfloat16, 32>(g, B, m, stats, sms, stream);
-        return launch_backward<__nv_bfloat16, 64>(g, B, m, stats, sms, stream);
+        if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, stats, taken, sms, stream);
+        if (head_dim == 32) return launch_backward<__nv_bfloat16, 32>(g, B, m, stats, taken, sms, stream);
+        return launch_backward<__nv_bfloat16, 64>(g, B, m, stats, taken, sms, stream);
     }
-    if (head_dim == 16) return launch_backward<float, 16>(g, B, m, stats, sms, stream);
-    if (head_dim == 32) return launch_backward<float, 32>(g, B, m, stats, sms, stream);
-    return launch_backward<float, 64>(g, B, m, stats, sms, stream);
+    if (head_dim == 16) return launch_backward<float, 16>(g, B, m, stats, taken, sms, stream);
+    if (head_dim == 32) return launch_backward<float, 32>(g, B, m, stats, taken, sms, stream);
+    return launch_backward<float, 64>(g, B, m, stats, taken, sms, stream);
 }
 
 }  // namespace slide_attn

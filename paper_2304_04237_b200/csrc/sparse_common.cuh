@@ -410,7 +410,7 @@ struct Cursor {
 // the next step there when they are done with one.
 template <int S> struct Ring {
     static constexpr int kLate = S - 2;                          // steps between sending for one and handing it over
-    int sent = 0, slot = 0, late_slot = 0;
+    int sent = 0, handed = 0, slot = 0, late_slot = 0;
     static __device__ __forceinline__ int full(int slot) { return 1 + slot; }
     static __device__ __forceinline__ int empty(int slot) { return 1 + S + slot; }
     static __device__ __forceinline__ int after(int slot) { return slot == S - 1 ? 0 : slot + 1; }
@@ -419,21 +419,25 @@ template <int S> struct Ring {
     // ... behind them ...
     __device__ __forceinline__ void commit() {
         copies_commit();
-        if (sent >= kLate) {
-            copies_wait<kLate>();
-            bar_arrive<kBlock>(full(late_slot));
-            late_slot = after(late_slot);
-        }
         slot = after(slot);
-        ++sent;
-    }
-    // ... and at the end: the last steps are handed over, and the barriers are left as they were found.
-    __device__ __forceinline__ void finish() {
-        copies_wait<0>();
-        for (int i = min(sent, kLate); i > 0; --i) {
-            bar_arrive<kBlock>(full(late_slot));
-            late_slot = after(late_slot);
+        if (++sent - handed > kLate) {
+            copies_wait<kLate>();
+            hand_over();
         }
+    }
+    __device__ __forceinline__ void hand_over() {
+        bar_arrive<kBlock>(full(late_slot));
+        late_slot = after(late_slot);
+        ++handed;
+    }
+    // ... before a pause ...
+    __device__ __forceinline__ void drain() {
+        copies_wait<0>();
+        while (handed < sent) hand_over();
+    }
+    // ... and at the end: the barriers are left as they were found.
+    __device__ __forceinline__ void finish() {
+        drain();
         slot = sent >= S ? slot : 0;
         for (int i = min(sent, S); i > 0; --i) {
             bar_sync<kBlock>(empty(slot));

@@ -116,6 +116,22 @@ def test_long_lists_of_queries():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 64])
+def test_more_blocks_than_the_gpu_takes_at_a_time(d, dtype):
+    """Every CTA takes one block after the other; some blocks are seen by most of the others, some by none, and parts of blocks hold nothing."""
+    B, H, W, heads, block = 30, 22, 33, 2, (9, 10)                # blocks of two tiles, of which those at the lower edge fill one
+    q, k, v, g = inputs((B, H, W, heads, d), dtype, seed=13 + d)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    idx = torch.randint(-2, blocks_of(H, W, block), (B, heads, 12, 3), device="cuda", generator=gen, dtype=torch.int32)
+    idx[::2, :, :, 0] = 5
+    idx[idx == 2] = -1
+    idx[3] = -1                                                    # an image where nobody sees anything
+    got = call(q, k, v, idx, block, g)
+    check(got, ops.sparse(back(q), back(k), back(v), idx.cpu().numpy(), block, back(g), back(got["out"])), dtype)
+    assert all((got[n][3] == 0).all() for n in ("out", "dq", "dk", "dv")) and torch.isneginf(got["lse"][3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_extreme_values(dtype):
     """Scores of -inf mask keys, all of a query's among them; scores of hundreds overflow nothing; what no list names does not matter."""
     B, H, W, heads, d, block = 1, 8, 12, 1, 32, (4, 4)
