@@ -454,7 +454,7 @@ slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const
                                              int block_h, int block_w, int top, slide_attn_dtype dtype,
                                              void* workspace, size_t workspace_bytes, void* cuda_stream);
 slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, int head_dim,
-                                              int block_h, int block_w, size_t* bytes);
+                                              int block_h, int block_w, int top, size_t* bytes);
 
 /* Frees the context and everything it owns.  NULL is accepted.  The caller must make sure no
  * forward of this context is still running. */

@@ -82,7 +82,7 @@ def load() -> ctypes.CDLL:
         lib.slide_attn_select_workspace.argtypes = [i] * 7 + [ctypes.POINTER(sz)]
         lib.slide_attn_sparse_forward.argtypes = [vp] * 6 + [i] * 9 + [vp]
         lib.slide_attn_sparse_backward.argtypes = [vp] * 10 + [i] * 9 + [vp, sz, vp]
-        lib.slide_attn_sparse_workspace.argtypes = [i] * 7 + [ctypes.POINTER(sz)]
+        lib.slide_attn_sparse_workspace.argtypes = [i] * 8 + [ctypes.POINTER(sz)]
         lib.slide_attn_query_status.argtypes = [vp, vp]
         lib.slide_attn_destroy.argtypes = [vp]
         lib.slide_attn_status_string.argtypes = [i]
@@ -409,5 +409,5 @@ def slide_attn_sparse_backward(q, k, v, idx, block, out, lse, dout, dq, dk, dv, 
     bh, bw, top = _lists(where, q, idx, block)
     lib = load()
     ptrs = _device_ptrs(where, q, k, v, idx, out, lse, dout, dq, dk, dv)
-    workspace, at, size = _workspace(where, workspace, stream, "slide_attn_sparse_workspace", B, H, W, heads, d, bh, bw)
+    workspace, at, size = _workspace(where, workspace, stream, "slide_attn_sparse_workspace", B, H, W, heads, d, bh, bw, top)
     _check(lib.slide_attn_sparse_backward(*ptrs, B, H, W, heads, d, bh, bw, top, dtype, at, size, _stream_ptr(stream)), where)

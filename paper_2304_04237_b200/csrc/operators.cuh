@@ -17,7 +17,7 @@ bool dropout_supports(long long images, long long per_image, bool whole_images);
 cudaError_t launch_dropout(const void* x, const void* residual, void* y, long long images, long long per_image, double p, bool whole_images,
                            const unsigned long long* rng, slide_attn_dtype dtype, int num_sms, cudaStream_t stream);
 
-// pooled: 2 B heads blocks head_dim doubles; the backward's workspace: two floats a query and 16 bytes.
+// pooled: 2 B heads blocks head_dim doubles; the backward's workspace: see Prepared in sparse_bwd_kernel.cu.
 cudaError_t launch_select(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k, double* pooled,
                           int* idx, int num_sms, cudaStream_t stream);
 cudaError_t launch_sparse_forward(sparse::Geometry g, long long B, int head_dim, slide_attn_dtype dtype, const void* q, const void* k,

@@ -83,7 +83,10 @@ bool poolable(const sparse::Geometry& g, long long B, int head_dim) { return B *
 
 size_t map_bytes(const sparse::Geometry& g, int B, int head_dim, slide_attn_dtype t) { return (size_t)B * g.H * g.W * g.heads * head_dim * size_of(t); }
 size_t lse_bytes(const sparse::Geometry& g, int B) { return (size_t)B * g.H * g.W * g.heads * sizeof(float); }
-size_t backward_bytes(const sparse::Geometry& g, int B) { return 2 * lse_bytes(g, B) + 16; }
+// Two floats a query, a counter, and the lists turned round.
+size_t backward_bytes(const sparse::Geometry& g, int B) {
+    return 2 * lse_bytes(g, B) + sizeof(int) * (1 + (size_t)B * g.heads * (g.blocks + 1 + (size_t)g.blocks * g.top));
+}
 size_t list_bytes(const sparse::Geometry& g, int B) { return (size_t)B * g.heads * g.blocks * g.top * sizeof(int); }
 size_t pooled_bytes(const sparse::Geometry& g, int B, int head_dim) { return 2 * (size_t)B * g.heads * g.blocks * head_dim * sizeof(double); }
 
@@ -238,11 +241,12 @@ slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const 
     return launched(launch_sparse_forward(g, B, head_dim, dtype, q, k, v, idx, out, lse, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
-slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, size_t* bytes)
+slide_attn_status slide_attn_sparse_workspace(int B, int H, int W, int heads, int head_dim, int block_h, int block_w, int top, size_t* bytes)
 {
     if (!bytes) return SLIDE_ATTN_ERR_INVALID_ARG;
     sparse::Geometry g;
-    const slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    slide_attn_status st = sparse_shape(B, H, W, heads, head_dim, block_h, block_w, &g);
+    if (st == SLIDE_ATTN_OK) st = with_top(&g, top);
     if (st == SLIDE_ATTN_OK) *bytes = backward_bytes(g, B);
     return st;
 }

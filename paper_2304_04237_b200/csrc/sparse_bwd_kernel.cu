@@ -3,8 +3,8 @@
 //
 //   dS = P (dout v^T - delta),   dq = dS k / sqrt(d),   dk = dS^T q / sqrt(d),   dv = P^T dout
 //
-// Three launches: each query's logarithm and delta, side by side; queries (dq, over the blocks of their list); keys (dk and dv, over the blocks of
-// queries whose lists name the key's block, found by going through the image's lists in their order).  None adds to memory that
+// Three launches: each query's logarithm and delta, side by side, and the lists turned round; queries (dq, over the blocks of their list); keys (dk
+// and dv, over the blocks of queries whose lists name the key's block, in the order of the lists).  None adds to memory that
 // another CTA writes, so results do not depend on which CTA runs first.
 // Bound by latency: a warp's products, exponentials and products again wait for one another, and registers allow 12 to 16 such warps an SM.  128 x 128 x 2,
 // 3 heads, bf16, lists of 16 blocks of 8 x 8: queries 74 us, keys 104 (tensor pipe 50 and 44 %, issue slots 40 and 33 %); with the forward 231 in all, of 27 for the
@@ -34,15 +34,98 @@ template <> __device__ __forceinline__ float dot_piece<__nv_bfloat16>(const __nv
     return s;
 }
 
-// Less each query's logarithm of the sum (base 2), and less its delta: a query and head by as many neighbouring lanes as it has 16-byte pieces.
+// What the first launch leaves in the workspace.
+struct Prepared {
+    float2* stats;                   // of each query and head: less its logarithm of the sum (base 2), less its delta
+    unsigned* taken;                 // units that the keys' kernel has begun
+    int* starts;                     // [B][heads][blocks + 1]: of each block's part of `seers`
+    int* seers;                      // [B][heads][blocks top]: the blocks of queries that see a block, in the order of the lists
+};
+constexpr int kInvertWarps = 8;
+
+// One image's and head's lists turned round, by a CTA: each warp counts the blocks in its part of the lists, and puts them where the counts of the warps and blocks
+// ahead say.  counts: [warp][blocks]
+__device__ __forceinline__ void invert(const Geometry& g, const int* lists, int* starts, int* seers, int* counts) {
+    __shared__ int warp_sums[kInvertWarps];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, entries = g.blocks * g.top;
+    const int each = (entries + kInvertWarps * 32 - 1) / (kInvertWarps * 32) * 32, first = warp * each, end = min(entries, first + each);
+    int* own = counts + warp * g.blocks;
+    for (int i = threadIdx.x; i < kInvertWarps * g.blocks; i += 32 * kInvertWarps) counts[i] = 0;
+    __syncthreads();
+    // each_entry(entry, its block or -1, the lanes ahead that name the same block, all that do), by all lanes; 128 entries a trip to memory
+    auto go = [&](auto each_entry) {
+        for (int i0 = first; i0 < end; i0 += 128) {
+            int id[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = i0 + j * 32 + lane;
+                id[j] = i < end ? lists[i] : -1;
+                if ((unsigned)id[j] >= (unsigned)g.blocks) id[j] = -1;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i0 + j * 32 >= end) break;
+                const unsigned same = __match_any_sync(0xffffffffu, id[j]);
+                each_entry(i0 + j * 32 + lane, id[j], __popc(same & ((1u << lane) - 1u)), __popc(same));
+                __syncwarp();
+            }
+        }
+    };
+    go([&](int, int id, int rank, int count) {
+        if (id >= 0 && rank == 0) own[id] += count;
+    });
+    __syncthreads();
+    // where each block's and, in it, each warp's begin; a thread takes neighbouring blocks
+    const int span = (g.blocks + 32 * kInvertWarps - 1) / (32 * kInvertWarps), b0 = min(g.blocks, (int)threadIdx.x * span), b1 = min(g.blocks, b0 + span);
+    int sum = 0;
+    for (int b = b0; b < b1; ++b)
+        for (int w = 0; w < kInvertWarps; ++w) sum += counts[w * g.blocks + b];
+    int before = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += x;
+    }
+    if (lane == 31) warp_sums[warp] = before;
+    __syncthreads();
+    before -= sum;
+    for (int w = 0; w < warp; ++w) before += warp_sums[w];
+    for (int b = b0; b < b1; ++b) {
+        starts[b] = before;
+        for (int w = 0; w < kInvertWarps; ++w) {
+            const int n = counts[w * g.blocks + b];
+            counts[w * g.blocks + b] = before;
+            before += n;
+        }
+    }
+    if (threadIdx.x == 32 * kInvertWarps - 1) starts[g.blocks] = before;
+    __syncthreads();
+    go([&](int i, int id, int rank, int count) {
+        const int at = id >= 0 ? own[id] : 0;
+        __syncwarp();
+        if (id < 0) return;
+        seers[at + rank] = (int)g.by_top.quotient((unsigned)i);
+        if (rank == 0) own[id] = at + count;
+    });
+}
+
+// The first CTAs turn the lists round, one each of `lists`; the others take a query and head by as many neighbouring lanes as it has 16-byte pieces.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* out, const T* dout, const float* lse, float2* stats, unsigned* taken)
+__global__ void __launch_bounds__(32 * kInvertWarps) sparse_rows_kernel(const Geometry g, unsigned lists, long long n, const int* idx, const T* out,
+                                                                        const T* dout, const float* lse, const Prepared to)
 {
     constexpr int kPiece = 16 / sizeof(T), kLanes = D / kPiece, kEach = 4, kAtOnce = 256 / kLanes;
+    static_assert(kInvertWarps == 8, "256 threads");
+    extern __shared__ __align__(128) unsigned char smem[];
     grid_dependency_wait();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *taken = 0;
+    if (blockIdx.x < lists) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) *to.taken = 0;
+        const size_t entries = (size_t)(g.blocks * g.top);
+        invert(g, idx + blockIdx.x * entries, to.starts + (size_t)blockIdx.x * (unsigned)(g.blocks + 1), to.seers + blockIdx.x * entries, reinterpret_cast<int*>(smem));
+        return;
+    }
     const int lane = threadIdx.x % kLanes;
-    const long long first = (long long)blockIdx.x * (kAtOnce * kEach) + threadIdx.x / kLanes;
+    const long long first = (long long)(blockIdx.x - lists) * (kAtOnce * kEach) + threadIdx.x / kLanes;
     float s[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -54,7 +137,7 @@ __global__ void __launch_bounds__(256) sparse_rows_kernel(long long n, const T* 
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o /= 2) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
         const long long row = first + i * kAtOnce;
-        if (row < n && lane == 0) stats[row] = make_float2(-log2_of_sum(lse[row]), -s[i]);
+        if (row < n && lane == 0) to.stats[row] = make_float2(-log2_of_sum(lse[row]), -s[i]);
     }
 }
 
@@ -155,8 +238,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, const T* q, const T* k, 
     }
 }
 
-constexpr int kScanEach = 2, kScan = 128 * kScanEach;    // entries of the image's lists that are looked at in one go: four neighbours a lane, again and again
-constexpr int kListed = 4 * kScan;                              // entries that a table holds
+constexpr int kListed = 512;                                    // entries that a table holds
 
 // Shared memory of the keys' kernel: the pipe's, two tables, of each stage the queries' numbers (less the logarithms, then less the deltas) and a
 // word on what the stage holds.
@@ -168,78 +250,55 @@ template <typename T, int D> struct KeysPlan {
 };
 constexpr unsigned kLast = 1u << 16;                            // the unit's last tile; below: its rows
 
-// The blocks of queries that see a block, in the order of the lists, found by a warp.
+// The blocks of queries that see a block: a table of some of them, made by a warp, 32 at a time.
 struct Seers {
     Unit unit;
     Entry* table;
-    int seen, n, total;                                         // entries looked at; of the table; their rows
-    int4 mine[kScanEach];
-    __device__ __forceinline__ void begin(const Geometry& g, unsigned u, Entry* room) {
+    const int* from;
+    int left, n, total;                                         // left: not in the table yet; n: of the table; total: their rows
+    int mine;
+    bool reading;
+    __device__ __forceinline__ void begin(const Geometry& g, unsigned u, const Prepared& by, Entry* room) {
         unit.find(g, u);
+        const int* starts = by.starts + unit.list * (unsigned)(g.blocks + 1) + unit.r;
+        const int start = starts[0];
+        from = by.seers + unit.list * (unsigned)(g.blocks * g.top) + start;
+        left = starts[1] - start;
         table = room;
-        seen = n = total = 0;
+        n = total = 0;
+        reading = false;
     }
-    __device__ __forceinline__ bool room(const Geometry& g) const { return seen < g.blocks * g.top && n + kScan <= kListed; }
-    // Entries sent for, and looked at.
-    __device__ __forceinline__ void read(const Geometry& g, const int* idx, int lane) {
-        const int entries = g.blocks * g.top;
-        const int* lists = idx + unit.list * (unsigned)entries;
-#pragma unroll
-        for (int e = 0; e < kScanEach; ++e) {
-            const int i = seen + e * 128 + lane * 4;
-            mine[e] = make_int4(-1, -1, -1, -1);
-            if (entries % 4 == 0) {
-                if (i < entries) mine[e] = *reinterpret_cast<const int4*>(lists + i);
-            } else {
-                if (i < entries) mine[e].x = lists[i];
-                if (i + 1 < entries) mine[e].y = lists[i + 1];
-                if (i + 2 < entries) mine[e].z = lists[i + 2];
-                if (i + 3 < entries) mine[e].w = lists[i + 3];
-            }
+    __device__ __forceinline__ bool room() const { return left > 0 && n + 32 <= kListed; }
+    // Half of a step: sends for 32 entries, or writes those down that were sent for.
+    __device__ __forceinline__ void step(const Geometry& g, int lane) {
+        if (!reading) {
+            mine = lane < left ? from[lane] : -1;
+            reading = true;
+            return;
         }
-    }
-    __device__ __forceinline__ void look(const Geometry& g, int lane) {
+        Block block = {};
+        if (mine >= 0) block = block_of(g, mine);
+        int end = block.size();
 #pragma unroll
-        for (int e = 0; e < kScanEach; ++e) {
-            const int4 m = mine[e];
-            const bool is[4] = {m.x == unit.r, m.y == unit.r, m.z == unit.r, m.w == unit.r};
-            if (!__any_sync(0xffffffffu, is[0] || is[1] || is[2] || is[3])) continue;
-            Block block[4] = {};
-            unsigned own = 0;                                    // blocks << 24 | rows
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (is[j]) {
-                    block[j] = block_of(g, (int)g.by_top.quotient((unsigned)(seen + e * 128 + lane * 4 + j)));
-                    own += (1u << 24) + (unsigned)block[j].size();
-                }
-            unsigned before = own;
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const unsigned x = __shfl_up_sync(0xffffffffu, before, d);
-                if (lane >= d) before += x;
-            }
-            const unsigned all = __shfl_sync(0xffffffffu, before, 31);
-            before -= own;
-            int place = n + (int)(before >> 24), end = total + (int)(before & 0xFFFFFFu);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (is[j]) {
-                    end += block[j].size();
-                    table[place++] = Entry::of(g, block[j], end);
-                }
-            n += (int)(all >> 24);
-            total += (int)(all & 0xFFFFFFu);
+        for (int d = 1; d < 32; d *= 2) {
+            const int x = __shfl_up_sync(0xffffffffu, end, d);
+            if (lane >= d) end += x;
         }
-        seen += kScan;
+        if (mine >= 0) table[n + lane] = Entry::of(g, block, total + end);
+        const int taken = min(32, left);
+        n += taken;
+        left -= taken;
+        from += 32;
+        total += __shfl_sync(0xffffffffu, end, 31);
+        reading = false;
     }
 };
 
-// What the copying warp of the keys' kernel does.  Units are taken from a counter, one ahead: how many blocks see a block is known only when the lists have been
-// gone through, and a fixed share of the units would leave the CTAs with the sought-after blocks behind.  While a unit's tiles are sent for, the next one's
-// lists are gone through, a part beside each tile.
+// What the copying warp of the keys' kernel does.  Units are taken from a counter, one ahead: some blocks are seen by many more than others, and a fixed share of
+// the units would leave the CTAs with these behind.  The next unit's table is made while this one's tiles are sent for.
 template <typename T, int D>
-__device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, unsigned char* smem, const T* q, const T* k, const T* v, const int* idx,
-                                           const float2* stats, const T* dout, unsigned* taken) {
+__device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, unsigned char* smem, const T* q, const T* k, const T* v, const T* dout,
+                                           const Prepared& by) {
     using K = KeysPlan<T, D>;
     using P = BackwardPipe<T, D>;
     constexpr int N = P::N;
@@ -249,7 +308,7 @@ __device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, un
     unsigned* words = reinterpret_cast<unsigned*>(smem + K::kWordsAt);
     const unsigned pixel_bytes = (unsigned)(g.heads * D * (int)sizeof(T));
     Ring<P::S> ring;
-    auto ask = [&]() { return lane == 0 ? atomicAdd(taken, 1u) : 0u; };
+    auto ask = [&]() { return lane == 0 ? atomicAdd(by.taken, 1u) : 0u; };
     auto take = [&](unsigned asked) {                            // the next unit that has rows
         for (;;) {
             const unsigned u = __shfl_sync(0xffffffffu, asked, 0);
@@ -262,7 +321,7 @@ __device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, un
     };
     Seers next;
     unsigned u = take(ask()), turn = 0;
-    if (u < units) next.begin(g, u, tables);
+    if (u < units) next.begin(g, u, by, tables);
 #pragma unroll 1
     while (u < units) {
         const Unit unit = next.unit;
@@ -286,33 +345,26 @@ __device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, un
                 ring.commit();
             }
         }
-        if (next.room(g)) ring.drain();
-        const float2* from_stats = stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
+        if (next.room()) ring.drain();
+        const float2* from_stats = by.stats + unit.image * (unsigned)(g.H * g.W) * (unsigned)g.heads + (unsigned)unit.h;
         bool last = false, ahead = false;                        // ahead: `next` is the unit after this one
         unsigned u_next = units;
         while (!last) {
-            // what is left of this unit's lists, as far as the table goes
-            while (next.room(g)) {
-                next.read(g, idx, lane);
-                next.look(g, lane);
-            }
+            while (next.room()) next.step(g, lane);              // what is left of this unit, as far as the table goes
             __syncwarp();
             const int total = next.total;
-            const bool whole = next.seen >= g.blocks * g.top;    // no more tables of this unit
+            const bool whole = next.left == 0;                   // no more tables of this unit
             if (whole) {
                 u_next = take(asked);
                 ahead = u_next < units;
-                if (ahead) next.begin(g, u_next, tables + (turn ^= 1u) * kListed);
+                if (ahead) next.begin(g, u_next, by, tables + (turn ^= 1u) * kListed);
             }
-            const int looks = max((g.blocks * g.top / kScan + 1) * N / max(total, 1), 1);       // at each tile: about all of the lists in all
             Cursor cursor;
             cursor.reset(table);
             int done = 0;
 #pragma unroll 1
             do {
                 if (done >= total && !whole) break;              // an empty table, and more of them
-                const bool look = ahead && next.room(g);
-                if (look) next.read(g, idx, lane);               // on its way while this tile is sent for
                 unsigned pixels[N / 32];
 #pragma unroll
                 for (int i = 0; i < N / 32; ++i) pixels[i] = done + 32 * i + lane < total ? cursor.pixel(g, done + 32 * i + lane) : 0u;
@@ -329,12 +381,7 @@ __device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, un
                         copy4(at + (N + 32 * i + lane) * 4, from + 1);
                     }
                 ring.commit();
-                if (look) next.look(g, lane);
-#pragma unroll 1
-                for (int i = 1; i < looks && ahead && next.room(g); ++i) {
-                    next.read(g, idx, lane);
-                    next.look(g, lane);
-                }
+                if (ahead && next.room()) next.step(g, lane);
                 done += N;
             } while (done < total);
             __syncwarp();                                        // the table is free again
@@ -350,8 +397,7 @@ __device__ __forceinline__ void send_seers(const Geometry& g, unsigned units, un
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kBlock, sizeof(T) == 4 ? D == 64 ? 1 : 2 : D == 64 ? 2 : 3)
-sparse_keys_kernel(const Geometry g, unsigned units, const T* q, const T* k, const T* v, const int* idx, const float2* stats, const T* dout, T* dk, T* dv,
-                   unsigned* taken)
+sparse_keys_kernel(const Geometry g, unsigned units, const T* q, const T* k, const T* v, const T* dout, T* dk, T* dv, const Prepared by)
 {
     using K = KeysPlan<T, D>;
     using P = BackwardPipe<T, D>;
@@ -364,7 +410,7 @@ sparse_keys_kernel(const Geometry g, unsigned units, const T* q, const T* k, con
     // No wait here: this kernel starts when every CTA of the queries' kernel has waited for what was launched before the two, and takes nothing
     // from it.  The wait for it is at the end.
     if (warp == kThreads / 32) {
-        send_seers<T, D>(g, units, smem, q, k, v, idx, stats, dout, taken);
+        send_seers<T, D>(g, units, smem, q, k, v, dout, by);
         grid_dependency_wait();                              // complete only when the queries' kernel is
         return;
     }
@@ -450,7 +496,7 @@ sparse_keys_kernel(const Geometry g, unsigned units, const T* q, const T* k, con
 }
 
 template <typename T, int D>
-cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, float2* stats, unsigned* taken, int sms, cudaStream_t stream) {
+cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& m, const Prepared& to, int sms, cudaStream_t stream) {
     constexpr size_t smem_q = BackwardPipe<T, D>::kSmem, smem_k = KeysPlan<T, D>::kSmem;
     int ctas = 0, ctas_k = 0;
     cudaError_t e = resident<sparse_queries_kernel<T, D>, smem_q>(sms, &ctas);
@@ -459,15 +505,17 @@ cudaError_t launch_backward(const Geometry& g, long long B, const BackwardMaps& 
     const unsigned units = (unsigned)(B * g.blocks * g.tiles * g.heads), grid = units < (unsigned)ctas ? units : (unsigned)ctas;
     const long long n = B * g.H * g.W * g.heads;
     auto in = [](const void* p) { return static_cast<const T*>(p); };
-    auto to = [](void* p) { return static_cast<T*>(p); };
+    auto map = [](void* p) { return static_cast<T*>(p); };
     constexpr long long rows = 256 / (D * sizeof(T) / 16) * 4;      // of a block
-    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)((n + rows - 1) / rows)), 256, 0, stream, n, in(m.out), in(m.dout), m.lse, stats, taken);
+    const unsigned lists = (unsigned)(B * g.heads);
+    e = launch_chained(sparse_rows_kernel<T, D>, dim3((unsigned)(lists + (n + rows - 1) / rows)), 256, kInvertWarps * g.blocks * sizeof(int), stream, g, lists, n, m.idx,
+                       in(m.out), in(m.dout), m.lse, to);
     if (e != cudaSuccess) return e;
     e = launch_chained(sparse_queries_kernel<T, D>, dim3(grid), kBlock, smem_q, stream, g, units, in(m.q), in(m.k),
-                       in(m.v), m.idx, in(m.dout), static_cast<const float2*>(stats), to(m.dq));
+                       in(m.v), m.idx, in(m.dout), static_cast<const float2*>(to.stats), map(m.dq));
     if (e != cudaSuccess) return e;
     return launch_chained(sparse_keys_kernel<T, D>, dim3(units < (unsigned)ctas_k ? units : (unsigned)ctas_k), kBlock, smem_k, stream, g, units, in(m.q), in(m.k),
-                          in(m.v), m.idx, static_cast<const float2*>(stats), in(m.dout), to(m.dk), to(m.dv), taken);
+                          in(m.v), in(m.dout), map(m.dk), map(m.dv), to);
 }
 
 }  // namespace sparse
@@ -476,16 +524,19 @@ cudaError_t launch_sparse_backward(sparse::Geometry g, long long B, int head_dim
                                    void* workspace, int sms, cudaStream_t stream) {
     using namespace sparse;
     g.complete();
-    float2* stats = static_cast<float2*>(workspace);             // and behind them the counter of the units that are taken
-    unsigned* taken = reinterpret_cast<unsigned*>(stats + B * g.H * g.W * g.heads);
+    Prepared to;
+    to.stats = static_cast<float2*>(workspace);
+    to.taken = reinterpret_cast<unsigned*>(to.stats + B * g.H * g.W * g.heads);
+    to.starts = reinterpret_cast<int*>(to.taken) + 1;
+    to.seers = to.starts + B * g.heads * (g.blocks + 1);
     if (dtype == SLIDE_ATTN_BF16) {
-        if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, stats, taken, sms, stream);
-        if (head_dim == 32) return launch_backward<__nv_bfloat16, 32>(g, B, m, stats, taken, sms, stream);
-        return launch_backward<__nv_bfloat16, 64>(g, B, m, stats, taken, sms, stream);
+        if (head_dim == 16) return launch_backward<__nv_bfloat16, 16>(g, B, m, to, sms, stream);
+        if (head_dim == 32) return launch_backward<__nv_bfloat16, 32>(g, B, m, to, sms, stream);
+        return launch_backward<__nv_bfloat16, 64>(g, B, m, to, sms, stream);
     }
-    if (head_dim == 16) return launch_backward<float, 16>(g, B, m, stats, taken, sms, stream);
-    if (head_dim == 32) return launch_backward<float, 32>(g, B, m, stats, taken, sms, stream);
-    return launch_backward<float, 64>(g, B, m, stats, taken, sms, stream);
+    if (head_dim == 16) return launch_backward<float, 16>(g, B, m, to, sms, stream);
+    if (head_dim == 32) return launch_backward<float, 32>(g, B, m, to, sms, stream);
+    return launch_backward<float, 64>(g, B, m, to, sms, stream);
 }
 
 }  // namespace slide_attn

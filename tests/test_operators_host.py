@@ -73,7 +73,7 @@ CASES = {
     sparse: SPARSE + [(c, ARG) for c in [dict(q=None), dict(k=None), dict(v=None), dict(idx=None), dict(out=None), dict(lse=None), dict(out=A), dict(out=F2),
                                          dict(lse=C2)]] + [(dict(v=C2 + 8), ALIGN), (dict(lse=F2 + 4), ALIGN)],
     sparse_back: SPARSE + [(c, ARG) for c in [dict(q=None), dict(out=None), dict(lse=None), dict(dout=None), dict(dq=None), dict(dk=None), dict(dv=None),
-                                              dict(ws=None), dict(size=2 * 4 * 2 * 64 * 2 + 16 - 1), dict(dq=A), dict(dk=G2), dict(dv=I2), dict(dq=J2), dict(ws=F2),
+                                              dict(ws=None), dict(size=2 * 4 * 2 * 64 * 2 + 4 * (1 + 4 * (5 + 8)) - 1), dict(dq=A), dict(dk=G2), dict(dv=I2), dict(dq=J2), dict(ws=F2),
                                               dict(ws=H2)]] + [(dict(dk=I2 + 8), ALIGN), (dict(ws=K2 + 4), ALIGN)],
 }
 
@@ -129,10 +129,11 @@ def test_workspace_sizes(lib):
     assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 6, 1, 0, ctypes.byref(n)) == sa.OK and n.value == 0
     assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 6, 1, 1, ctypes.byref(n)) == sa.OK and n.value == 8 * 3 * 6 + 2 * 4 * 3 * 48
     assert lib.slide_attn_select_workspace(3, 9, 7, 2, 16, 4, 4, ctypes.byref(n)) == sa.OK and n.value == 2 * 8 * 3 * 2 * 6 * 16
-    assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, ctypes.byref(n)) == sa.OK and n.value == 2 * 4 * 3 * 63 * 2 + 16
+    assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, 3, ctypes.byref(n)) == sa.OK and n.value == 2 * 4 * 3 * 63 * 2 + 4 * (1 + 6 * (7 + 18))
     assert lib.slide_attn_group_norm_workspace(3, 5, 7, 48, 7, 1, 0, ctypes.byref(n)) == sa.ERR_UNSUPPORTED
     assert lib.slide_attn_select_workspace(3, 9, 7, 2, 8, 4, 4, ctypes.byref(n)) == sa.ERR_UNSUPPORTED
-    assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, None) == sa.ERR_INVALID_ARG
+    assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, 3, None) == sa.ERR_INVALID_ARG
+    assert lib.slide_attn_sparse_workspace(3, 9, 7, 2, 16, 4, 4, 65, ctypes.byref(n)) == sa.ERR_UNSUPPORTED
 
 
 def test_binding_refuses_what_it_can_see(lib):
