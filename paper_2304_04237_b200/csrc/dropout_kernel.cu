@@ -5,8 +5,8 @@
 // computes it again.  In units of images the word of image b decides for all of its elements.
 //
 // fp32 is bound by memory (3 maps forward, 2 backward).  bf16 is bound by the generator's integer instructions, ten products of 32 x 32 -> 64
-// bits and ten exclusive ors for two elements, on pipes of half rate: 64 x 56 x 56 x 96 takes 39.5 us for
-// forward and backward, the memory alone 29.5.
+// bits and ten exclusive ors for two elements, on pipes of half rate: 64 x 56 x 56 x 96 takes 40 us for
+// forward and backward, the memory alone 29.5.  Whole images, 32 x 28 x 42 x 192, fp32, p = 0.2: 13.8 us, of 13.2.
 // The products with the scale are fp32, and the sum is rounded to the storage type once.
 #include "operators.cuh"
 

@@ -52,8 +52,8 @@ __device__ __forceinline__ void invert(const Geometry& g, const int* lists, int*
     int* own = counts + warp * g.blocks;
     for (int i = threadIdx.x; i < kInvertWarps * g.blocks; i += 32 * kInvertWarps) counts[i] = 0;
     __syncthreads();
-    // each_entry(entry, its block or -1, the lanes ahead that name the same block, all that do), by all lanes; 128 entries a trip to memory
-    auto go = [&](auto each_entry) {
+    // f(first of 128 entries, of each lane's four the block, or -1)
+    auto go = [&](auto f) {
         for (int i0 = first; i0 < end; i0 += 128) {
             int id[4];
 #pragma unroll
@@ -62,17 +62,13 @@ __device__ __forceinline__ void invert(const Geometry& g, const int* lists, int*
                 id[j] = i < end ? lists[i] : -1;
                 if ((unsigned)id[j] >= (unsigned)g.blocks) id[j] = -1;
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (i0 + j * 32 >= end) break;
-                const unsigned same = __match_any_sync(0xffffffffu, id[j]);
-                each_entry(i0 + j * 32 + lane, id[j], __popc(same & ((1u << lane) - 1u)), __popc(same));
-                __syncwarp();
-            }
+            f(i0, id);
         }
     };
-    go([&](int, int id, int rank, int count) {
-        if (id >= 0 && rank == 0) own[id] += count;
+    go([&](int, const int (&id)[4]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (id[j] >= 0) atomicAdd(own + id[j], 1);
     });
     __syncthreads();
     // where each block's and, in it, each warp's begin; a thread takes neighbouring blocks
@@ -100,12 +96,20 @@ __device__ __forceinline__ void invert(const Geometry& g, const int* lists, int*
     }
     if (threadIdx.x == 32 * kInvertWarps - 1) starts[g.blocks] = before;
     __syncthreads();
-    go([&](int i, int id, int rank, int count) {
-        const int at = id >= 0 ? own[id] : 0;
-        __syncwarp();
-        if (id < 0) return;
-        seers[at + rank] = (int)g.by_top.quotient((unsigned)i);
-        if (rank == 0) own[id] = at + count;
+    go([&](int i0, const int (&id)[4]) {
+        unsigned same[4];                                        // the lanes that name the same block
+#pragma unroll
+        for (int j = 0; j < 4; ++j) same[j] = __match_any_sync(0xffffffffu, id[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = id[j] >= 0 ? own[id[j]] : 0, rank = __popc(same[j] & ((1u << lane) - 1u));
+            __syncwarp();
+            if (id[j] >= 0) {
+                seers[at + rank] = (int)g.by_top.quotient((unsigned)(i0 + j * 32 + lane));
+                if (rank == 0) own[id[j]] = at + __popc(same[j]);
+            }
+            __syncwarp();
+        }
     });
 }
 
