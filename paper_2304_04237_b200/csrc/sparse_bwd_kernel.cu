@@ -7,8 +7,8 @@
 // and dv, over the blocks of queries whose lists name the key's block, in the order of the lists).  None adds to memory that
 // another CTA writes, so results do not depend on which CTA runs first.
 // Bound by latency: a warp's products, exponentials and products again wait for one another, and registers allow 12 to 16 such warps an SM.  128 x 128 x 2,
-// 3 heads, bf16, lists of 16 blocks of 8 x 8: queries 74 us, keys 104 (tensor pipe 50 and 44 %, issue slots 40 and 33 %); with the forward 231 in all, of 27 for the
-// products at the rate of large matrices.
+// 3 heads, bf16, lists of 16 blocks of 8 x 8: queries 81 us, keys 103 by themselves (tensor pipe 45 and 47 %, issue slots 34 and 30 %); with the forward 222 in
+// all, of 27 for the products at the rate of large matrices.
 #include "operators.cuh"
 
 namespace slide_attn {

@@ -7,7 +7,8 @@
 // the second product.
 // A list names blocks of a few dozen rows for 64 queries, so tiles of 64 rows and products of 16 rows a warp: mma.sync, whose operands and results are
 // in the registers that the softmax works on.  Bound by latency: 64 x 56 x 56, 2 heads, bf16, 4 blocks of 7 x 7, takes 82.6 us, of 15.7 for its bytes (issue slots
-// 44 %, exponentials 34 % of their pipe, tensor pipe 29 %); 2 x 128 x 128, 3 heads, fp32, 8 blocks of 8 x 8, 145 us (tensor pipe 50 %: six products for one).
+// 45 %, exponentials 36 % of their pipe, tensor pipe 30 %); 2 x 128 x 128, 3 heads, fp32, 8 blocks of 8 x 8, 156 us with the choice of the blocks (tensor pipe
+// 45 %: six products for one).
 // 32-row tiles with more CTAs, and fewer registers with spills, were slower.
 #include "operators.cuh"
 
