@@ -2,6 +2,8 @@
 // context and workspaces instead of owning any; here their arguments are checked, the arithmetic lives in the kernel files.
 #include <math.h>
 
+#include <atomic>
+
 #include "operators.cuh"
 
 using namespace slide_attn;
@@ -27,10 +29,10 @@ size_t size_of(slide_attn_dtype t) { return t == SLIDE_ATTN_BF16 ? 2 : 4; }
 
 // The current device is one that the kernels run on; its SMs.
 slide_attn_status current_device(int* num_sms) {
-    static int known[64] = {};
+    static std::atomic<int> known[64];                 // host threads may call at once
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SLIDE_ATTN_ERR_CUDA; }
-    if (dev < 64) n = known[dev];
+    if (dev < 64) n = known[dev].load(std::memory_order_relaxed);
     if (n == 0) {
         int major = 0;
         if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
@@ -39,7 +41,7 @@ slide_attn_status current_device(int* num_sms) {
             return SLIDE_ATTN_ERR_CUDA;
         }
         if (major != 10) return SLIDE_ATTN_ERR_ARCH;
-        if (dev < 64) known[dev] = n;
+        if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
     }
     *num_sms = n;
     return SLIDE_ATTN_OK;

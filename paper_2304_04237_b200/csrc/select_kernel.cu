@@ -138,14 +138,14 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const Geometry g, lo
 template <int D>
 cudaError_t launch_rank(const Geometry& g, long long B, const double* pooled, int* idx, cudaStream_t stream) {
     constexpr int kFixed = (kRankRows * D + kRankColumns * (D + 1)) * 8, kMost = kFixed + kRankRows * kMaxBlocks * 8;
-    static bool ready[64] = {};
+    static std::atomic<bool> ready[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !ready[dev]) {
+    if (dev >= 64 || !ready[dev].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(rank_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e != cudaSuccess) return e;
-        if (dev < 64) ready[dev] = true;
+        if (dev < 64) ready[dev].store(true, std::memory_order_release);
     }
     const long long groups = (g.blocks + kRankRows - 1) / kRankRows;
     return launch_chained(rank_kernel<D>, dim3((unsigned)(B * g.heads * groups)), kRankThreads, (size_t)(kFixed + kRankRows * g.blocks * 8), stream, g, B,

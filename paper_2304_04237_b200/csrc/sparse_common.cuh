@@ -478,7 +478,7 @@ template <typename T, int D, int N> struct Sender {
     }
 };
 
-// What the kernels that keep queries share: a CTA takes its even share of the units, neighbours, one after the other, and the copies run ahead of the
+// What the kernels that keep queries share (the one that keeps keys takes its stages and operands, and sends for them in its own way): a CTA takes its even share of the units, neighbours, one after the other, and the copies run ahead of the
 // arithmetic across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
 // trips to memory.  There are as many CTAs as the SMs hold.  (Several times as many, of up to eight units, took 85.2 us instead of 82.6 for the
 // forward of 64 x 56 x 56, 2 heads, bf16, and 161 instead of 155.5 for 32 x 28 x 42, 3 heads of 64, bf16, forward and backward.)
