@@ -30,8 +30,9 @@ constexpr int kOnce = 8;               // rounds of an image that one CTA keeps
 struct NormShape {
     int P, C, groups, per_group;       // per_group: channels of a group
     int columns, rows, threads;        // 16-byte columns of a pixel; pixels that a CTA takes at a time (a round)
-    int rounds, chunks;                // of a CTA; CTAs of an image.  One chunk: an image in one launch
-};
+    int rounds, chunks;                // of a CTA; CTAs of an image
+    bool once;                         // forward: a CTA keeps its whole image in registers (kOnce rounds at most), one launch.  Not the same as one
+};                                     // chunk: where there are many images, each is one chunk however large it is
 
 struct NormArgs {
     const void* x;
@@ -466,7 +467,7 @@ __global__ void __launch_bounds__(Threads, kForwardCtas * 256 / Threads) norm_fo
     }
 }
 
-// An image of one chunk: all of the forward, from registers.
+// An image of kOnce rounds at most (NormShape::once): all of the forward, from registers.
 template <int Threads, typename T, int Act>
 __global__ void __launch_bounds__(Threads, 2 * 256 / Threads) norm_forward_once_kernel(const NormArgs a, const NormShape s)
 {
@@ -670,6 +671,7 @@ bool make_shape(long long B, long long P, int C, int groups, int size, int maps,
         // an image in one CTA's registers
         if (P > (long long)s.rows * kOnce) { s.threads = 512; s.rows = 512 / s.columns; }
         s.rounds = kOnce;
+        s.once = true;
     } else {
         // What a thread does once (some hundred instructions) wants many rounds: as many CTAs as the SMs hold together, or the images' number.
         const long long all = (P + s.rows - 1) / s.rows, room = 148LL * (maps == 1 ? kForwardCtas : kBackwardCtas) * 256 / s.threads;
@@ -714,8 +716,7 @@ bool joins_inline(const NormShape& s) { return s.groups <= s.threads / 32; }
 struct NormRoom {
     size_t joined, channels, bytes;
     NormRoom(const NormShape& s, long long B, int maps) {
-        const bool once = maps == 1 && s.chunks == 1;
-        joined = once ? 0 : align16((size_t)B * s.groups * s.chunks * sizeof(float2));
+        joined = s.once ? 0 : align16((size_t)B * s.groups * s.chunks * sizeof(float2));
         channels = joined + (maps == 1 || joins_inline(s) ? 0 : align16((size_t)B * s.groups * sizeof(float2)));
         bytes = channels + (maps == 1 ? 0 : (size_t)B * s.chunks * 2 * s.C * sizeof(float));
     }
@@ -726,7 +727,7 @@ cudaError_t forward_as(const NormArgs& a, const NormShape& s, long long B, cudaS
     const dim3 grid((unsigned)(B * s.chunks));
     constexpr size_t ring = Stream<Threads, 1, kTogether>::kSmem;
     const size_t smem = (size_t)(s.threads * 2 * Vec<T>::pairs + 2 * s.groups) * 4;
-    if (s.chunks == 1) return launch_with<norm_forward_once_kernel<Threads, T, Act>>(grid, Threads, smem, stream, a, s);
+    if (s.once) return launch_with<norm_forward_once_kernel<Threads, T, Act>>(grid, Threads, smem, stream, a, s);
     cudaError_t e = launch_with<norm_sums_kernel<Threads, T>>(grid, Threads, ring + smem, stream, a, s);
     if (e == cudaSuccess && !a.join)
         e = launch_chained(norm_join_kernel<false>, dim3((unsigned)((B * s.groups + 7) / 8)), 256, 0, stream, a, s, B * s.groups);
