@@ -661,10 +661,10 @@ __global__ void __launch_bounds__(32 * kWeightRows) norm_weight_kernel(const flo
 
 // False where a pixel has too many columns for a CTA, or the call too many CTAs for a grid.  `maps`: 1 forward, 2 backward.
 bool make_shape(long long B, long long P, int C, int groups, int size, int maps, NormShape* out) {
+    if (C > 512 * 16 / size) return false;            // more than 512 columns; C is anything so far, and products with it may overflow
     NormShape s = {};
     s.P = (int)P; s.C = C; s.groups = groups; s.per_group = C / groups;
     s.columns = C * size / 16;
-    if (s.columns > 512) return false;
     s.threads = s.columns > 256 ? 512 : 256;
     s.rows = s.threads / s.columns;
     if (maps == 1 && P <= (long long)(512 / s.columns) * kOnce) {
