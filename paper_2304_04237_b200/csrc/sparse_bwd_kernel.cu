@@ -157,7 +157,7 @@ sparse_queries_kernel(const Geometry g, unsigned units, const T* q, const T* k, 
     constexpr float scale = root<D>();
 
     grid_dependency_wait();
-    grid_launch_dependents();                                // the keys' kernel needs nothing of this one
+    grid_launch_dependents();                                // CTAs of the keys' kernel take the places that become free, and wait there
     P pipe(smem, units);
     if (warp == kThreads / 32) {
         pipe.copy_all(g, q, dout, k, v, idx);
@@ -411,11 +411,10 @@ sparse_keys_kernel(const Geometry g, unsigned units, const T* q, const T* k, con
     const int warp = uniform((int)threadIdx.x / 32), lane = threadIdx.x % 32;
     constexpr float scale = root<D>();
 
-    // No wait here: this kernel starts when every CTA of the queries' kernel has waited for what was launched before the two, and takes nothing
-    // from it.  The wait for it is at the end.
+    // It takes nothing from the queries' kernel, but only a wait of its own makes visible to it what was written before that one.
+    grid_dependency_wait();
     if (warp == kThreads / 32) {
         send_seers<T, D>(g, units, smem, q, k, v, dout, by);
-        grid_dependency_wait();                              // complete only when the queries' kernel is
         return;
     }
     P pipe(smem, units);
