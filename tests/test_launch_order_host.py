@@ -6,7 +6,7 @@ import re
 import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2304_04237_b200", "csrc")
-SOURCES = ["dropout_kernel.cu", "select_kernel.cu", "sparse_bwd_kernel.cu", "sparse_kernel.cu"]
+SOURCES = ["dropout_kernel.cu", "norm_kernel.cu", "select_kernel.cu", "sparse_bwd_kernel.cu", "sparse_kernel.cu"]
 
 
 def kernels(source):
