@@ -95,45 +95,55 @@ __device__ __forceinline__ pair rcp_2(pair x) {
     return make_pair(rcp_approx(a), rcp_approx(b));
 }
 
-// The normal distribution's integral up to z and, from the same exponential, its density.  erfc by M. Abramowitz, I. Stegun, Handbook of
-// Mathematical Functions, 7.1.26 (error below 1.5e-7): erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + p x), x = |z| / sqrt 2.  An
-// infinity gives 0 or 1 and a NaN a NaN.
-__device__ __forceinline__ void normal_2(pair z, pair& cdf, pair& density) {
+// The normal distribution's integral up to -|z| and the exponential exp(-z^2 / 2) that is in it: with t = 1 / (1 + p |z|) it is that times t q(t), q a polynomial
+// fitted up to |z| = 13.5, where the exponential is below fp32's normal numbers.  fp32: degree 7, of the least relative error, 1.3e-7.  bf16: degree 5,
+// off by 1.1e-7 or by 1.1e-4 of itself, whichever is less, a 35th of a rounding to bf16 (with fp32's polynomial 64 x 56 x 56 x 96, forward and backward,
+// takes 97.2 us instead of 93.8).  The arithmetic adds five or six roundings, and the exponential's argument some z^2 of them, as z's own does.  a: |z|, or a
+// large number in an infinity's place, times which nothing is still nothing.
+template <typename T> __device__ __forceinline__ pair normal_tail(pair z, pair& a, pair& e) {
+    constexpr bool kWide = sizeof(T) == 4;
+    constexpr int kTerms = kWide ? 8 : 6;
+    constexpr float kFit[8] = {kWide ? 0.119626395f : 0.165674686f, kWide ? 0.120798312f : 0.179397747f, kWide ? 0.0996377915f : 0.0673380196f,
+                               kWide ? 0.129468247f : 0.266205519f, kWide ? -0.0553920753f : -0.23595579f, kWide ? 0.208204731f : 0.0573398992f,
+                               -0.158274934f, 0.0359314866f};
     float z0, z1;
     split_pair(z, z0, z1);
-    const pair a = make_pair(fabsf(z0), fabsf(z1));
-    const pair t = rcp_2(fma2(a, both(0.3275911f * 0.70710678f), both(1.0f)));
-    pair p = fma2(t, both(0.5f * 1.061405429f), both(-0.5f * 1.453152027f));      // half of the polynomial
-    p = fma2(p, t, both(0.5f * 1.421413741f));
-    p = fma2(p, t, both(-0.5f * 0.284496736f));
-    p = fma2(p, t, both(0.5f * 0.254829592f));
-    const pair e = exp2_2(mul2(mul2(z, both(-0.72134752f)), z));                 // exp(-z^2 / 2)
-    const pair d = fma2(mul2(p, t), mul2(e, both(-1.0f)), both(0.5f));           // 1/2 - integral up to -|z|
-    float d0, d1;
-    split_pair(d, d0, d1);
-    cdf = add2(make_pair(copysignf(d0, z0), copysignf(d1, z1)), both(0.5f));
-    density = mul2(e, both(0.39894228f));
+    a = make_pair(fminf(fabsf(z0), 1e30f), fminf(fabsf(z1), 1e30f));
+    const pair t = rcp_2(fma2(a, both(kWide ? 0.3f : 0.4175f), both(1.0f)));
+    pair q = both(kFit[kTerms - 1]);
+#pragma unroll
+    for (int i = kTerms - 2; i >= 0; --i) q = fma2(q, t, both(kFit[i]));
+    e = exp2_2(mul2(mul2(z, both(-0.72134752f)), z));
+    return mul2(mul2(q, t), e);
 }
 
-template <int Act> __device__ __forceinline__ pair act_value(pair z) {
+template <typename T, int Act> __device__ __forceinline__ pair act_value(pair z) {
     if constexpr (Act == SLIDE_ATTN_ACT_SILU) {
         return mul2(z, rcp_2(add2(exp2_2(mul2(z, both(-1.44269504f))), both(1.0f))));
     } else if constexpr (Act == SLIDE_ATTN_ACT_GELU) {
-        pair cdf, density;
-        normal_2(z, cdf, density);
-        return mul2(z, cdf);
+        // z times the integral up to z, which for z > 0 is 1 less the tail: max(z, 0) - |z| tail.  Nothing of the tail is lost for z < 0.
+        pair a, e;
+        const pair tail = normal_tail<T>(z, a, e);
+        float z0, z1;
+        split_pair(z, z0, z1);
+        return fma2(mul2(a, both(-1.0f)), tail, make_pair(fmaxf(z0, 0.0f), fmaxf(z1, 0.0f)));
     } else {
         return z;
     }
 }
-template <int Act> __device__ __forceinline__ pair act_slope(pair z) {
+template <typename T, int Act> __device__ __forceinline__ pair act_slope(pair z) {
     if constexpr (Act == SLIDE_ATTN_ACT_SILU) {
         const pair g = rcp_2(add2(exp2_2(mul2(z, both(-1.44269504f))), both(1.0f)));
         return mul2(g, fma2(z, fma2(g, both(-1.0f), both(1.0f)), both(1.0f)));    // g (1 + z (1 - g))
     } else if constexpr (Act == SLIDE_ATTN_ACT_GELU) {
-        pair cdf, density;
-        normal_2(z, cdf, density);
-        return fma2(z, density, cdf);
+        // The integral up to z plus z times the density: for z < 0 tail - |z| density, otherwise 1 less that.
+        pair a, e;
+        const pair tail = normal_tail<T>(z, a, e), below = fma2(mul2(a, both(-0.39894228f)), e, tail), above = fma2(below, both(-1.0f), both(1.0f));
+        float z0, z1, b0, b1, c0, c1;
+        split_pair(z, z0, z1);
+        split_pair(below, b0, b1);
+        split_pair(above, c0, c1);
+        return make_pair(z0 < 0.0f ? b0 : c0, z1 < 0.0f ? b1 : c1);
     } else {
         return both(1.0f);
     }
@@ -418,7 +428,7 @@ __device__ __forceinline__ uint4 normalised(const uint4& raw, const pair (&mean)
     pair v[Vec<T>::pairs];
     Vec<T>::get(raw, v);
 #pragma unroll
-    for (int e = 0; e < Vec<T>::pairs; ++e) v[e] = act_value<Act>(fma2(add2(v[e], mean[e]), scale[e], beta[e]));
+    for (int e = 0; e < Vec<T>::pairs; ++e) v[e] = act_value<T, Act>(fma2(add2(v[e], mean[e]), scale[e], beta[e]));
     return Vec<T>::put(v);
 }
 
@@ -555,7 +565,7 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
 #pragma unroll
                 for (int e = 0; e < Q; ++e) {
                     c[e] = add2(c[e], mean[e]);
-                    if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<Act>(fma2(c[e], scale[e], beta[e])));
+                    if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<T, Act>(fma2(c[e], scale[e], beta[e])));
                     s1[e] = add2(s1[e], dz[e]);
                     s2[e] = fma2(dz[e], c[e], s2[e]);
                 }
@@ -656,7 +666,7 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_b
 #pragma unroll
                 for (int e = 0; e < Q; ++e) {
                     c[e] = add2(c[e], mean[e]);
-                    if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<Act>(fma2(c[e], scale[e], beta[e])));
+                    if constexpr (Act != SLIDE_ATTN_ACT_NONE) dz[e] = mul2(dz[e], act_slope<T, Act>(fma2(c[e], scale[e], beta[e])));
                     dz[e] = fma2(dz[e], scale[e], fma2(c[e], quad[e], shift[e]));
                 }
                 *reinterpret_cast<uint4*>(dst + i * at.step) = Vec<T>::put(dz);
