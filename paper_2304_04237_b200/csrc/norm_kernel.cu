@@ -12,7 +12,7 @@
 // over on the same maps, 30 us and 46).  Each pass reads its maps again, and the activation's special functions and roundings share the issue slots.
 // (One pass for all, with an image's pixels kept in the shared memory of a cluster of CTAs that exchange their sums, read every map once,
 // but its barriers and low occupancy made 64 x 56 x 56 x 96, bf16, GELU, forward and backward, take 114 us.)
-// All sums are fp32, in an order that only the shape decides.
+// Sums are fp32 (the weights' over many chunks fp64), in an order that only the shape decides.
 #include <atomic>
 
 #include "operators.cuh"
@@ -591,21 +591,30 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_s
         a.partial[((size_t)at.image * s.groups + g) * s.chunks + at.chunk] = make_float2(local[g], local[s.groups + g]);
 }
 
-// dbeta and dgamma: the chunks' sums, added up in their order.  32 of the 2 C columns a CTA, a row a warp at a time.  part: [warp][32]
+// dbeta and dgamma: the chunks' sums, added up in their order.  32 of the 2 C columns a CTA, a row a warp at a time.  There may be a hundred thousand
+// chunks (images of a few pixels): 32 of a warp's at a time in fp32, those sums in fp64, so that the error does not grow with their number.
+// part: [warp][32]
 template <int Threads>
-__device__ __forceinline__ void sum_weights(const NormArgs& a, int C, float (*part)[32]) {
-    constexpr int kRowsAtOnce = Threads / 32;
+__device__ __forceinline__ void sum_weights(const NormArgs& a, int C, double (*part)[32]) {
+    constexpr int kRowsAtOnce = Threads / 32, kRun = 32;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
-    float sum = 0.0f;
-    if (c < 2 * C)
+    double sum = 0.0;
+    if (c < 2 * C) {
+        const float* from = a.channels + c;
+        for (long long r0 = warp; r0 < a.all_chunks; r0 += kRun * kRowsAtOnce) {
+            const long long end = min(a.all_chunks, r0 + kRun * kRowsAtOnce);
+            float run = 0.0f;
 #pragma unroll 8
-        for (long long r = warp; r < a.all_chunks; r += kRowsAtOnce) sum += a.channels[(size_t)r * 2 * C + c];
+            for (long long r = r0; r < end; r += kRowsAtOnce) run += from[(size_t)r * 2 * C];
+            sum += run;
+        }
+    }
     part[warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && c < 2 * C) {
 #pragma unroll
         for (int i = 1; i < kRowsAtOnce; ++i) sum += part[i][lane];
-        (c < C ? a.dbeta : a.dgamma)[c < C ? c : c - C] = sum;
+        (c < C ? a.dbeta : a.dgamma)[c < C ? c : c - C] = (float)sum;
     }
 }
 
@@ -619,7 +628,7 @@ __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_b
     using Maps = Stream<Threads, 2, kPair>;
     grid_dependency_wait();
     if (blockIdx.x < a.weight_ctas) {
-        sum_weights<Threads>(a, s.C, reinterpret_cast<float (*)[32]>(smem));
+        sum_weights<Threads>(a, s.C, reinterpret_cast<double (*)[32]>(smem));
         return;
     }
     const Place at = find_place<T>(s, blockIdx.x - a.weight_ctas);

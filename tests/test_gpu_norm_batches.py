@@ -3,8 +3,11 @@ larger ones, several chunks an image and one, 256 and 512 threads, chunks joined
 
 Tolerances are those of test_gpu_norm: of the sums here the longest chain of additions is a thread's rounds (at most 38), the threads' rows (at most 64) and, in the
 weights' sums, an eighth of the chunks (at most 56): 158 of the 335 steps of 2^-24 that are allowed."""
+import numpy as np
 import pytest
+import torch
 
+import paper_2304_04237_b200 as sa
 from oracle import operators as ops
 from test_gpu_norm import back, call, check, inputs
 
@@ -23,3 +26,21 @@ def test_many_images(dtype, shape):
     B, H, W, C, groups = shape
     x, dy, (gamma, beta) = inputs(B, H, W, C, dtype, seed=B + H * W)
     check(call(x, gamma, beta, groups, "silu", dy), ops.group_norm(back(x), back(gamma), back(beta), groups, 1e-5, "silu", back(dy)), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B", [1, 31, 257, 100000])
+def test_weights_of_a_batch_of_single_pixels(B, dtype):
+    """Equal gradients, whose roundings all go the same way.  32 of an eighth of the images are added up in fp32, which is off by 31 half steps at most, the rest in
+    fp64; dz u has four roundings of its own (deviation, scale, product, rstd)."""
+    C, groups = 32, 2
+    x = inputs(B, 1, 1, C, dtype, seed=B)[0]
+    dy = torch.full_like(x, 0.7)
+    dx, y = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = (torch.empty(B, groups, device="cuda") for _ in range(2))
+    dgamma, dbeta = (torch.empty(C, device="cuda") for _ in range(2))
+    sa.slide_attn_group_norm_forward(x, None, None, groups, 1e-5, sa.ACT_NONE, y, mean, rstd)
+    sa.slide_attn_group_norm_backward(x, None, None, groups, sa.ACT_NONE, mean, rstd, dy, dx, dgamma, dbeta)
+    assert (np.abs(back(dbeta) - back(dy).sum((0, 1, 2))) <= 32 * 2.0 ** -24 * back(dbeta)).all()
+    u = (back(x).reshape(B, groups, -1) - back(mean)[..., None]) * back(rstd)[..., None] * float(dy[0, 0, 0, 0])     # with the statistics that the call was given
+    assert (np.abs(back(dgamma) - u.sum(0).ravel()) <= 36 * 2.0 ** -24 * np.abs(u).sum(0).ravel()).all()
