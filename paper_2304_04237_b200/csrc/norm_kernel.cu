@@ -26,6 +26,7 @@ constexpr int kTogether = 4;           // 16-byte pieces that a thread works on 
 constexpr int kForwardCtas = 4, kBackwardCtas = 3;     // of 256 threads on an SM, as registers allow
 constexpr int kPair = kTogether / 2;
 constexpr int kOnce = 8;               // rounds of an image that one CTA keeps
+constexpr long long kSms = 148;        // that chunks are made for.  B200's, whatever device is current, so that the workspace and the order of the sums depend on the shape alone
 
 struct NormShape {
     int P, C, groups, per_group;       // per_group: channels of a group
@@ -700,8 +701,8 @@ bool make_shape(long long B, long long P, int C, int groups, int size, int maps,
         s.rounds = kOnce;
         s.once = true;
     } else {
-        // What a thread does once (some hundred instructions) wants many rounds: as many CTAs as the SMs hold together, or the images' number.
-        const long long all = (P + s.rows - 1) / s.rows, room = 148LL * (maps == 1 ? kForwardCtas : kBackwardCtas) * 256 / s.threads;
+        // What a thread does once (some hundred instructions) wants many rounds: as many CTAs as kSms SMs hold together, or the images' number.
+        const long long all = (P + s.rows - 1) / s.rows, room = kSms * (maps == 1 ? kForwardCtas : kBackwardCtas) * 256 / s.threads;
         const long long each = room / B > 0 ? room / B : 1;
         long long rounds = (all + each - 1) / each;
         if (rounds < kTogether) rounds = kTogether;
