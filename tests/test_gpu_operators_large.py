@@ -14,6 +14,14 @@ from test_gpu_norm import back, call, check
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def nothing_kept():
+    """Leaves no memory in torch's cache, which other large tests look at."""
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
 def room(gigabytes):
     if torch.cuda.mem_get_info()[0] < gigabytes * 1e9:
         pytest.skip(f"needs {gigabytes} GB")
