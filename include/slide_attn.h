@@ -447,6 +447,10 @@ slide_attn_status slide_attn_sparse_forward(const void* q, const void* k, const 
  * Its gradients for dout = d(loss)/d(out); the lists are constants.
  *   q, k, v, idx, out, lse  [in] what the forward was given and gave
  *   dq, dk, dv              [out] [B][H][W][heads][head_dim], overwritten
+ * fp32 storage: as the forward.  bf16: products of bf16 operands; the softmax weights and the scores'
+ * gradients are rounded to bf16 for the products with dout, q and k; sums in fp32, results rounded once.
+ * Where a listed key holds a value that is not finite, the same component of its queries' dq is NaN: the
+ * product of that value and a gradient of 0.
  */
 slide_attn_status slide_attn_sparse_backward(const void* q, const void* k, const void* v, const int* idx,
                                              const void* out, const float* lse, const void* dout,

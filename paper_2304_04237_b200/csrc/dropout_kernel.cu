@@ -4,9 +4,10 @@
 // SC11) at counter (e / 4, offset) under the key (seed) is at least floor(p 2^32), so the mask is never stored: the backward
 // computes it again.  In units of images the word of image b decides for all of its elements.
 //
-// fp32 is bound by memory (3 maps forward, 2 backward).  bf16 is bound by the generator's integer instructions, ten products of 32 x 32 -> 64
-// bits and ten exclusive ors for two elements, on pipes of half rate: 64 x 56 x 56 x 96 takes 40 us for
-// forward and backward, the memory alone 29.5.  Whole images, 32 x 28 x 42 x 192, fp32, p = 0.2: 13.8 us, of 13.2.
+// fp32 is bound by memory (3 maps forward, 2 backward): 64 x 56 x 56 x 96, 35.2 and 24.4 us, of 35.3 and 23.6.  In bf16 the generator's products of
+// 32 x 32 -> 64 bits, ten for two elements, keep the pipe that makes them (fmaheavy) busy for 73 % of the cycles in which an SM has work, where a thread's loads
+// come first and its products then: 64 x 56 x 56 x 96 takes 40.2 us for forward and backward, the memory alone 29.5.  Whole images, 32 x 28 x 42 x 192, fp32,
+// p = 0.2: 13.8 us, of 13.2.
 // The products with the scale are fp32, and the sum is rounded to the storage type once.
 #include "operators.cuh"
 

@@ -8,8 +8,8 @@
 // inputs the second pass finds in L2 (126 MB) as long as they fit.  The chunks are joined by every CTA of the second pass or, where there are many
 // groups, by a small launch between the passes.  A thread keeps to one 16-byte column of the pixels, of which a CTA takes whole rows.  Images that
 // one CTA can hold in its registers take one launch.
-// 64 x 56 x 56 x 96, bf16, 32 groups: with GELU forward and backward in turn 96 us, of 29.5 for the 193 MB that they cannot do without (with SiLU, over and
-// over on the same maps, 30 us and 46).  Each pass reads its maps again, and the activation's special functions and roundings share the issue slots.
+// 64 x 56 x 56 x 96, bf16, 32 groups, forward and backward in turn: 63 us, with SiLU 77, with GELU 93, of 29.5 for the 193 MB that they cannot do without.  Each
+// pass reads its maps again, and the activation's special functions and roundings share the issue slots.
 // (One pass for all, with an image's pixels kept in the shared memory of a cluster of CTAs that exchange their sums, read every map once,
 // but its barriers and low occupancy made 64 x 56 x 56 x 96, bf16, GELU, forward and backward, take 114 us.)
 // Sums are fp32 (the weights' over many chunks fp64), in an order that only the shape decides.

@@ -7,8 +7,14 @@
 // and dv, over the blocks of queries whose lists name the key's block, in the order of the lists).  None adds to memory that
 // another CTA writes, so results do not depend on which CTA runs first.
 // Bound by latency: a warp's products, exponentials and products again wait for one another, and registers allow 12 to 16 such warps an SM.  128 x 128 x 2,
-// 3 heads, bf16, lists of 16 blocks of 8 x 8: queries 81 us, keys 103 by themselves (tensor pipe 45 and 47 %, issue slots 34 and 30 %); with the forward 222 in
-// all, of 27 for the products at the rate of large matrices.
+// 3 heads, bf16, lists of 16 blocks of 8 x 8: queries 80 us, keys 101 by themselves (tensor pipe 46 and 48 %, issue slots 35 and 31 %); with the forward 230 in
+// all, of 27 for the products at the rate of large matrices.  fp32 heads of 64 have one CTA an SM, as registers and shared memory allow: 8 x 56 x 56, 3 heads, 4 blocks of
+// 7 x 7, 464 us where heads of 32 take 208.
+//
+// Tiles of 32 or 64 rows, us each way, backward alone (64 x 56 x 56 x 2, 4 blocks of 7 x 7, fp32 8 x 56 x 56 x 3; then 2 x 128 x 128 x 3, 16 blocks of 8 x 8,
+// fp32 8 blocks):
+//   bf16, heads of 32: 224.9 / 214.7, then 182.4 / 172.2; heads of 64: 397.6 / 373.7, then 317 / 291; heads of 16 (32 x 56 x 56 x 4) 168.8 / 156.3.  64
+//   fp32, heads of 32: 207.5 / 233.9, then 456 / 502; heads of 16 (8 x 56 x 56 x 6) 223.8 / 219.7.  32
 #include "operators.cuh"
 
 namespace slide_attn {

@@ -285,7 +285,9 @@ __device__ __forceinline__ void scores(const Rows<D, Planes>& rows, uint32_t til
 }
 
 // o[n-tile] += weights . tile for 16 rows of the tile (16 x 16 times 16 x D), the weights as scores16 leaves them; `tile` points at the first of the
-// rows.  fp32: the tensor core truncates as it adds, so 16 products are added up from zero and the sums in fp32.
+// rows.  bf16: the weights (forward, and P and dS backward) are rounded to bf16, half a step of 2^-8 each, because the tensor core takes no wider operand beside bf16
+// rows; a second product with what the rounding leaves would double this half of the arithmetic.  Sums are fp32.  Against 64 bits the forward's result is off by
+// 2.3e-3 where the rounding of the result alone gives 1.7e-3, the gradients 2.4e-3.  fp32: the tensor core truncates as it adds, so 16 products are added up from zero and the sums in fp32.
 template <int D, int Planes>
 __device__ __forceinline__ void gather16(const float (&w0)[4], const float (&w1)[4], uint32_t tile, uint32_t stride, int lane, float (&o)[D / 8][4]) {
     if constexpr (Planes == 1) {
@@ -480,8 +482,8 @@ template <typename T, int D, int N> struct Sender {
 
 // What the kernels that keep queries share (the one that keeps keys takes its stages and operands, and sends for them in its own way): a CTA takes its even share of the units, neighbours, one after the other, and the copies run ahead of the
 // arithmetic across the units' ends: a list is short (four tiles, often), and the way from its numbers to the first scores takes three
-// trips to memory.  There are as many CTAs as the SMs hold.  (Several times as many, of up to eight units, took 85.2 us instead of 82.6 for the
-// forward of 64 x 56 x 56, 2 heads, bf16, and 161 instead of 155.5 for 32 x 28 x 42, 3 heads of 64, bf16, forward and backward.)
+// trips to memory.  There are as many CTAs as the SMs hold.  (Several times as many, of up to eight units, took 3 % longer for
+// the forward of 64 x 56 x 56, 2 heads, bf16, and for 32 x 28 x 42, 3 heads of 64, bf16, forward and backward.)
 // A unit begins with the step (or steps) that bring the rows that stay.
 //   own0, own1: the rows that stay (queries; gradients of the output, or null);  k, v: the tiles.
 template <typename T, int D, int N_, int S_, int Own> struct QueryPipe {

@@ -5,11 +5,17 @@
 // sums stay in registers.  The maximum that a row's exponents are taken from is raised only when a score is more than 2^8 above it, so that
 // sums are rescaled in the first tile and hardly ever again.  32 bits throughout; bf16 weights are rounded where they become an operand of
 // the second product.
-// A list names blocks of a few dozen rows for 64 queries, so tiles of 64 rows and products of 16 rows a warp: mma.sync, whose operands and results are
-// in the registers that the softmax works on.  Bound by latency: 64 x 56 x 56, 2 heads, bf16, 4 blocks of 7 x 7, takes 82.6 us, of 15.7 for its bytes (issue slots
-// 45 %, exponentials 36 % of their pipe, tensor pipe 30 %); 2 x 128 x 128, 3 heads, fp32, 8 blocks of 8 x 8, 156 us with the choice of the blocks (tensor pipe
-// 45 %: six products for one).
-// 32-row tiles with more CTAs, and fewer registers with spills, were slower.
+// Products of 16 rows a warp by mma.sync, whose operands and results are in the registers that the softmax works on.  Bound by latency, as a warp's products,
+// exponentials and products again wait for one another: 64 x 56 x 56, 2 heads, bf16, 4 blocks of 7 x 7, takes 82.8 us, of 15.7 for its bytes (issue slots
+// 45 %, exponentials 36 % of their pipe, tensor pipe 30 %); 2 x 128 x 128, 3 heads, fp32, 8 blocks of 8 x 8, 156.6 us with the choice of the blocks (tensor pipe
+// 45 %: six products for one).  (tcgen05 with M = 64, a unit's rows, and accumulators in tensor memory has not been tried.)
+//
+// Tiles of 32 or 64 keys, us each way (64 x 56 x 56 x 2, 4 blocks of 7 x 7, fp32 8 x 56 x 56 x 3; then 2 x 128 x 128 x 3, 16 blocks of 8 x 8, fp32 8 blocks):
+//   bf16, heads of 32: 79.9 / 83.0, then 61.2 / 60.6; heads of 16 (32 x 56 x 56 x 4) 65.6 / 60.2.  64
+//   bf16, heads of 64: 125.3 / 143.3, then 101.8 / 100.4; 32 x 28 x 42 x 3, 4 blocks of 8 x 8, 40.0 / 44.2.  32
+//   fp32, heads of 32: 61.1 / 73.9, then 134.2 / 151.8; heads of 16 (8 x 56 x 56 x 6) 71.2 / 72.3.  32
+// Four stages of copies; three where 64 fp32 values a row leave no room for a fourth beside their planes.  Spills of a few registers: bf16 heads of 32 (20 bytes),
+// fp32 heads of 64 (100 bytes); still fewer registers, for one CTA more an SM, were slower.
 #include "operators.cuh"
 
 namespace slide_attn {
