@@ -349,8 +349,8 @@ typedef enum {
  *   workspace    slide_attn_group_norm_workspace bytes with backward = 0; may be NULL where that is 0 (small images)
  * Arithmetic is fp32 (the variance from deviations from the mean, so that a large mean costs nothing);
  * y is rounded to the dtype once.  GELU's integral is held to 1.3e-7 of itself, also where it is small; of
- * bf16 maps to 1.1e-7 or 1.1e-4 of itself, whichever is less.  Supported: C a multiple of 8 and of groups, up to 4096 (bf16) or
- * 2048 (fp32); eps >= 0.
+ * bf16 maps to 1.1e-7 or 1.1e-4 of itself, whichever is less.  Supported: C a multiple of 8 and of groups,
+ * up to 4096 (bf16) or 2048 (fp32); eps >= 0.
  */
 slide_attn_status slide_attn_group_norm_forward(const void* x, const float* gamma, const float* beta,
                                                 void* y, float* mean, float* rstd,

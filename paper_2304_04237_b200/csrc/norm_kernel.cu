@@ -26,7 +26,8 @@ constexpr int kTogether = 4;           // 16-byte pieces that a thread works on 
 constexpr int kForwardCtas = 4, kBackwardCtas = 3;     // of 256 threads on an SM, as registers allow
 constexpr int kPair = kTogether / 2;
 constexpr int kOnce = 8;               // rounds of an image that one CTA keeps
-constexpr long long kSms = 148;        // that chunks are made for.  B200's, whatever device is current, so that the workspace and the order of the sums depend on the shape alone
+constexpr long long kSms = 148;        // that chunks are made for: B200's, whatever device is current, so that the workspace and the order of the sums depend on
+                                       // the shape alone
 
 struct NormShape {
     int P, C, groups, per_group;       // per_group: channels of a group
@@ -619,8 +620,8 @@ __device__ __forceinline__ void sum_weights(const NormArgs& a, int C, double (*p
     }
 }
 
-// Second pass, backward.  Its first CTAs add up the weights' gradients beside it, which need nothing of it: 64 x 56 x 56 x 96, bf16, forward and backward 90.7 us,
-// of some 95 with a launch of their own behind it.
+// Second pass, backward.  Its first CTAs add up the weights' gradients beside it, which need nothing of it: 64 x 56 x 56 x 96, bf16, GELU, forward and backward
+// 93.4 us, some 4 more with a launch of their own behind it.
 template <int Threads, typename T, int Act>
 __global__ void __launch_bounds__(Threads, kBackwardCtas * 256 / Threads) norm_backward_kernel(const NormArgs a, const NormShape s)
 {
